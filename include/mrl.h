@@ -6,7 +6,9 @@
  * sampled tokens under the learner (LM-head projection, log-softmax over the
  * full vocabulary, gather at the target id), group-relative advantages, the
  * clipped importance-ratio surrogate with a KL term to a reference policy,
- * and the backward pass to the hidden states and the LM-head weight.
+ * and the backward pass to the hidden states and the LM-head weight; and what stands
+ * around that in a training step: the norm that makes the hidden states, its
+ * backward pass, the clipping of the gradients and the AdamW update.
  *
  * Conventions for every entry point
  *   - Returns an mrl_status (0 = MRL_OK, negative = error).  Never throws,
@@ -22,7 +24,8 @@
  *     valid once the caller has synchronised that stream.  No host
  *     synchronisation happens inside a call (debug_sync of call (3) excepted).
  *   - Inputs are never modified.  Outputs are fully overwritten, except
- *     out_dW when accumulate_dw = 1.
+ *     out_dW (out_dweight) when accumulate_dw = 1.  (Call (8) updates in place, and calls (5) and (6) may be given
+ *     an output that is one of their inputs.)
  *   - All tensors are dense and row-major.  lm_head_w is [V, d], one row per
  *     vocabulary id (the layout of a linear layer's weight).  Row n of hidden
  *     is the final hidden state that PREDICTS target_ids[n]; the shift
@@ -61,7 +64,11 @@ typedef enum {
                                     than the library's built-in buffer holds                      */
 } mrl_status;
 
-typedef enum { MRL_F32 = 0, MRL_BF16 = 1 } mrl_dtype;
+typedef enum {
+  MRL_F32 = 0,
+  MRL_BF16 = 1,
+  MRL_E4M3 = 2 /* 8 bits, OCP e4m3 (no infinities, largest value 448), next to float scales: outputs of call (5), moments of call (8) */
+} mrl_dtype;
 
 typedef enum {
   MRL_ADV_CENTER = 0,   /* A = r - mean(group)                     (Sec. 3, A-tilde)            */
@@ -321,6 +328,118 @@ int mrl_thl_word_align(const float* src_logp /*[B,S_src] dev*/, const uint8_t* s
                        const int32_t* tgt_map_len /*[B] dev*/, int64_t B, int32_t S_src, int32_t S_tgt,
                        int32_t max_words, float ignore_value, float* out /*[B,S_tgt] dev*/,
                        int64_t* out_bad_words /*[1] dev | NULL*/, void* stream);
+
+/* ------------------------------------------------------------------------
+ * (5) Root-mean-square norm of hidden states, with the residual's addition: what makes the
+ *     `hidden` of calls (1) and (3), or with 8-bit outputs the input of a layer that multiplies
+ *     8-bit rows.
+ *
+ *   h[n, :] = x[n, :] + residual[n, :]            (residual NULL: h = x)
+ *   y[n, k] = h[n, k] / sqrt(mean_k h[n, k]^2 + eps) * weight[k]
+ *
+ *   x_dtype, weight_dtype: MRL_F32 or MRL_BF16; residual_dtype: that of x or MRL_F32 (a residual
+ *   stream in 32 bits).  Sums, norms and products are in fp32; the norm is that of the unrounded h.
+ *   out_sum [N, d], the type of residual: h.  Required with a residual, NULL without.
+ *   out_y [N, d], y_dtype MRL_F32, MRL_BF16 or MRL_E4M3.  MRL_E4M3: out_y holds codes q and out_scale
+ *   the floats they are multiplied by, scale = max(max |y|, 2^-100) / 448 over the row
+ *   (scale_block = 0, out_scale [N]) or over every 128 columns (scale_block = 128,
+ *   out_scale [N, ceil(d / 128)]), q = y / scale rounded to nearest even.  A NaN among them makes the scale
+ *   NaN, an infinity makes it infinite.  Other types: out_scale NULL, scale_block 0.
+ *   token_mask [N] or NULL: rows with mask 0 are not read; their h and y are zero, their scales
+ *   those of a zero row.
+ *   Any d from 1 to 16384, any alignment that the types have.  N = 0 is a no-op.  The mean square is
+ *   taken in fp32: entries beyond 1e19 overflow it.
+ *   out_sum may be the buffer of residual or x, out_y that of x, where the types have the same size.
+ *   A row's results do not depend on what other rows hold.  eps > 0.
+ * ---------------------------------------------------------------------- */
+int mrl_rms_norm(const void* x /*[N,d] dev*/, const void* residual /*[N,d] dev | NULL*/, const void* weight /*[d] dev*/,
+                 const uint8_t* token_mask /*[N] dev | NULL*/, int64_t N, int32_t d, float eps,
+                 int32_t x_dtype, int32_t residual_dtype, int32_t weight_dtype, int32_t y_dtype, int32_t scale_block,
+                 void* out_sum /*[N,d] dev | NULL*/, void* out_y /*[N,d] dev*/, float* out_scale /*dev | NULL*/, void* stream);
+
+/* ------------------------------------------------------------------------
+ * (6) Backward pass of call (5), from out_dH of call (3) as a rule.
+ *
+ *   g = dy * weight,  r = 1 / sqrt(mean h^2 + eps),  u = h r
+ *   out_dx = r (g - u mean(g u)) + d_residual      the gradient of x and of residual alike
+ *   out_dweight[k] = (or +=) sum_n dy[n, k] u[n, k]
+ *
+ *   h: what was normalised, out_sum or, without a residual, x.  r is taken from it again (a sum
+ *   over values in registers; no statistic is kept).  d_residual [N, d], h's type, or NULL: what the residual stream
+ *   brings to h from further on.  dy_dtype, h_dtype, weight_dtype, dx_dtype: MRL_F32 or MRL_BF16 each.
+ *   token_mask: rows with mask 0 add nothing to out_dweight and neither dy nor h is read there; their
+ *   out_dx is d_residual, or zero.
+ *   out_dweight [d] float, or NULL to skip it; accumulate_dw = 1 adds into it.  Sums over rows have a fixed
+ *   order: bit-reproducible.  The workspace is needed with out_dweight only; a smaller one is refused.
+ *   out_dx may be the buffer of dy, h or d_residual where the types have the same size.
+ * ---------------------------------------------------------------------- */
+size_t mrl_rms_norm_backward_workspace(int64_t N, int32_t d);
+int mrl_rms_norm_backward(const void* dy /*[N,d] dev*/, const void* h /*[N,d] dev*/, const void* weight /*[d] dev*/,
+                          const void* d_residual /*[N,d] dev | NULL*/, const uint8_t* token_mask /*[N] dev | NULL*/,
+                          int64_t N, int32_t d, float eps, int32_t dy_dtype, int32_t h_dtype, int32_t weight_dtype, int32_t dx_dtype,
+                          int32_t accumulate_dw, void* out_dx /*[N,d] dev*/, float* out_dweight /*[d] dev | NULL*/,
+                          void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * (7), (8) The update: global norm of the gradients with the clip coefficient, and AdamW, over
+ *     any number of tensors at once (the head's out_dW, the norm's out_dweight, and whatever else
+ *     the caller trains).
+ *
+ * One mrl_param_tensor for each, in HOST memory; it is read during the call only.  Device
+ * pointers need the alignment of their type.  Tensors with n = 0 are skipped.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  float* param;        /* [n] float: the weights (what an update adds is far below half a step of a 16-bit weight at the
+                          learning rates of policy training: 1e-6 against 2^-9 of the weight, so 16 bits alone would not move) */
+  void* copy;          /* [n] bfloat16 | NULL: the new weights rounded to nearest, for the next scoring pass */
+  const void* grad;    /* [n], grad_dtype */
+  void* m;             /* [n] first moment: float, or e4m3 codes */
+  void* v;             /* [n] second moment: float, or e4m3 codes of its square root */
+  float* m_scale;      /* state_dtype MRL_E4M3: [ceil(n / 256)], one for every 256 elements; else unused */
+  float* v_scale;
+  int64_t n;
+  float weight_decay;  /* >= 0; decoupled */
+  int32_t grad_dtype;  /* MRL_F32 or MRL_BF16 */
+} mrl_param_tensor;
+
+/* (7)  out_norm_coef[0] = norm = sqrt(sum over all tensors of grad^2), in fp64 and in a fixed order,
+ *      out_norm_coef[1] = min(1, max_norm / norm): the factor that clips the gradients to max_norm
+ *      (> 0, infinity allowed).  NaN where the norm is not finite.  Of each tensor grad, n and grad_dtype are used. */
+size_t mrl_grad_norm_workspace(const mrl_param_tensor* tensors /*host*/, int32_t count);
+int mrl_grad_norm(const mrl_param_tensor* tensors /*host*/, int32_t count, double max_norm,
+                  float* out_norm_coef /*[2] dev*/, void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
+/* (8)  g = grad * *grad_coef,   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,
+ *      param -= lr (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + weight_decay param),   copy = bf16(param)
+ *      in fp32 from the unrounded moments.  grad_coef [1]: out_norm_coef + 1 of call (7), or NULL for 1.
+ *
+ *      state_dtype MRL_E4M3 keeps a quarter of the moments' bytes.  Every 256 elements of a tensor (the last
+ *      block may be shorter) share a scale, max(largest magnitude, 2^-100) / 448, of m and of sqrt(v): the square root
+ *      halves the binades that v spans, so that the 17.8 of e4m3 hold gradients of that range.
+ *      Codes are rounded at random, up with the probability of the fraction: b2 = 0.999 moves sqrt(v) by 0.05 %
+ *      a step where codes are 6 - 12 % apart, so rounded to nearest it would stay for good.  A positive
+ *      sqrt(v) keeps a positive code.  The random bits of element i of tensor j (its place in `tensors`) are
+ *      mix(lo(i) ^ mix(key + hi(i))), key = mix(lo(seed) ^ mix(hi(seed) ^ mix(lo(t) ^ mix(j)))), with
+ *      mix(x): x = (x ^ x >> 16) * 0x6A09E667, x = (x ^ x >> 15) * 0xBB67AE85, x ^ x >> 16 on 32 bits, lo and hi the
+ *      32-bit halves; the low 16 bits serve m, the high 16 sqrt(v).  The same seed gives the same bits.
+ *      A gradient that is not finite makes its block of 8-bit moments NaN; with 32-bit moments its element.
+ *      The buffers of all tensors are updated in place and must not overlap: mrl_adamw_check says whether they do. */
+typedef struct {
+  double lr, beta1, beta2, eps;  /* lr >= 0; 0 <= beta < 1; eps >= 1e-30 */
+  int64_t step;                  /* t, from 1 */
+  uint64_t seed;                 /* of the roundings to 8 bits */
+  int32_t state_dtype;           /* MRL_F32 or MRL_E4M3 */
+  int32_t skip_nonfinite;        /* 1: where *grad_coef is not finite, nothing is written */
+  const float* lr_dev;           /* [1] dev | NULL: learning rate, in place of lr (a captured graph replays
+                                    with what these two hold by then) */
+  const int64_t* step_dev;       /* [1] dev | NULL: t, in place of step (values below 1 count as 1) */
+} mrl_adamw_config;
+int mrl_adamw(const mrl_param_tensor* tensors /*host*/, int32_t count, const mrl_adamw_config* cfg /*host*/,
+              const float* grad_coef /*[1] dev | NULL*/, void* stream);
+
+/* Checks what mrl_adamw checks of the tensors and, beyond that, that no two of the buffers it writes overlap and none holds a gradient
+ * (MRL_ERR_CONFIG).  Host only, once for a set of tensors: it sorts them, which takes longer than a small update. */
+int mrl_adamw_check(const mrl_param_tensor* tensors /*host*/, int32_t count, int32_t state_dtype);
 
 #ifdef __cplusplus
 }

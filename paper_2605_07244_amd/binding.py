@@ -13,12 +13,12 @@ import ctypes
 import importlib.util
 import os
 import warnings
-from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 from dataclasses import dataclass
 
 import torch
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 ADV_CENTER, ADV_GROUP_ZN, ADV_BATCH_ZN = 0, 1, 2
 PROF_CLASSES = ("prep", "adv", "gemm_fwd", "row_epilogue", "operand_prep", "gemm_dh", "gemm_dw", "final")
 
@@ -41,6 +41,16 @@ class _LossConfig(ctypes.Structure):
                 ("sgt_lambda", c_float), ("loss_agg", c_int32), ("accumulate_dw", c_int32),
                 ("dh_dtype", c_int32), ("chunk_rows", c_int32), ("scored_rows_hint", c_int64),
                 ("ratio_level", c_int32), ("debug_sync", c_int32)]
+
+
+class _ParamTensor(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("copy", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p),
+                ("v_scale", c_void_p), ("n", c_int64), ("weight_decay", c_float), ("grad_dtype", c_int32)]
+
+
+class _AdamWConfig(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("step", c_int64), ("seed", c_uint64),
+                ("state_dtype", c_int32), ("skip_nonfinite", c_int32), ("lr_dev", c_void_p), ("step_dev", c_void_p)]
 
 
 @dataclass
@@ -113,6 +123,20 @@ def lib() -> ctypes.CDLL:
     L.mrl_thl_word_align.restype = c_int
     L.mrl_thl_word_align.argtypes = [c_void_p] * 7 + [c_int64, c_int32, c_int32, c_int32, c_float, c_void_p,
                                                       c_void_p, c_void_p]
+    L.mrl_rms_norm.restype = c_int
+    L.mrl_rms_norm.argtypes = [c_void_p] * 4 + [c_int64, c_int32, c_float] + [c_int32] * 5 + [c_void_p] * 4
+    L.mrl_rms_norm_backward_workspace.restype = c_size_t
+    L.mrl_rms_norm_backward_workspace.argtypes = [c_int64, c_int32]
+    L.mrl_rms_norm_backward.restype = c_int
+    L.mrl_rms_norm_backward.argtypes = [c_void_p] * 5 + [c_int64, c_int32, c_float] + [c_int32] * 5 + [c_void_p] * 3 + [c_size_t, c_void_p]
+    L.mrl_grad_norm_workspace.restype = c_size_t
+    L.mrl_grad_norm_workspace.argtypes = [POINTER(_ParamTensor), c_int32]
+    L.mrl_grad_norm.restype = c_int
+    L.mrl_grad_norm.argtypes = [POINTER(_ParamTensor), c_int32, c_double, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.mrl_adamw.restype = c_int
+    L.mrl_adamw.argtypes = [POINTER(_ParamTensor), c_int32, POINTER(_AdamWConfig), c_void_p, c_void_p]
+    L.mrl_adamw_check.restype = c_int
+    L.mrl_adamw_check.argtypes = [POINTER(_ParamTensor), c_int32, c_int32]
     L.mrl_diag_dw_tail_plan.restype = c_int
     L.mrl_diag_dw_tail_plan.argtypes = [c_int32, c_int32, POINTER(c_int32)]
     L.mrl_diag_gemm_cut.restype = c_int
@@ -130,7 +154,7 @@ _HOST = None
 
 class _NoHost:
     """Takes nothing as it is: every call goes through ctypes."""
-    advantages = align = staticmethod(lambda *args: None)
+    advantages = align = rms_norm = rms_norm_backward = staticmethod(lambda *args: None)
 
 
 def _load_host():
@@ -146,7 +170,7 @@ def _load_host():
         why = f"was built against torch {module.torch_version}, this is {torch.__version__}"
     except (ImportError, OSError) as e:        # (a file that is not there is an ImportError or FileNotFoundError)
         why = str(e)
-    warnings.warn(f"{path}: {why}; advantages and alignment go through ctypes, which takes 4 - 5 us more a call "
+    warnings.warn(f"{path}: {why}; advantages, alignment and norms go through ctypes, which takes 4 - 5 us more a call "
                   "(`python -m paper_2605_07244_amd.build` builds it)", RuntimeWarning, stacklevel=4)
     return None
 
@@ -411,3 +435,206 @@ def thl_word_align(src_logp, src_mask, src_word_map, src_map_len, tgt_mask, tgt_
         _ptr(tgt_map_len, torch.int32, "tgt_map_len"), B, S_src, S_tgt, int(max_words), float(ignore_value),
         _ptr(out), _ptr(bad) if bad is not None else None, _stream()), "mrl_thl_word_align")
     return out, bad
+
+
+def _here(*tensors):
+    """The device that the tensors are on: the current one, on whose stream a call runs."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device (cuda:{dev}), got one on {t.device}")
+
+
+def _float_code(t, name):
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return _dtype_code(t)
+
+
+def _shaped(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+
+
+def rms_norm(x, weight, eps=1e-6, residual=None, token_mask=None, out_dtype=None, scale_block=0):
+    """mrl_rms_norm: (y [N, d], h [N, d] or None, scale or None) of x [N, d].  h = x + residual is returned with a residual, in
+    its type; out_dtype float8_e4m3fn (None: the type of x) makes y codes, to be multiplied by scale [N] or, with
+    scale_block = 128, by scale [N, ceil(d / 128)]."""
+    if _native and type(x) is torch.Tensor and x.is_cuda:
+        dev = _get_device()
+        r = (_HOST or _host()).rms_norm(x, weight, eps, residual, token_mask, x.dtype if out_dtype is None else out_dtype, scale_block, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_rms_norm")
+            return r[1:]
+    out_dtype = x.dtype if out_dtype is None else out_dtype
+    codes = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}
+    if out_dtype not in codes:
+        raise TypeError(f"out_dtype must be float32, bfloat16 or float8_e4m3fn, got {out_dtype}")
+    if x.dim() != 2:
+        raise ValueError("x must be [N, d]")
+    N, d = x.shape
+    _shaped(weight, (d,), "weight")
+    _shaped(residual, (N, d), "residual")
+    if token_mask is not None and token_mask.numel() != N:
+        raise ValueError("token_mask must have N entries")
+    xt, wt = _float_code(x, "x"), _float_code(weight, "weight")
+    rt = _float_code(residual, "residual") if residual is not None else F32
+    args = [_ptr(x, name="x"), _ptr(residual, name="residual"), _ptr(weight, name="weight"), _ptr(token_mask, torch.uint8, "token_mask")]
+    _here(x, residual, weight, token_mask)
+    y = torch.empty((N, d), dtype=out_dtype, device=x.device)
+    h = torch.empty((N, d), dtype=residual.dtype, device=x.device) if residual is not None else None
+    scale = torch.empty((N, -(-d // scale_block)) if scale_block > 0 else (N,), dtype=torch.float32, device=x.device) if out_dtype == torch.float8_e4m3fn else None
+    _check(lib().mrl_rms_norm(*args, N, d, float(eps), xt, rt, wt, codes[out_dtype], int(scale_block), _ptr(h), _ptr(y), _ptr(scale), _stream()),
+           "mrl_rms_norm")
+    return y, h, scale
+
+
+def rms_norm_backward(dy, h, weight, eps=1e-6, d_residual=None, token_mask=None, dx_dtype=None, out_dweight=None, accumulate=False,
+                      want_dweight=True, workspace=None):
+    """mrl_rms_norm_backward: (dx [N, d] in dx_dtype (None: the type of h), dweight [d] float32 or None).  h is what rms_norm returned as h
+    or, without a residual, its x; accumulate adds into out_dweight."""
+    if dx_dtype is None:
+        dx_dtype = h.dtype
+    if _native and type(h) is torch.Tensor and h.is_cuda:
+        dev = _get_device()
+        r = (_HOST or _host()).rms_norm_backward(dy, h, weight, eps, d_residual, token_mask, dx_dtype, out_dweight, accumulate, want_dweight,
+                                                 workspace, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_rms_norm_backward")
+            return r[1:]
+    if dx_dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"dx_dtype must be float32 or bfloat16, got {dx_dtype}")
+    if h.dim() != 2:
+        raise ValueError("h must be [N, d]")
+    N, d = h.shape
+    _shaped(dy, (N, d), "dy")
+    _shaped(weight, (d,), "weight")
+    _shaped(d_residual, (N, d), "d_residual")
+    _shaped(out_dweight, (d,), "out_dweight")
+    if token_mask is not None and token_mask.numel() != N:
+        raise ValueError("token_mask must have N entries")
+    if d_residual is not None and d_residual.dtype != h.dtype:
+        raise TypeError("d_residual must have the dtype of h")
+    if accumulate and out_dweight is None:
+        raise ValueError("accumulate needs out_dweight")
+    types = [_float_code(dy, "dy"), _float_code(h, "h"), _float_code(weight, "weight"), F32 if dx_dtype == torch.float32 else BF16]
+    args = [_ptr(dy, name="dy"), _ptr(h, name="h"), _ptr(weight, name="weight"), _ptr(d_residual, name="d_residual"),
+            _ptr(token_mask, torch.uint8, "token_mask")]
+    dw_ptr = _ptr(out_dweight, torch.float32, "out_dweight")
+    _here(dy, h, weight, d_residual, token_mask, out_dweight, workspace)
+    dx = torch.empty((N, d), dtype=dx_dtype, device=h.device)
+    if out_dweight is None and want_dweight:
+        out_dweight = torch.empty(d, dtype=torch.float32, device=h.device)
+        dw_ptr = out_dweight.data_ptr()
+    if workspace is None and out_dweight is not None:
+        workspace = _workspace(lib().mrl_rms_norm_backward_workspace(N, d), h.device)
+    _check(lib().mrl_rms_norm_backward(*args, N, d, float(eps), *types, int(bool(accumulate)), _ptr(dx), dw_ptr, _ptr(workspace, torch.uint8, "workspace"),
+                                       workspace.numel() if workspace is not None else 0, _stream()), "mrl_rms_norm_backward")
+    return dx, out_dweight
+
+
+STATE_BLOCK = 256              # elements of a tensor that share the scales of 8-bit moments
+
+
+class GradPlan:
+    """The gradients of a set of tensors, laid out for grad_norm: built once, good for as long as the tensors keep their memory (which the
+    plan holds on to).  Calls with one plan share its workspace: they belong on one stream, or must be ordered."""
+
+    def __init__(self, grads):
+        self.grads = list(grads)
+        self._fill(len(self.grads))
+        for row, g in zip(self.table, self.grads):
+            row.n, row.grad, row.grad_dtype = g.numel(), _ptr(g, name="grad"), _float_code(g, "grad")
+        _here(*self.grads)
+        self.device = self.grads[0].device if self.grads else torch.device("cuda", torch.cuda.current_device())
+        self.workspace = _workspace(lib().mrl_grad_norm_workspace(self.table, self.count), self.device)
+
+    def _fill(self, count):
+        self.count, self.table = count, (_ParamTensor * count)()
+
+
+class AdamWPlan(GradPlan):
+    """Parameters, gradients and moments of a set of tensors, laid out for adamw_step (and grad_norm); see adamw_plan.  m, v, m_scale and
+    v_scale are its lists of moments, updated in place: what a checkpoint saves and a new plan is given."""
+
+    def __init__(self, params, grads, copies, m, v, m_scale, v_scale, state_dtype, weight_decay):
+        super().__init__(grads)
+        if state_dtype not in (torch.float32, torch.float8_e4m3fn):
+            raise TypeError(f"state_dtype must be float32 or float8_e4m3fn, got {state_dtype}")
+        codes = state_dtype == torch.float8_e4m3fn
+        self.state_dtype, self.params = E4M3 if codes else F32, list(params)
+        sizes = [g.numel() for g in self.grads]
+
+        def of(given, dtype, sizes, name):
+            if given is None:
+                return [torch.zeros(n, dtype=dtype, device=self.device) for n in sizes]
+            given = list(given)
+            if [t.numel() for t in given] != sizes:
+                raise ValueError(f"{name} must hold a tensor for each of {len(sizes)}, of their sizes")
+            return given
+
+        if [p.numel() for p in self.params] != sizes:
+            raise ValueError("params and grads must be as many, and of the same sizes")
+        self.copies = None if copies is None else of(copies, torch.bfloat16, sizes, "copies")
+        self.m, self.v = of(m, state_dtype, sizes, "m"), of(v, state_dtype, sizes, "v")
+        blocks = [-(-n // STATE_BLOCK) for n in sizes]
+        self.m_scale, self.v_scale = (of(x, torch.float32, blocks, name) if codes else None for x, name in ((m_scale, "m_scale"), (v_scale, "v_scale")))
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * self.count
+        if len(decay) != self.count:
+            raise ValueError("weight_decay must be a number or one for each tensor")
+        for i, row in enumerate(self.table):
+            row.param, row.m, row.v = (_ptr(t[i], dt, name) for t, dt, name in
+                                       ((self.params, torch.float32, "param"), (self.m, state_dtype, "m"), (self.v, state_dtype, "v")))
+            row.copy = _ptr(self.copies[i], torch.bfloat16, "copy") if self.copies is not None else None
+            if codes:
+                row.m_scale, row.v_scale = (_ptr(t[i], torch.float32, name) for t, name in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")))
+            row.weight_decay = decay[i]
+        _here(*self.params, *(self.copies or []), *self.m, *self.v, *(self.m_scale or []), *(self.v_scale or []))
+        _check(lib().mrl_adamw_check(self.table, self.count, self.state_dtype), "mrl_adamw_check")
+
+
+def grad_plan(grads) -> GradPlan:
+    """A plan of gradients (float32 or bfloat16) for grad_norm."""
+    return GradPlan(grads)
+
+
+def adamw_plan(params, grads, copies=None, m=None, v=None, m_scale=None, v_scale=None, state_dtype=None, weight_decay=0.01) -> AdamWPlan:
+    """A plan for adamw_step: params float32 tensors, grads (float32 or bfloat16) the buffers that their gradients are written to, copies
+    the bfloat16 tensors that new weights are copied to, or None.  Moments that are not given start at zero, in state_dtype: float32 (the default, or that
+    of m) or float8_e4m3fn.  weight_decay: a number, or one for each tensor."""
+    if state_dtype is None:
+        m = None if m is None else list(m)
+        state_dtype = m[0].dtype if m else torch.float32
+    return AdamWPlan(params, grads, copies, m, v, m_scale, v_scale, state_dtype, weight_decay)
+
+
+def grad_norm(plan: GradPlan, max_norm: float = float("inf"), out=None):
+    """mrl_grad_norm: a float32 tensor [norm, clip coefficient] of the plan's gradients (not synchronised)."""
+    if out is None:
+        out = torch.empty(2, dtype=torch.float32, device=plan.device)
+    elif out.numel() != 2:
+        raise ValueError("out must have two entries")
+    _here(out, plan.workspace)
+    _check(lib().mrl_grad_norm(plan.table, plan.count, float(max_norm), _ptr(out, torch.float32, "out"), plan.workspace.data_ptr(),
+                               plan.workspace.numel(), _stream()), "mrl_grad_norm")
+    return out
+
+
+def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm_coef=None, seed=0, skip_nonfinite=False):
+    """mrl_adamw: updates the plan's params, moments and copies in place.  step counts from 1.  lr and step are numbers or, for graphs that are
+    replayed with other values, tensors of one float32 and one int64 on the GPU.  norm_coef: what grad_norm returned, whose coefficient the gradients
+    are multiplied by; skip_nonfinite leaves everything as it is where that is not finite."""
+    c = _AdamWConfig(0.0, beta1, beta2, eps, 1, int(seed) & 0xFFFFFFFFFFFFFFFF, plan.state_dtype, int(bool(skip_nonfinite)), None, None)
+    for name, x, dtype in (("lr", lr, torch.float32), ("step", step, torch.int64)):
+        if isinstance(x, torch.Tensor):
+            if x.numel() != 1:
+                raise ValueError(f"{name} must have one entry")
+            setattr(c, name + "_dev", _ptr(x, dtype, name))
+            _here(x)
+        else:
+            setattr(c, name, x)
+    if norm_coef is not None and norm_coef.numel() != 2:
+        raise ValueError("norm_coef must have two entries")
+    coef = None if norm_coef is None else _ptr(norm_coef, torch.float32, "norm_coef") + 4
+    _here(norm_coef, plan.workspace)
+    _check(lib().mrl_adamw(plan.table, plan.count, ctypes.byref(c), coef, _stream()), "mrl_adamw")

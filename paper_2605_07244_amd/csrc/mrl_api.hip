@@ -346,7 +346,7 @@ const char* mrl_status_string(int status) {
   }
 }
 
-int mrl_version(void) { return 100; }
+int mrl_version(void) { return 101; }
 
 int mrl_profile_enable(int on) {
   std::lock_guard<std::mutex> lk(g_prof_mu);

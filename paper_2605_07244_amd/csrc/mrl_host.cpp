@@ -9,6 +9,7 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/mrl.h"
@@ -122,9 +123,116 @@ PyObject* align(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// A tensor argument of one of the types that calls (5) and (6) take, on the given device; its shape is checked by the caller.
+bool typed_arg(PyObject* o, int64_t device, const at::Tensor** t, int32_t* type) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& x = THPVariable_Unpack(o);
+  if (!x.is_cuda() || !x.is_contiguous() || x.get_device() != device) return false;
+  if (x.scalar_type() == at::kBFloat16) *type = MRL_BF16;
+  else if (x.scalar_type() == at::kFloat) *type = MRL_F32;
+  else return false;
+  *t = &x;
+  return true;
+}
+bool same_rows(const at::Tensor& a, const at::Tensor& b) { return a.dim() == 2 && a.size(0) == b.size(0) && a.size(1) == b.size(1); }
+bool mask_arg(PyObject* o, int64_t device, int64_t N, const uint8_t** mask) {
+  void* p;
+  if (!tensor_arg(o, at::kByte, true, &p)) return false;
+  if (o != Py_None && (THPVariable_Unpack(o).numel() != N || THPVariable_Unpack(o).get_device() != device)) return false;
+  *mask = static_cast<const uint8_t*>(p);
+  return true;
+}
+
+// (x, weight, eps, residual, token_mask, out_dtype, scale_block, device, stream) -> (status, y, h or None, scale or None) or None
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    const at::Tensor *x, *w, *res = nullptr;
+    int32_t xt, wt, rt = MRL_F32, yt, block;
+    int64_t device, stream;
+    float eps;
+    const uint8_t* mask;
+    if (n != 9 || !int_arg(a[7], &device) || !int_arg(a[8], &stream) || !typed_arg(a[0], device, &x, &xt) || !typed_arg(a[1], device, &w, &wt) ||
+        !float_arg(a[2], &eps) || (a[3] != Py_None && !typed_arg(a[3], device, &res, &rt)) || x->dim() != 2 || x->numel() == 0 ||
+        !mask_arg(a[4], device, x->size(0), &mask) || !THPDtype_Check(a[5]) || !int32_arg(a[6], &block) || x->size(1) > INT32_MAX ||
+        w->dim() != 1 || w->size(0) != x->size(1) || (res != nullptr && !same_rows(*res, *x)) || (block != 0 && block != 128))
+      Py_RETURN_NONE;
+    const at::ScalarType out = reinterpret_cast<THPDtype*>(a[5])->scalar_type;
+    if (out == at::kFloat) yt = MRL_F32;
+    else if (out == at::kBFloat16) yt = MRL_BF16;
+    else if (out == at::kFloat8_e4m3fn) yt = MRL_E4M3;
+    else Py_RETURN_NONE;
+    const int64_t N = x->size(0), d = x->size(1);
+    at::Tensor y = new_like(*x, {N, d}, out), h, scale;
+    if (res != nullptr) h = new_like(*x, {N, d}, res->scalar_type());
+    if (yt == MRL_E4M3) scale = block != 0 ? new_like(*x, {N, (d + block - 1) / block}, at::kFloat) : new_like(*x, {N}, at::kFloat);
+    const void *xp = x->const_data_ptr(), *wp = w->const_data_ptr(), *rp = res != nullptr ? res->const_data_ptr() : nullptr;
+    void *yp = y.mutable_data_ptr(), *hp = h.defined() ? h.mutable_data_ptr() : nullptr;
+    float* const sp = scale.defined() ? static_cast<float*>(scale.mutable_data_ptr()) : nullptr;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_rms_norm(xp, rp, wp, mask, N, (int32_t)d, eps, xt, rt, wt, yt, block, hp, yp, sp, reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iNNN)", rc, THPVariable_Wrap(std::move(y)), THPVariable_Wrap(std::move(h)), THPVariable_Wrap(std::move(scale)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// (dy, h, weight, eps, d_residual, token_mask, dx_dtype, out_dweight, accumulate, want_dweight, workspace, device, stream)
+// -> (status, dx, dweight or None) or None
+PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    const at::Tensor *dy, *h, *w, *res = nullptr, *given = nullptr;
+    int32_t dyt, ht, wt, rt, gt, dxt;
+    int64_t device, stream;
+    float eps;
+    const uint8_t* mask;
+    if (n != 13 || !int_arg(a[11], &device) || !int_arg(a[12], &stream) || !typed_arg(a[0], device, &dy, &dyt) || !typed_arg(a[1], device, &h, &ht) ||
+        !typed_arg(a[2], device, &w, &wt) || !float_arg(a[3], &eps) || (a[4] != Py_None && !typed_arg(a[4], device, &res, &rt)) || h->dim() != 2 ||
+        h->numel() == 0 || !mask_arg(a[5], device, h->size(0), &mask) || !THPDtype_Check(a[6]) ||
+        (a[7] != Py_None && !typed_arg(a[7], device, &given, &gt)) || (a[8] != Py_True && a[8] != Py_False) || (a[9] != Py_True && a[9] != Py_False) ||
+        a[10] != Py_None || h->size(1) > INT32_MAX || !same_rows(*dy, *h) || w->dim() != 1 || w->size(0) != h->size(1) ||
+        (res != nullptr && (rt != ht || !same_rows(*res, *h))) ||
+        (given != nullptr && (gt != MRL_F32 || given->dim() != 1 || given->size(0) != h->size(1))) || (a[8] == Py_True && given == nullptr))
+      Py_RETURN_NONE;
+    const at::ScalarType out = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
+    if (out == at::kFloat) dxt = MRL_F32;
+    else if (out == at::kBFloat16) dxt = MRL_BF16;
+    else Py_RETURN_NONE;
+    const int64_t N = h->size(0), d = h->size(1);
+    at::Tensor dx = new_like(*h, {N, d}, out), dw, ws;
+    if (given != nullptr) dw = *given;
+    else if (a[9] == Py_True) dw = new_like(*h, {d}, at::kFloat);
+    size_t bytes = 0;
+    if (dw.defined()) {
+      bytes = mrl_rms_norm_backward_workspace(N, (int32_t)d);
+      if (bytes == 0) Py_RETURN_NONE;
+      ws = new_like(*h, {(int64_t)bytes}, at::kByte);
+    }
+    const void *dyp = dy->const_data_ptr(), *hp = h->const_data_ptr(), *wp = w->const_data_ptr(), *rp = res != nullptr ? res->const_data_ptr() : nullptr;
+    void *dxp = dx.mutable_data_ptr(), *wsp = ws.defined() ? ws.mutable_data_ptr() : nullptr;
+    float* const dwp = dw.defined() ? static_cast<float*>(dw.mutable_data_ptr()) : nullptr;
+    const int accumulate = a[8] == Py_True;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_rms_norm_backward(dyp, hp, wp, rp, mask, N, (int32_t)d, eps, dyt, ht, wt, dxt, accumulate, dxp, dwp, wsp, bytes,
+                               reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    PyObject* second = a[7];
+    if (given != nullptr) Py_INCREF(second); else second = THPVariable_Wrap(std::move(dw));
+    return Py_BuildValue("(iNN)", rc, THPVariable_Wrap(std::move(dx)), second);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
 PyMethodDef methods[] = {
     {"advantages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(advantages)), METH_FASTCALL, nullptr},
     {"align", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(align)), METH_FASTCALL, nullptr},
+    {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm)), METH_FASTCALL, nullptr},
+    {"rms_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm_backward)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "mrl_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

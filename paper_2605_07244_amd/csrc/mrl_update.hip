@@ -1,0 +1,452 @@
+// What becomes of a step's gradients: their global norm with the clip coefficient, and the AdamW update of many tensors in
+// one launch, with moments in 32 bits or as 8-bit codes.
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,  p -= lr (m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps) + wd p)
+//
+// A handful of operations on every element read: memory bounds the large calls, launches the small ones.  The tensors'
+// addresses travel as kernel arguments (no table in device memory: nothing to copy, and a captured launch carries its own).
+#include "../../include/mrl.h"
+#include "mrl_internal.h"
+#include "mrl_vec.h"
+
+#include <algorithm>
+#include <cmath>
+#include <new>
+
+namespace mrl {
+namespace {
+
+constexpr int kChunk = 2048;                 // elements of a tensor that a workgroup takes at a time: eight blocks of 8-bit states
+constexpr int kStateBlock = 256;             // elements that share a scale: a wave's four a lane
+
+// ------------------------------------------------------------------ global norm
+constexpr int kNormTensors = 96;             // a launch: 96 * 24 bytes of arguments
+constexpr int kNormBlocks = 1024;            // workgroups of a launch at most, a partial sum each
+struct NormTable {
+  const void* grad[kNormTensors];
+  int64_t n[kNormTensors];
+  int32_t chunk0[kNormTensors];              // the launch's chunks before the tensor's own; behind the last tensor INT32_MAX
+  uint32_t bf16[kNormTensors / 32];
+  int32_t chunks;
+  double* parts;
+};
+
+// Index of the tensor that the launch's chunk belongs to: how many of the (ascending) first chunks are not above it, less one.
+template <int kMost> __device__ inline int tensor_of(const int32_t* chunk0, int chunk) {
+  const int lane = threadIdx.x & 63;
+  int below = 0;
+#pragma unroll
+  for (int k = 0; k < kMost; k += 64) {
+    const bool in = k + lane < kMost && chunk0[k + lane < kMost ? k + lane : 0] <= chunk;
+    below += __popcll(__ballot(in));
+  }
+  return __builtin_amdgcn_readfirstlane(below - 1);
+}
+
+__device__ inline double wave_sum_f64(double x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+  return x;
+}
+template <int kWaves> __device__ inline double block_sum_f64(double x, double* sh) {
+  x = wave_sum_f64(x);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  double s = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) s += sh[w];
+  return s;
+}
+
+__global__ __launch_bounds__(256) void k_square_sums(NormTable a) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+    const int i = tensor_of<kNormTensors>(a.chunk0, chunk);
+    const int64_t at = (int64_t)(chunk - a.chunk0[i]) * kChunk;
+    const int left = (int)min((int64_t)kChunk, a.n[i] - at), c = threadIdx.x * 8;
+    if (a.bf16[i >> 5] >> (i & 31) & 1) {
+      Eight<true> g;
+      g.load(static_cast<const uint16_t*>(a.grad[i]) + at, c, left);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+    } else {
+      Eight<false> g;
+      g.load(static_cast<const float*>(a.grad[i]) + at, c, left);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+    }
+  }
+  s = block_sum_f64<4>(s, sh);
+  if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
+}
+
+// out[0] = norm, out[1] = min(1, max_norm / norm), or NaN where the norm is no number.
+__global__ __launch_bounds__(1024) void k_norm_coef(const double* parts, int n, double max_norm, float* out) {
+  __shared__ double sh[16];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 1024) s += parts[i];
+  s = block_sum_f64<16>(s, sh);
+  if (threadIdx.x != 0) return;
+  const double norm = sqrt(s), ratio = max_norm / norm;
+  out[0] = (float)norm;
+  out[1] = s < (double)INFINITY ? (ratio < 1.0 ? (float)ratio : 1.f) : __builtin_nanf("");
+}
+
+// ------------------------------------------------------------------ AdamW
+constexpr int kAdamTensors = 44;             // a launch: 44 * 84 bytes of arguments
+struct AdamTensor {
+  float* param; uint16_t* copy; const void* grad; void* m; void* v; float* m_scale; float* v_scale;
+  int64_t n; float weight_decay; int32_t grad_bf16; int32_t place /*in the call*/;
+};
+struct AdamTable {
+  AdamTensor t[kAdamTensors];
+  int32_t chunk0[kAdamTensors];
+  int32_t skip_nonfinite;
+  float lr, inv_fix1, inv_root_fix2;         // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float b1, one_b1, b2, one_b2, eps;
+  double beta1, beta2;
+  int64_t step;
+  uint64_t seed;
+  const float* lr_dev; const int64_t* step_dev; const float* coef;
+};
+
+// b1^t by squaring.
+__host__ __device__ inline double power(double b, int64_t t) {
+  double r = 1.0;
+  for (; t > 0; t >>= 1) {
+    if (t & 1) r *= b;
+    b *= b;
+  }
+  return r;
+}
+
+// Random bits of element i of a tensor: mix(lo(i) ^ mix(key + hi(i))), the key mixed of the seed, the step and the tensor's place.
+// Two rounds of multiplication and shift: every bit of the argument moves every bit of the result.
+__host__ __device__ inline uint32_t mix(uint32_t x) {
+  x = (x ^ x >> 16) * 0x6A09E667u;           // (fractional bits of the square roots of 2 and 3)
+  x = (x ^ x >> 15) * 0xBB67AE85u;
+  return x ^ x >> 16;
+}
+__device__ inline uint32_t key_of(uint64_t seed, int64_t step, int place) {
+  return mix((uint32_t)seed ^ mix((uint32_t)(seed >> 32) ^ mix((uint32_t)step ^ mix((uint32_t)place))));
+}
+
+// x >= 0, at most 448 (a little above by rounding): the e4m3 value below or above, above with the probability of the fraction.  u: 16
+// random bits, a fraction of the step.
+__device__ inline float to_code(float x, uint32_t u16) {
+  const uint32_t top = __float_as_uint(x) & 0x7f800000u;
+  const uint32_t binade = top > (121u << 23) ? top : 121u << 23;                                     // subnormals: that of 2^-6
+  const float per_step = __uint_as_float((257u << 23) - binade), step = __uint_as_float(binade - (3u << 23));
+  return fminf(floorf(fmaf((float)u16, 0x1p-16f, x * per_step)) * step, kE4m3Max);
+}
+
+template <bool kCodes>
+__global__ __launch_bounds__(256) void k_adamw(AdamTable a) {
+  const int i = tensor_of<kAdamTensors>(a.chunk0, blockIdx.x);
+  const AdamTensor& t = a.t[i];
+  const int64_t at = (int64_t)((int)blockIdx.x - a.chunk0[i]) * kChunk;
+  const float coef = a.coef != nullptr ? *a.coef : 1.f;
+  if (a.skip_nonfinite && !(fabsf(coef) < INFINITY)) return;
+  float lr = a.lr, inv_fix1 = a.inv_fix1, inv_root_fix2 = a.inv_root_fix2;
+  int64_t step = a.step;
+  if (a.lr_dev != nullptr) lr = *a.lr_dev;
+  if (a.step_dev != nullptr) {
+    step = max(*a.step_dev, (int64_t)1);
+    inv_fix1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
+    inv_root_fix2 = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int left = (int)min((int64_t)kChunk, t.n - at);
+  const uint32_t key = kCodes ? mix(key_of(a.seed, step, t.place) + (uint32_t)(at >> 32)) : 0;
+#pragma unroll
+  for (int k = 0; k < kChunk / 1024; ++k) {
+    const int c = k * 1024 + wave * kStateBlock + lane * 4;
+    if (k * 1024 + wave * kStateBlock >= left) return;  // (whole waves)
+    float p[4], g[4], m[4], v[4], root[4];
+    const bool whole = c + 4 <= left;
+    const int some = whole ? 4 : c < left ? left - c : 0;
+    // every element of the four that the tensor has; the others as zeros
+    if (whole) {
+      const u32x4 pw = load_any<4, u32x4>(t.param + at + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = __uint_as_float(pw[e]);
+      if (t.grad_bf16) {
+        const u32x2 w = load_any<2, u32x2>(static_cast<const uint16_t*>(t.grad) + at + c);
+        g[0] = bf16_low(w[0]); g[1] = bf16_high(w[0]); g[2] = bf16_low(w[1]); g[3] = bf16_high(w[1]);
+      } else {
+        const u32x4 w = load_any<4, u32x4>(static_cast<const float*>(t.grad) + at + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) g[e] = __uint_as_float(w[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = e < some ? t.param[at + c + e] : 0.f;
+        g[e] = e >= some ? 0.f : t.grad_bf16 ? bf16_low(static_cast<const uint16_t*>(t.grad)[at + c + e]) : static_cast<const float*>(t.grad)[at + c + e];
+      }
+    }
+    if (kCodes) {
+      uint32_t mw = 0, vw = 0;
+      const uint8_t *mp = static_cast<const uint8_t*>(t.m) + at + c, *vp = static_cast<const uint8_t*>(t.v) + at + c;
+      if (whole) {
+        mw = load_any<1, uint32_t>(mp);
+        vw = load_any<1, uint32_t>(vp);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (e < some) { mw |= (uint32_t)mp[e] << 8 * e; vw |= (uint32_t)vp[e] << 8 * e; }
+      }
+      const int64_t block = (at + c) / kStateBlock;
+      const float ms = t.m_scale[block], vs = t.v_scale[block];
+      const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, true);
+      const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, true);
+      m[0] = m01[0] * ms; m[1] = m01[1] * ms; m[2] = m23[0] * ms; m[3] = m23[1] * ms;
+      v[0] = v01[0] * vs; v[1] = v01[1] * vs; v[2] = v23[0] * vs; v[3] = v23[1] * vs;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= v[e];
+    } else if (whole) {
+      const u32x4 mw = load_any<4, u32x4>(static_cast<const float*>(t.m) + at + c), vw = load_any<4, u32x4>(static_cast<const float*>(t.v) + at + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { m[e] = __uint_as_float(mw[e]); v[e] = __uint_as_float(vw[e]); }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        m[e] = e < some ? static_cast<const float*>(t.m)[at + c + e] : 0.f;
+        v[e] = e < some ? static_cast<const float*>(t.v)[at + c + e] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float ge = g[e] * coef;
+      m[e] = fmaf(a.b1, m[e], a.one_b1 * ge);
+      v[e] = fmaf(a.b2, v[e], a.one_b2 * ge * ge);
+      root[e] = sqrtf(v[e]);
+      p[e] = fmaf(-lr, fmaf(t.weight_decay, p[e], m[e] * inv_fix1 / fmaf(root[e], inv_root_fix2, a.eps)), p[e]);
+    }
+    if (whole) {
+      store_any<4>(t.param + at + c, u32x4{__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3])});
+      if (t.copy != nullptr) store_any<2>(t.copy + at + c, u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])});
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        if (e >= some) continue;
+        t.param[at + c + e] = p[e];
+        if (t.copy != nullptr) t.copy[at + c + e] = (uint16_t)pack_bf16(p[e], 0.f);
+      }
+    }
+    if (!kCodes) {
+      if (whole) {
+        store_any<4>(static_cast<float*>(t.m) + at + c, u32x4{__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])});
+        store_any<4>(static_cast<float*>(t.v) + at + c, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+          if (e >= some) continue;
+          static_cast<float*>(t.m)[at + c + e] = m[e];
+          static_cast<float*>(t.v)[at + c + e] = v[e];
+        }
+      }
+      continue;
+    }
+    // 8-bit moments: m and sqrt(v) as multiples of their largest in 256 elements over 448
+    uint32_t m_most = kScaleLeast, v_most = kScaleLeast;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= some) m[e] = root[e] = 0.f;
+      m_most = larger(m_most, magnitude(m[e]));
+      v_most = larger(v_most, magnitude(root[e]));
+    }
+    const float m_max = __uint_as_float(wave_max(m_most)), v_max = __uint_as_float(wave_max(v_most));
+    const float m_inv = kE4m3Max / m_max, v_inv = kE4m3Max / v_max;
+    float mq[4], vq[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t bits = mix((uint32_t)(at + c + e) ^ key);
+      mq[e] = copysignf(to_code(fabsf(m[e]) * m_inv, bits & 0xffffu), m[e]);
+      // a positive root keeps a positive code: at zero the next step would divide by that step's gradient alone
+      vq[e] = fmaxf(to_code(root[e] * v_inv, bits >> 16), root[e] > 0.f ? 0x1p-9f : 0.f);
+    }
+    const uint32_t mw = pack_e4m3(mq[0], mq[1], mq[2], mq[3]), vw = pack_e4m3(vq[0], vq[1], vq[2], vq[3]);
+    uint8_t *mp = static_cast<uint8_t*>(t.m) + at + c, *vp = static_cast<uint8_t*>(t.v) + at + c;
+    if (whole) {
+      store_any<1>(mp, mw);
+      store_any<1>(vp, vw);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < some) { mp[e] = (uint8_t)(mw >> 8 * e); vp[e] = (uint8_t)(vw >> 8 * e); }
+    }
+    if (lane == 0) {
+      const int64_t block = (at + c) / kStateBlock;
+      t.m_scale[block] = m_max / kE4m3Max;
+      t.v_scale[block] = v_max / kE4m3Max;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+constexpr int64_t kMaxElements = (int64_t)1 << 40;
+int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+
+int check_tensors(const mrl_param_tensor* t, int32_t count, bool update, bool codes) {
+  if (count < 0) return MRL_ERR_SHAPE;
+  if (count > 0 && t == nullptr) return MRL_ERR_NULL;
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].n < 0 || t[i].n > kMaxElements) return MRL_ERR_SHAPE;
+    if (t[i].grad_dtype != MRL_F32 && t[i].grad_dtype != MRL_BF16) return MRL_ERR_DTYPE;
+    if (t[i].n == 0) continue;
+    chunks += chunks_of(t[i].n);
+    if (!t[i].grad) return MRL_ERR_NULL;
+    if (!update) continue;
+    if (!t[i].param || !t[i].m || !t[i].v || (codes && (!t[i].m_scale || !t[i].v_scale))) return MRL_ERR_NULL;
+    if (!(t[i].weight_decay >= 0.f && t[i].weight_decay < INFINITY)) return MRL_ERR_CONFIG;
+  }
+  return chunks < (int64_t)1 << 31 ? MRL_OK : MRL_ERR_SHAPE;
+}
+
+// Calls f(first, last) for the tensors of each launch: at most kMost of them that are not empty.
+template <int kMost, class F> void in_launches(const mrl_param_tensor* t, int32_t count, F f) {
+  int32_t first = 0, held = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].n == 0) continue;
+    if (held == kMost) { f(first, i); first = i; held = 0; }
+    ++held;
+  }
+  if (held > 0) f(first, count);
+}
+
+int64_t norm_parts(const mrl_param_tensor* t, int32_t count) {
+  int64_t parts = 0;
+  in_launches<kNormTensors>(t, count, [&](int32_t first, int32_t last) {
+    int64_t chunks = 0;
+    for (int32_t i = first; i < last; ++i) chunks += chunks_of(t[i].n);
+    parts += std::min<int64_t>(chunks, kNormBlocks);
+  });
+  return parts;
+}
+
+}  // namespace
+}  // namespace mrl
+
+using namespace mrl;
+
+extern "C" size_t mrl_grad_norm_workspace(const mrl_param_tensor* tensors, int32_t count) {
+  if (check_tensors(tensors, count, false, false) != MRL_OK) return 0;
+  return (size_t)round_up(norm_parts(tensors, count) * 8 + 8, 256);
+}
+
+extern "C" int mrl_grad_norm(const mrl_param_tensor* tensors, int32_t count, double max_norm, float* out_norm_coef, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  int rc = check_tensors(tensors, count, false, false);
+  if (rc != MRL_OK) return rc;
+  if (!out_norm_coef) return MRL_ERR_NULL;
+  if (!(max_norm > 0.0)) return MRL_ERR_CONFIG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < mrl_grad_norm_workspace(tensors, count)) return MRL_ERR_WORKSPACE;
+  rc = require_gfx950();
+  if (rc != MRL_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  double* const parts = static_cast<double*>(workspace);
+  int n_parts = 0;
+  in_launches<kNormTensors>(tensors, count, [&](int32_t first, int32_t last) {
+    NormTable a = {};
+    int k = 0;
+    int64_t chunks = 0;
+    for (int32_t i = first; i < last; ++i) {
+      if (tensors[i].n == 0) continue;
+      a.grad[k] = tensors[i].grad;
+      a.n[k] = tensors[i].n;
+      a.chunk0[k] = (int32_t)chunks;
+      if (tensors[i].grad_dtype == MRL_BF16) a.bf16[k >> 5] |= 1u << (k & 31);
+      chunks += chunks_of(tensors[i].n);
+      ++k;
+    }
+    for (; k < kNormTensors; ++k) a.chunk0[k] = INT32_MAX;
+    a.chunks = (int32_t)chunks;
+    a.parts = parts + n_parts;
+    const int blocks = (int)std::min<int64_t>(chunks, kNormBlocks);
+    n_parts += blocks;
+    hipLaunchKernelGGL(k_square_sums, dim3(blocks), dim3(256), 0, s, a);
+  });
+  hipLaunchKernelGGL(k_norm_coef, dim3(1), dim3(1024), 0, s, parts, n_parts, max_norm, out_norm_coef);
+  return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
+}
+
+extern "C" int mrl_adamw(const mrl_param_tensor* tensors, int32_t count, const mrl_adamw_config* cfg, const float* grad_coef, void* stream) {
+  if (!cfg) return MRL_ERR_NULL;
+  if (cfg->state_dtype != MRL_F32 && cfg->state_dtype != MRL_E4M3) return MRL_ERR_DTYPE;
+  const bool codes = cfg->state_dtype == MRL_E4M3;
+  int rc = check_tensors(tensors, count, true, codes);
+  if (rc != MRL_OK) return rc;
+  if (!(cfg->lr >= 0.0 && cfg->lr < 1e30) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) ||
+      !(cfg->eps >= 1e-30 && cfg->eps < 1e30) || (cfg->step_dev == nullptr && cfg->step < 1) || (cfg->skip_nonfinite != 0 && cfg->skip_nonfinite != 1))
+    return MRL_ERR_CONFIG;
+  if (count == 0) return MRL_OK;
+  rc = require_gfx950();
+  if (rc != MRL_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  in_launches<kAdamTensors>(tensors, count, [&](int32_t first, int32_t last) {
+    AdamTable a = {};
+    int k = 0;
+    int64_t chunks = 0;
+    for (int32_t i = first; i < last; ++i) {
+      const mrl_param_tensor& t = tensors[i];
+      if (t.n == 0) continue;
+      a.t[k] = {t.param, static_cast<uint16_t*>(t.copy), t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n, t.weight_decay, t.grad_dtype == MRL_BF16, i};
+      a.chunk0[k] = (int32_t)chunks;
+      chunks += chunks_of(t.n);
+      ++k;
+    }
+    for (; k < kAdamTensors; ++k) a.chunk0[k] = INT32_MAX;
+    a.skip_nonfinite = cfg->skip_nonfinite;
+    a.beta1 = cfg->beta1; a.beta2 = cfg->beta2;
+    a.lr = (float)cfg->lr;
+    a.b1 = (float)cfg->beta1; a.one_b1 = (float)(1.0 - cfg->beta1);
+    a.b2 = (float)cfg->beta2; a.one_b2 = (float)(1.0 - cfg->beta2);
+    a.eps = (float)cfg->eps;
+    a.step = cfg->step; a.seed = cfg->seed;
+    a.inv_fix1 = (float)(1.0 / (1.0 - power(cfg->beta1, cfg->step)));
+    a.inv_root_fix2 = (float)(1.0 / std::sqrt(1.0 - power(cfg->beta2, cfg->step)));
+    a.lr_dev = cfg->lr_dev; a.step_dev = cfg->step_dev; a.coef = grad_coef;
+    hipLaunchKernelGGL(codes ? k_adamw<true> : k_adamw<false>, dim3((unsigned)chunks), dim3(256), 0, s, a);
+  });
+  return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
+}
+
+extern "C" int mrl_adamw_check(const mrl_param_tensor* tensors, int32_t count, int32_t state_dtype) {
+  if (state_dtype != MRL_F32 && state_dtype != MRL_E4M3) return MRL_ERR_DTYPE;
+  const bool codes = state_dtype == MRL_E4M3;
+  const int rc = check_tensors(tensors, count, true, codes);
+  if (rc != MRL_OK || count == 0) return rc;
+  struct Range { uintptr_t first, last; bool written; };
+  const size_t most = (size_t)count * 7;
+  Range* const r = new (std::nothrow) Range[most];
+  if (r == nullptr) return MRL_ERR_DEVICE;
+  size_t k = 0;
+  auto add = [&](const void* p, int64_t bytes, bool written) {
+    if (p != nullptr && bytes > 0) r[k++] = {reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written};
+  };
+  for (int32_t i = 0; i < count; ++i) {
+    const mrl_param_tensor& t = tensors[i];
+    const int64_t moment = codes ? 1 : 4, scales = codes ? (t.n + kStateBlock - 1) / kStateBlock * 4 : 0;
+    add(t.param, t.n * 4, true);
+    add(t.copy, t.n * 2, true);
+    add(t.m, t.n * moment, true);
+    add(t.v, t.n * moment, true);
+    add(t.m_scale, scales, true);
+    add(t.v_scale, scales, true);
+    add(t.grad, t.n * (t.grad_dtype == MRL_BF16 ? 2 : 4), false);
+  }
+  std::sort(r, r + k, [](const Range& a, const Range& b) { return a.first < b.first; });
+  // (two gradients may overlap: nothing writes them)
+  uintptr_t written_to = 0, read_to = 0;
+  bool apart = true;
+  for (size_t i = 0; i < k && apart; ++i) {
+    apart = r[i].first >= written_to && !(r[i].written && r[i].first < read_to);
+    uintptr_t& to = r[i].written ? written_to : read_to;
+    to = std::max(to, r[i].last);
+  }
+  delete[] r;
+  return apart ? MRL_OK : MRL_ERR_CONFIG;
+}

@@ -1,0 +1,139 @@
+// Elements of float and bfloat16 tensors eight (or four) at a time, and sums and maxima over lanes: what the row and
+// update kernels share.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mrl {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Vector accesses at the alignment of one element: rows of odd widths and slices of flat buffers begin anywhere.  gfx950
+// takes global accesses of 8 and 16 bytes at any address, so an aligned tensor loses nothing by it.
+template <class V, int kAlign> struct __attribute__((packed, aligned(kAlign))) AtAnyAddress { V v; };
+template <int kAlign, class V> __device__ inline V load_any(const void* p) { return static_cast<const AtAnyAddress<V, kAlign>*>(p)->v; }
+template <int kAlign, class V> __device__ inline void store_any(void* p, V v) { static_cast<AtAnyAddress<V, kAlign>*>(p)->v = v; }
+
+__device__ inline float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ inline uint32_t pack_bf16(float lo, float hi) {          // nearest even; NaN stays NaN
+  const __bf16 a = (__bf16)lo, b = (__bf16)hi;
+  return (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
+}
+// Four e4m3 codes (OCP: no infinities, largest 448), nearest even, of values up to 448.
+__device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Elements c .. c + 7 of a row of d as they lie in memory, zeros from d on.  Nothing behind the row is read.
+template <bool kBf16> struct Eight;
+template <> struct Eight<true> {
+  u32x4 w;
+  __device__ void load(const void* row, int c, int d) {
+    const uint16_t* p = static_cast<const uint16_t*>(row) + c;
+    w = u32x4{0, 0, 0, 0};
+    if (c + 8 <= d) {
+      w = load_any<2, u32x4>(p);
+    } else if (c < d) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < d) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
+  }
+  __device__ float operator[](int e) const { return e & 1 ? bf16_high(w[e >> 1]) : bf16_low(w[e >> 1]); }
+};
+template <> struct Eight<false> {
+  u32x4 w[2];
+  __device__ void load(const void* row, int c, int d) {
+    const uint32_t* p = static_cast<const uint32_t*>(row) + c;
+    w[0] = w[1] = u32x4{0, 0, 0, 0};
+    if (c + 8 <= d) {
+      w[0] = load_any<4, u32x4>(p);
+      w[1] = load_any<4, u32x4>(p + 4);
+    } else if (c < d) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < d) w[e >> 2][e & 3] = p[e];
+    }
+  }
+  __device__ float operator[](int e) const { return __uint_as_float(w[e >> 2][e & 3]); }
+};
+
+// Elements c .. c + 7 of a row of d, those below d.
+__device__ inline void store_eight(void* row, bool bf16, int c, int d, const float (&v)[8]) {
+  if (c >= d) return;
+  if (bf16) {
+    uint16_t* p = static_cast<uint16_t*>(row) + c;
+    const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    if (c + 8 <= d) {
+      store_any<2>(p, w);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < d) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
+  } else {
+    float* p = static_cast<float*>(row) + c;
+    if (c + 8 <= d) {
+      store_any<4>(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+      store_any<4>(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+    } else {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (c + e < d) p[e] = v[e];
+    }
+  }
+}
+__device__ inline void store_eight_e4m3(void* row, int c, int d, const float (&v)[8]) {
+  if (c >= d) return;
+  uint8_t* p = static_cast<uint8_t*>(row) + c;
+  const u32x2 w = {pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+  if (c + 8 <= d) {
+    store_any<1>(p, w);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (c + e < d) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+  }
+}
+
+// Over the 16 lanes of a row by rotation, then over the wave's four rows through scalar registers.  Lanes that a step pairs
+// add the same two numbers, so all lanes end with the same bits.
+template <int kRotate> __device__ inline uint32_t rotated(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + kRotate, 0xf, 0xf, true);
+}
+__device__ inline float row16_sum(float x) {
+  x += __uint_as_float(rotated<8>(__float_as_uint(x)));
+  x += __uint_as_float(rotated<4>(__float_as_uint(x)));
+  x += __uint_as_float(rotated<2>(__float_as_uint(x)));
+  return x + __uint_as_float(rotated<1>(__float_as_uint(x)));
+}
+__device__ inline float wave_sum_f32(float x) {
+  const int s = __float_as_int(row16_sum(x));
+  const float a = __int_as_float(__builtin_amdgcn_readlane(s, 0)), b = __int_as_float(__builtin_amdgcn_readlane(s, 16));
+  const float c = __int_as_float(__builtin_amdgcn_readlane(s, 32)), d = __int_as_float(__builtin_amdgcn_readlane(s, 48));
+  return (a + b) + (c + d);
+}
+// Maxima of absolute values as their bits, whose order is that of the values, with infinity above all numbers and NaN above
+// infinity: a NaN is kept, where a maximum of floats would drop it.
+__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ inline uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ inline uint32_t row16_max(uint32_t x) {
+  x = larger(x, rotated<8>(x));
+  x = larger(x, rotated<4>(x));
+  x = larger(x, rotated<2>(x));
+  return larger(x, rotated<1>(x));
+}
+__device__ inline uint32_t wave_max(uint32_t x) {
+  const int m = (int)row16_max(x);
+  return larger(larger((uint32_t)__builtin_amdgcn_readlane(m, 0), (uint32_t)__builtin_amdgcn_readlane(m, 16)),
+                larger((uint32_t)__builtin_amdgcn_readlane(m, 32), (uint32_t)__builtin_amdgcn_readlane(m, 48)));
+}
+
+// Scales of e4m3 values: the largest magnitude, at least 2^-100 (whose inverse times 448 still is a number), maps to 448.
+constexpr float kE4m3Max = 448.f;
+constexpr uint32_t kScaleLeast = (127u - 100u) << 23;
+
+}  // namespace mrl

@@ -1,0 +1,386 @@
+"""Gradient norm and AdamW against 64 bits: sizes around lanes, blocks and chunks, many tensors, both kinds of moments, and a whole training step of
+head and norm.
+
+Bounds.  U = 2^-24.  m is two products and a fused addition of numbers known to U: 3 U of its terms; v has one more product.  The update's
+quotient adds the root (half of v's error, one rounding), a product, the addition of eps and the division: 10 U of itself; p itself is rounded once."""
+import numpy as np
+import pytest
+import torch
+
+from tests import update_oracle as uo
+from tests.update_oracle import f64
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def mrl():
+    import paper_2605_07244_amd as m
+    m.lib()
+    return m
+
+
+def _rand(n, seed, scale=1.0, dtype=F32):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (scale * torch.randn(n, device="cuda", generator=g)).to(dtype)
+
+
+def _moments(n, seed, states):
+    """Moments of a run under way: (m, v, m_scale, v_scale)."""
+    m, root = _rand(n, seed, 3e-4), _rand(n, seed + 1, 1e-3).abs() + 1e-5
+    if states == F32:
+        return m, root.square(), None, None
+    out = []
+    for x in (m, root):
+        scale = torch.tensor(uo.block_max(f64(x)) / 448 if n else np.zeros(0), dtype=F32, device="cuda")
+        out.append(((x / scale.repeat_interleave(256)[:n]).clamp(-448, 448).to(E4M3), scale))
+    return out[0][0], out[1][0], out[0][1], out[1][1]
+
+
+class Set:
+    """Tensors of the given sizes, with copies of them as they were."""
+
+    def __init__(self, mrl, sizes, grad=F32, states=F32, copy=True, seed=0, decay=0.01, gap=0):
+        self.mrl, self.sizes, self.states = mrl, sizes, states
+        at = np.cumsum([0] + [n + gap for n in sizes])
+
+        def parts(flat):
+            return [flat[a:a + n] for a, n in zip(at, sizes)]
+        total = int(at[-1])
+        self.p = parts(_rand(total, seed + 1, 0.02))
+        self.g = parts(_rand(total, seed + 2, 1e-3, grad))
+        self.copies = parts(torch.zeros(total, dtype=BF16, device="cuda")) if copy else None
+        mom = [_moments(n, seed + 10 + 2 * i, states) for i, n in enumerate(sizes)]
+        self.m, self.v, ms, vs = (list(x) for x in zip(*mom))
+        self.ms, self.vs = (ms, vs) if states == E4M3 else (None, None)
+        self.decay = decay if isinstance(decay, list) else [decay] * len(sizes)
+        self.plan = mrl.adamw_plan(self.p, self.g, self.copies, self.m, self.v, self.ms, self.vs, weight_decay=decay)
+        self.keep()
+
+    def all(self):
+        return [*self.p, *self.m, *self.v, *(self.copies or []), *(self.ms or []), *(self.vs or [])]
+
+    def keep(self):
+        torch.cuda.synchronize()
+        self.old = dict(p=[f64(x) for x in self.p], g=[f64(x) for x in self.g])
+        if self.states == F32:
+            self.old.update(m=[f64(x) for x in self.m], v=[f64(x) for x in self.v])
+        else:
+            self.old.update(m=[uo.decode(q, s) for q, s in zip(self.m, self.ms)], v=[uo.decode(q, s) ** 2 for q, s in zip(self.v, self.vs)])
+
+    def check(self, lr, t, coef=1.0, seed=0, b1=0.9, b2=0.999, eps=1e-8):
+        torch.cuda.synchronize()
+        for i, n in enumerate(self.sizes):
+            if n == 0:
+                continue
+            p0, g, m0, v0 = (self.old[k][i] for k in "pgmv")
+            g = g * coef
+            p, m, v = uo.adamw(p0, g, m0, v0, lr, t, b1, b2, eps, self.decay[i])
+            m_size, v_size = np.abs(b1 * m0) + np.abs((1 - b1) * g), v
+            # (decoded 8-bit moments: a product with the scale, and the square of one)
+            m_bound, v_bound = 5 * U * m_size, 7 * U * v_size
+            root = np.sqrt(v / (1 - b2 ** t)) + eps
+            step = lr * (m_size / (1 - b1 ** t) / root * 16 * U + self.decay[i] * np.abs(p0) * 3 * U)
+            err = np.abs(f64(self.p[i]) - p)
+            assert np.all(err <= U * np.abs(p) + step + 1e-45), (i, n, float(np.max(err / (U * np.abs(p) + step + 1e-45))))
+            if self.copies is not None:
+                assert torch.equal(self.copies[i], self.p[i].to(BF16)), i
+            if self.states == F32:
+                assert np.all(np.abs(f64(self.m[i]) - m) <= m_bound + 1e-45), i
+                assert np.all(np.abs(f64(self.v[i]) - v) <= v_bound + 1e-45), i
+            else:
+                bits = uo.random_bits(n, seed, t, i)
+                uo.check_codes(f"m of tensor {i}", self.m[i], self.ms[i], m, bits & 0xFFFF, False, rel=4e-6)
+                uo.check_codes(f"sqrt(v) of tensor {i}", self.v[i], self.vs[i], np.sqrt(v), bits >> 16, True)
+
+
+SIZES = [1, 2, 3, 4, 5, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025, 2047, 2048, 2049, 4097, 10001]
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+@pytest.mark.parametrize("grad", [F32, BF16])
+def test_sizes(mrl, states, grad):
+    s = Set(mrl, SIZES, grad, states)
+    mrl.adamw_step(s.plan, 1e-3, 5, seed=11)
+    s.check(1e-3, 5, seed=11)
+    for t in (6, 7):                                     # from what the step before left
+        s.keep()
+        mrl.adamw_step(s.plan, 3e-4, t, seed=12)
+        s.check(3e-4, t, seed=12)
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_slices_of_flat_buffers(mrl, states):
+    """Tensors one right behind the other at odd offsets, and what lies between them."""
+    for gap in (0, 1, 3):
+        s = Set(mrl, [5, 1, 259, 2050, 7, 4096, 300], F32, states, gap=gap)
+        flat = s.p[0].as_strided((sum(s.sizes) + gap * len(s.sizes),), (1,))
+        before = flat.clone()
+        mrl.adamw_step(s.plan, 1e-3, 2, seed=3)
+        s.check(1e-3, 2, seed=3)
+        after, at = flat.clone(), 0
+        for n in s.sizes:
+            assert torch.equal(before[at + n:at + n + gap], after[at + n:at + n + gap])
+            at += n + gap
+
+
+def test_8_bit_tails_stay_inside_their_tensors(mrl):
+    """Codes and scales in guarded buffers: not a byte beside them is written."""
+    for n in (1, 2, 3, 5, 255, 257, 2047, 2051):
+        m, v, ms, vs = _moments(n, 5, E4M3)
+        guards = [torch.full((x.numel() + 64,), 77, dtype=torch.uint8, device="cuda") for x in (m, v)]
+        scales = [torch.full((x.numel() + 2,), 7.0, device="cuda") for x in (ms, vs)]
+        for g, x in zip(guards, (m, v)):
+            g[3:3 + n] = x.view(torch.uint8)
+        for g, x in zip(scales, (ms, vs)):
+            g[1:-1] = x
+        p, g = _rand(n, 1), _rand(n, 2, 1e-3)
+        copy = torch.full((n + 4,), 5.0, dtype=BF16, device="cuda")
+        codes = [x[3:3 + n].view(E4M3) for x in guards]
+        plan = mrl.adamw_plan([p], [g], [copy[1:1 + n]], [codes[0]], [codes[1]], [scales[0][1:-1]], [scales[1][1:-1]])
+        mrl.adamw_step(plan, 1e-3, 9, seed=4)
+        p2 = _rand(n, 1)
+        plan2 = mrl.adamw_plan([p2], [g], None, [m], [v], [ms], [vs])
+        mrl.adamw_step(plan2, 1e-3, 9, seed=4)
+        torch.cuda.synchronize()
+        assert torch.equal(p, p2) and torch.equal(copy[1:1 + n], p.to(BF16)) and copy[0] == 5 and bool((copy[1 + n:] == 5).all())
+        for g, x in zip(guards, (m, v)):
+            assert torch.equal(g[3:3 + n], x.view(torch.uint8)) and bool((g[:3] == 77).all()) and bool((g[3 + n:] == 77).all())
+        for g, x in zip(scales, (ms, vs)):
+            assert torch.equal(g[1:-1], x) and g[0] == 7 and g[-1] == 7
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_many_tensors(mrl, states):
+    """More tensors than a launch takes, empty ones among them, a weight decay for each; as many calls of one tensor give the same."""
+    sizes = [(37 * i) % 1500 for i in range(203)]
+    decay = [0.01 * (i % 3) for i in range(203)]
+    s = Set(mrl, sizes, F32, states, decay=decay)
+    assert sizes.count(0) >= 1
+    mrl.adamw_step(s.plan, 1e-3, 4, seed=5)
+    s.check(1e-3, 4, seed=5)
+    coef = mrl.grad_norm(s.plan, 0.01)
+    norm, c = uo.grad_norm([f64(x) for x in s.g], 0.01)
+    assert abs(float(coef[0]) - norm) <= 2 * U * norm and abs(float(coef[1]) - c) <= 2 * U * c
+
+
+@pytest.mark.parametrize("sizes,grad", [([1], F32), ([2049], BF16), ([3, 70001, 0, 5], F32), ([2048 * 1024 + 1], F32), ([5000000, 33], BF16), ([100] * 300, F32), ([0], F32)])
+def test_grad_norm(mrl, sizes, grad):
+    g = [_rand(n, i, 1e-3 * (1 + i % 5), grad) for i, n in enumerate(sizes)]
+    plan = mrl.grad_plan(g)
+    norm, _ = uo.grad_norm([f64(x) for x in g], 1.0)
+    for most in (float("inf"), 1.0, 0.5 * norm, norm * 2) if norm else (1.0,):
+        got = mrl.grad_norm(plan, most)
+        # exact squares, sums in fp64, one rounding to fp32
+        assert abs(float(got[0]) - norm) <= 1.001 * U * norm
+        want = min(1.0, most / norm) if norm else 1.0
+        assert abs(float(got[1]) - want) <= 1.001 * U * want
+        assert torch.equal(got, mrl.grad_norm(plan, most))
+
+
+def test_grad_norm_of_large_small_and_no_numbers(mrl):
+    """Squares that overflow and underflow fp32 are sums in fp64; what is no number is said so, wherever it lies."""
+    big, small = torch.full((5000,), 3e38, device="cuda"), torch.full((5000,), 1e-30, device="cuda")
+    got = mrl.grad_norm(mrl.grad_plan([big]), 1.0)
+    # the norm, 2.1e40, is above fp32; its inverse 4.714e-41 is a subnormal, known to half of 2^-149: 7.0e-46 / 4.714e-41 = 1.49e-5 of itself
+    assert float(got[0]) == float("inf") and abs(float(got[1]) * 3e38 * 5000 ** 0.5 - 1) < 1.5e-5
+    got = mrl.grad_norm(mrl.grad_plan([small]), 1.0)
+    assert abs(float(got[0]) / (1e-30 * 5000 ** 0.5) - 1) < 1e-6 and float(got[1]) == 1.0
+    for odd in (float("nan"), float("inf"), -float("inf")):
+        for at in (0, 2048, 4999):
+            g = _rand(5000, 1)
+            g[at] = odd
+            got = mrl.grad_norm(mrl.grad_plan([_rand(77, 2), g]), 1.0)
+            assert not np.isfinite(float(got[0])) and np.isnan(float(got[1]))
+    none = mrl.grad_norm(mrl.grad_plan([]), 1.0)
+    assert none.tolist() == [0.0, 1.0]
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_clipped_and_skipped(mrl, states):
+    s = Set(mrl, [700, 3000], F32, states)
+    norm, c = uo.grad_norm(s.old["g"], 0.01)
+    coef = mrl.grad_norm(s.plan, 0.01)
+    mrl.adamw_step(s.plan, 1e-3, 3, norm_coef=coef, seed=1, skip_nonfinite=True)
+    s.check(1e-3, 3, coef=c, seed=1)
+    s.g[1][2999] = float("nan")
+    before = [x.clone() for x in s.all()]
+    coef = mrl.grad_norm(s.plan, 0.01)
+    mrl.adamw_step(s.plan, 1e-3, 4, norm_coef=coef, seed=1, skip_nonfinite=True)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, s.all()))
+    # without a coefficient, a NaN spoils its element or its block of 8-bit moments, and nothing else
+    mrl.adamw_step(s.plan, 1e-3, 4, seed=1)
+    assert bool(s.p[1][2999].isnan()) and int(s.p[1].isnan().sum()) == 1 and not bool(s.p[0].isnan().any())
+    m = s.m[1] if states == F32 else torch.tensor(uo.decode(s.m[1], s.ms[1]))
+    v = s.v[1] if states == F32 else torch.tensor(uo.decode(s.v[1], s.vs[1]))
+    lost = 1 if states == F32 else 3000 - 11 * 256
+    assert int(m.isnan().sum()) == lost and int(v.isnan().sum()) == lost
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_from_nothing(mrl, states):
+    """The first step of a new run: moments that the plan allocates, zero gradients among the others."""
+    p, g = _rand(3000, 1, 0.02), _rand(3000, 2, 1e-3)
+    g[:700] = 0.0
+    p0, copy = p.clone(), torch.empty(3000, dtype=BF16, device="cuda")
+    plan = mrl.adamw_plan([p], [g], [copy], state_dtype=states, weight_decay=0.0)
+    mrl.adamw_step(plan, 1e-3, 1)
+    torch.cuda.synchronize()
+    assert torch.equal(p[:700], p0[:700]) and torch.equal(copy, p.to(BF16))
+    # m / (1 - b1) = g and v / (1 - b2) = g^2: a step of lr each
+    want = f64(p0) - 1e-3 * f64(g) / (np.abs(f64(g)) + 1e-8)
+    assert np.all(np.abs(f64(p) - want) <= U * np.abs(want) + 1e-3 * 20 * U)
+    if states == E4M3:
+        assert float(uo.decode(plan.v[0], plan.v_scale[0])[700:].min()) > 0 and not uo.decode(plan.v[0], plan.v_scale[0])[:700].any()
+
+
+def test_8_bit_moments_follow_those_of_32_bits(mrl):
+    """After 3000 steps of gradients of steady size: sqrt(v) is right on average (rounded to nearest, its codes would have stopped after a few
+    steps, an error of 0.9 and more), and single values scatter by no more than a code's step."""
+    n = 256 * 64
+    sigma = 1e-3 * torch.exp(1.5 * _rand(n, 1))
+    g = torch.empty(n, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(3)
+    plans = [mrl.adamw_plan([torch.zeros(n, device="cuda")], [g], state_dtype=t, weight_decay=0.0) for t in (F32, E4M3)]
+    for t in range(1, 3001):
+        torch.randn(n, device="cuda", generator=gen, out=g)
+        g.mul_(sigma)
+        for plan in plans:
+            mrl.adamw_step(plan, 1e-3, t, seed=9)
+    root = f64(plans[0].v[0]) ** 0.5
+    got = uo.decode(plans[1].v[0], plans[1].v_scale[0])
+    large = root > 1e-3 * np.repeat(uo.block_max(root), 256)          # (well inside the normal codes)
+    ratio = got[large] / root[large]
+    # codes are at most 1/8 apart; of single steps' roundings, b2^i of each remains: 1/8 / sqrt(12 (1 - b2^2)) would be 0.8 for
+    # independent roundings that nothing restores, but a wrong root is pulled back by the same 0.1 % a step that moves it
+    print("sqrt(v), 8 bits over 32: mean", ratio.mean(), "deviation", ratio.std())
+    assert abs(ratio.mean() - 1) < 0.1
+
+
+def test_numbers_from_the_device_and_replays(mrl):
+    """A captured step takes its learning rate and step from the device; eager calls of the same steps give the same bits."""
+    for states in (F32, E4M3):
+        a, b = Set(mrl, [1000, 5000], F32, states), Set(mrl, [1000, 5000], F32, states)
+        lr, step = torch.zeros(1, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            mrl.grad_norm(a.plan, 0.01)                  # (the first call of a process loads the kernels)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step.add_(1)
+            coef = mrl.grad_norm(a.plan, 0.01)
+            mrl.adamw_step(a.plan, lr, step, norm_coef=coef, seed=21, skip_nonfinite=True)
+        for t in range(1, 5):
+            lr.fill_(1e-3 / t)
+            for k in range(2):
+                a.g[k].copy_(_rand(a.sizes[k], 50 * t + k, 1e-3))
+                b.g[k].copy_(a.g[k])
+            if t == 3:
+                a.g[0][5] = b.g[0][5] = float("inf")     # skipped
+            graph.replay()
+            torch.cuda.synchronize()
+            mrl.adamw_step(b.plan, float(lr), t, norm_coef=mrl.grad_norm(b.plan, 0.01), seed=21, skip_nonfinite=True)
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.all(), b.all())), t
+
+
+def test_more_than_2_32_elements(mrl):
+    """One tensor whose offsets pass 32 bits: its end is updated as a tensor of its own would be, with the random bits of its places."""
+    n, k = 2 ** 32 + 3 * 2048 + 301, 5000
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2))
+    ms, vs = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
+    g[-k:] = _rand(k, 1, 1e-3, BF16)
+    plan = mrl.adamw_plan([p], [g], None, [m], [v], [ms], [vs])
+    got = mrl.grad_norm(plan, 1e-3)
+    norm, c = uo.grad_norm([f64(g[-k:])], 1e-3)
+    assert abs(float(got[0]) - norm) <= 1.001 * U * norm
+    mrl.adamw_step(plan, 1e-3, 1, seed=6)
+    torch.cuda.synchronize()
+    first = (n - k) // 256 * 256                         # a block's beginning
+    grad = f64(g[first:])
+    want, m1, v1 = uo.adamw(np.zeros(n - first), grad, np.zeros(n - first), np.zeros(n - first), 1e-3, 1)
+    assert np.all(np.abs(f64(p[first:]) - want) <= 21 * U * 1e-3)
+    bits = uo.random_bits(n - first, 6, 1, 0, first)
+    uo.check_codes("m", m[first:], ms[first // 256:], m1, bits & 0xFFFF, False)
+    uo.check_codes("sqrt(v)", v[first:], vs[first // 256:], np.sqrt(v1), bits >> 16, True)
+    assert not bool(p[:2 ** 20].any()) and not bool(p[2 ** 31 - 1000:2 ** 31 + 1000].any())
+
+
+def test_refusals(mrl):
+    p, g = torch.zeros(10, device="cuda"), torch.zeros(10, device="cuda")
+    for bad in (lambda: mrl.adamw_plan([p.bfloat16()], [g]), lambda: mrl.adamw_plan([p], [g.half()]), lambda: mrl.adamw_plan([p], [g], [p]),
+                lambda: mrl.adamw_plan([p], [g], state_dtype=BF16), lambda: mrl.adamw_plan([p], [g], m=[p.bfloat16()], state_dtype=F32),
+                lambda: mrl.grad_plan([p.double()])):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: mrl.adamw_plan([p], [g[:9]]), lambda: mrl.adamw_plan([p, p], [g]), lambda: mrl.adamw_plan([p], [g], weight_decay=[0.1, 0.1]),
+                lambda: mrl.adamw_plan([p], [g], m=[]), lambda: mrl.grad_plan([torch.zeros(8, 8, device="cuda").t()]),
+                lambda: mrl.adamw_plan([p], [g], state_dtype=E4M3, m_scale=[torch.zeros(2, device="cuda")])):
+        with pytest.raises(ValueError):
+            bad()
+    plan = mrl.adamw_plan([p], [g])
+    for bad in (lambda: mrl.adamw_plan([p, p], [g, g]), lambda: mrl.adamw_plan([p], [p]), lambda: mrl.adamw_plan([p], [g], weight_decay=-1.0),
+                lambda: mrl.adamw_step(plan, -1.0, 1), lambda: mrl.adamw_step(plan, 1e-3, 0), lambda: mrl.adamw_step(plan, 1e-3, 1, beta1=1.0),
+                lambda: mrl.grad_norm(plan, 0.0)):
+        with pytest.raises(mrl.MrlError) as e:
+            bad()
+        assert e.value.status == -7
+    for bad in (lambda: mrl.adamw_step(plan, torch.zeros(2, device="cuda"), 1), lambda: mrl.adamw_step(plan, 1e-3, 1, norm_coef=torch.zeros(1, device="cuda")),
+                lambda: mrl.grad_norm(plan, 1.0, out=torch.zeros(3, device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        mrl.adamw_step(plan, torch.zeros(1, device="cuda", dtype=torch.float64), 1)
+
+
+def test_a_training_step_of_head_and_norm(mrl):
+    """Norm, scoring loss, both backward passes, clipping and update, as they follow one another, against the same chain in 64 bits."""
+    from oracle import mrl_oracle as orc
+    from tests import util
+    from workloads import synth
+    sp = synth.spec(2, n_prompts=2, T=24, V=1200)
+    b = synth.make(sp, "cuda")
+    N, d = b["H"].shape
+    V = b["W"].shape[0]
+    mask = b["mask"].reshape(-1)
+    x, res = b["H"], _rand(N * d, 3, 0.5, BF16).view(N, d)
+    norm_w, head = 1 + _rand(d, 4, 0.1), b["W"].float()
+    norm16, head16 = norm_w.to(BF16), b["W"].clone()
+    dhead, dnorm = torch.empty(V, d, device="cuda"), torch.empty(d, device="cuda")
+    adv, *_ = mrl.group_advantages(b["rewards_all"], b["group_all"], b["G"], b["in_stats"], b["scored"], b["is_own"])
+    seq_adv = synth.seq_adv_from(adv, b)
+    lc = mrl.LossConfig(kl_beta=sp.kl_beta, sgt_lambda=sp.sgt_lambda)
+    cfg = util.cfg_dict(sp)
+    # the oracle's chain, from the bf16 hidden states and gradients that the path hands on
+    m = mask.cpu().numpy()
+    y0, h0 = uo.rms_norm(f64(x), f64(norm16), EPS := 1e-5, f64(res), m)
+    H, h, _ = mrl.rms_norm(x, norm16, EPS, residual=res, token_mask=mask)
+    assert np.all(np.abs(f64(H) - y0) <= (2.0 ** -8 + 52 * U) * np.abs(y0))
+    b["H"] = H
+    first = util.oracle_loss(b, seq_adv.cpu().numpy(), cfg, need_grads=False)
+    b["behav"] = util.move_off_kinks(b, first["logp"], sp.clip_eps)
+    want = util.oracle_loss(b, seq_adv.cpu().numpy(), cfg)
+    for states in (F32, E4M3):
+        p, p16 = [head.clone(), norm_w.clone()], [head16.clone(), norm16.clone()]
+        plan = mrl.adamw_plan(p, [dhead, dnorm], p16, state_dtype=states, weight_decay=[0.01, 0.0])
+        out = mrl.grpo_loss_fwd_bwd(H, p16[0], b["targets"], mask, b["behav"], b["ref"], seq_adv, b["seq_group"], b["seq_kind"], b["B"], b["T"], b["G"],
+                                    lc, out_dW=dhead)
+        dx, _ = mrl.rms_norm_backward(out["dH"], h, p16[1], EPS, token_mask=mask, out_dweight=dnorm)
+        coef = mrl.grad_norm(plan, 0.1)
+        mrl.adamw_step(plan, 1e-3, 1, norm_coef=coef, seed=1, skip_nonfinite=True)
+        torch.cuda.synchronize()
+        dx_o, dn_o, *_ = uo.rms_norm_backward(want["dH"], f64(h), f64(norm16), EPS, None, m)
+        assert util.rel_fro(f64(dx), dx_o) <= util.REL_TOL and util.rel_fro(f64(dnorm), dn_o) <= util.REL_TOL
+        assert util.rel_fro(f64(dhead), want["dW"]) <= util.REL_TOL
+        norm_o, coef_o = uo.grad_norm([want["dW"], dn_o], 0.1)
+        assert abs(float(coef[0]) - norm_o) <= util.REL_TOL * norm_o
+        # the update from the path's own gradients: each stage is held to its inputs
+        for p_new, p_old, g, decay, c16 in ((p[0], head, dhead, 0.01, p16[0]), (p[1], norm_w, dnorm, 0.0, p16[1])):
+            gc = f64(g).reshape(-1) * float(coef[1])
+            p_o, m_o, v_o = uo.adamw(f64(p_old).reshape(-1), gc, 0 * gc, 0 * gc, 1e-3, 1, decay=decay)
+            assert np.all(np.abs(f64(p_new).reshape(-1) - p_o) <= U * np.abs(p_o) + 1e-3 * 24 * U)
+            assert torch.equal(c16, p_new.to(BF16))
