@@ -13,7 +13,7 @@ namespace {
 
 struct NormArgs {
   const void* x; const void* residual; const void* w; const uint8_t* mask;
-  int64_t N; int d; float eps;
+  int64_t N; int d; float eps, inv_d;
   int w_bf16, y_type /*mrl_dtype*/, scale_block;
   void* sum; void* y; float* scale;
 };
@@ -56,13 +56,11 @@ __device__ inline void load_weights(const void* w, bool bf16, int c, int d, floa
 
 // kT threads take a row, each kNV times eight elements, kT * 8 apart.  kRes: 0 no residual, 1 bf16, 2 float.
 template <bool kXBf16, int kRes, int kT, int kNV>
-__global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm(NormArgs a) {
+__global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
   __shared__ float sh_sum[16];
   __shared__ uint32_t sh_max[16];
-  constexpr int kRows = kT < 256 ? 256 / kT : 1;
-  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kT;
-  if (row >= a.N) return;                               // (whole waves; with more waves a row there is one row a block)
-  const int t = threadIdx.x % kT, d = a.d;
+  const int64_t row = blockIdx.x;
+  const int t = threadIdx.x, d = a.d;
   const int scales = a.scale_block ? (d + 127) / 128 : 1;
   const char* x = static_cast<const char*>(a.x) + row * d * (kXBf16 ? 2 : 4);
   const char* res = static_cast<const char*>(a.residual) + row * d * (kRes == 1 ? 2 : 4);
@@ -94,10 +92,10 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm(NormArgs a) {
   for (int i = 0; i < kNV; ++i) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) s = fmaf(h[i][e], h[i][e], s);
-    if (kRes) store_eight(sum, kRes == 1, (i * kT + t) * 8, d, h[i]);
+    if (kRes) store_eight<true>(sum, kRes == 1, (i * kT + t) * 8, d, h[i]);
   }
   s = group_sum<kT>(s, sh_sum);
-  const float r = 1.f / sqrtf(s / (float)d + a.eps);
+  const float r = __builtin_amdgcn_rsqf(fmaf(s, a.inv_d, a.eps));      // (the instruction is good to a step of fp32)
 #pragma unroll
   for (int i = 0; i < kNV; ++i) {
     float w[8];
@@ -143,18 +141,48 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm(NormArgs a) {
 
 struct NormBackArgs {
   const void* dy; const void* h; const void* w; const void* d_residual; const uint8_t* mask;
-  int64_t N; int d; float eps;
+  int64_t N; int d; float eps, inv_d;
   int w_bf16, dx_bf16;
   void* dx; float* parts /*[gridDim.x][ld] | nullptr*/; int ld;
 };
 
-// Rows of a workgroup one after the other (kT < 256: 256 / kT of them side by side); the columns' sums of dy u stay in registers until the last row,
-// then the rows that were side by side are added in LDS, in their order, and the workgroup writes one row of partial sums.
+// What a thread holds of a row.
+template <bool kHBf16, bool kDyBf16, int kT, int kNV> struct BackRow {
+  Eight<kHBf16> h[kNV], res[kNV];
+  Eight<kDyBf16> dy[kNV];
+  bool scored;
+  __device__ void load(const NormBackArgs& a, int64_t row, bool is_scored, int t) {
+    scored = is_scored;
+    const int64_t at = row * a.d;
+    const char* h_row = static_cast<const char*>(a.h) + at * (kHBf16 ? 2 : 4);
+    const char* dy_row = static_cast<const char*>(a.dy) + at * (kDyBf16 ? 2 : 4);
+    const char* res_row = static_cast<const char*>(a.d_residual) + at * (kHBf16 ? 2 : 4);
+    if (is_scored) {
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) {
+        h[i].load(h_row, (i * kT + t) * 8, a.d);
+        dy[i].load(dy_row, (i * kT + t) * 8, a.d);
+      }
+    }
+    if (a.d_residual != nullptr) {
+#pragma unroll
+      for (int i = 0; i < kNV; ++i) res[i].load(res_row, (i * kT + t) * 8, a.d);
+    }
+  }
+};
+
+// The rows of a workgroup one after the other (kT = 64: four waves side by side), the next one's elements on their way while one is
+// worked on, and the mask of the one behind it; the columns' sums of dy u stay in registers until the last row.  Then the rows that were
+// side by side are added in LDS, in their order, and the workgroup writes one row of partial sums.
+// In round k the workgroups take consecutive rows, turned by k times a golden section of their number: sequences of as many slots as there are
+// workgroups, whose heads are scored and whose tails are not, would else give some of them scored rows only.
 template <bool kHBf16, bool kDyBf16, int kT, int kNV>
-__global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm_back(NormBackArgs a) {
-  extern __shared__ float lds[];                        // kT < 256: [d] sums; else two sets of two sums a wave
-  constexpr int kRows = kT < 256 ? 256 / kT : 1;
+__global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackArgs a) {
+  extern __shared__ float lds[];                        // kT = 64: [d] sums; else two sets of two sums a wave
+  constexpr int kRows = kT == 64 ? 4 : 1;
   const int t = threadIdx.x % kT, side = threadIdx.x / kT, d = a.d;
+  const int slots = (int)gridDim.x * kRows, slot = (int)blockIdx.x * kRows + side;
+  const int turn_by = (int)(slots * 0.618f), rounds = (int)((a.N + slots - 1) / slots);
   float acc[kNV][8], w[kNV][8];                         // (weights stay in registers, too: every row needs them twice)
 #pragma unroll
   for (int i = 0; i < kNV; ++i) {
@@ -162,67 +190,71 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm_back(NormBackA
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
   }
-  int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + side; row < a.N; row += (int64_t)gridDim.x * kRows) {
-    const char* res = static_cast<const char*>(a.d_residual) + row * d * (kHBf16 ? 2 : 4);
-    char* dx = static_cast<char*>(a.dx) + row * d * (a.dx_bf16 ? 2 : 4);
-    Eight<kHBf16> hv[kNV], rv[kNV];
-    Eight<kDyBf16> gv[kNV];
-    const bool scored = a.mask == nullptr || a.mask[row] != 0;
-    if (a.d_residual != nullptr) {
+  int64_t base = 0;
+  int place = slot;
+  auto next_row = [&]() -> int64_t {                    // of the next round, or -1
+    const int64_t row = base + place;
+    base += slots;
+    place += turn_by;
+    if (place >= slots) place -= slots;
+    return row < a.N ? row : -1;
+  };
+  auto mask_of = [&](int64_t row) -> int { return row < 0 ? 0 : a.mask == nullptr ? 1 : a.mask[row]; };
+  constexpr bool kAhead = kNV < 4;                      // (two rows of more do not fit the registers)
+  BackRow<kHBf16, kDyBf16, kT, kNV> now, next;
+  int64_t row = next_row(), row1 = next_row();
+  int mask0 = mask_of(row), mask1 = mask_of(row1), turn = 0;
+  if (kAhead && row >= 0) now.load(a, row, __builtin_amdgcn_readfirstlane(mask0) != 0, t);
+  for (int k = 0; k < rounds; ++k) {
+    const int64_t row2 = next_row();
+    const int mask2 = mask_of(row2);
+    if (kAhead && row1 >= 0) next.load(a, row1, __builtin_amdgcn_readfirstlane(mask1) != 0, t);
+    if (!kAhead && row >= 0) now.load(a, row, __builtin_amdgcn_readfirstlane(mask0) != 0, t);
+    if (row >= 0) {                                     // (with more waves than one a row, the workgroup is of one mind)
+      char* dx = static_cast<char*>(a.dx) + row * d * (a.dx_bf16 ? 2 : 4);
+      float r = 0.f, along = 0.f;
+      if (now.scored) {
+        float hh = 0.f, gh = 0.f;
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) rv[i].load(res, (i * kT + t) * 8, d);
-    }
-    if (!scored) {
+        for (int i = 0; i < kNV; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            hh = fmaf(now.h[i][e], now.h[i][e], hh);
+            gh = fmaf(now.dy[i][e] * w[i][e], now.h[i][e], gh);
+          }
+        }
+        hh = wave_sum_f32(hh);
+        gh = wave_sum_f32(gh);
+        if (kT > 64) {                                  // (two sets of slots in turn from one scored row to the next: one barrier each)
+          float* sh = lds + turn * 32;
+          turn ^= 1;
+          if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6] = hh; sh[16 + (threadIdx.x >> 6)] = gh; }
+          __syncthreads();
+          hh = gh = 0.f;
+#pragma unroll
+          for (int v = 0; v < kT / 64; ++v) { hh += sh[v]; gh += sh[16 + v]; }
+        }
+        r = __builtin_amdgcn_rsqf(fmaf(hh, a.inv_d, a.eps));
+        along = gh * r * a.inv_d;
+      }
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
         float out[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[e] = a.d_residual != nullptr ? rv[i][e] : 0.f;
+        for (int e = 0; e < 8; ++e) {
+          out[e] = 0.f;
+          if (now.scored) {
+            const float u = now.h[i][e] * r;
+            acc[i][e] = fmaf(now.dy[i][e], u, acc[i][e]);
+            out[e] = r * (now.dy[i][e] * w[i][e] - u * along);
+          }
+          if (a.d_residual != nullptr) out[e] += now.res[i][e];
+        }
         store_eight(dx, a.dx_bf16, (i * kT + t) * 8, d, out);
       }
-      continue;
     }
-    const char* h = static_cast<const char*>(a.h) + row * d * (kHBf16 ? 2 : 4);
-    const char* dy = static_cast<const char*>(a.dy) + row * d * (kDyBf16 ? 2 : 4);
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      hv[i].load(h, (i * kT + t) * 8, d);
-      gv[i].load(dy, (i * kT + t) * 8, d);
-    }
-    float hh = 0.f, gh = 0.f;
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        hh = fmaf(hv[i][e], hv[i][e], hh);
-        gh = fmaf(gv[i][e] * w[i][e], hv[i][e], gh);
-      }
-    }
-    hh = wave_sum_f32(hh);
-    gh = wave_sum_f32(gh);
-    if (kT > 64) {                                      // (two sets of slots in turn: one barrier a row)
-      float* sh = lds + turn * 32;
-      turn ^= 1;
-      if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6] = hh; sh[16 + (threadIdx.x >> 6)] = gh; }
-      __syncthreads();
-      hh = gh = 0.f;
-#pragma unroll
-      for (int w = 0; w < kT / 64; ++w) { hh += sh[w]; gh += sh[16 + w]; }
-    }
-    const float r = 1.f / sqrtf(hh / (float)d + a.eps), along = gh * r / (float)d;
-#pragma unroll
-    for (int i = 0; i < kNV; ++i) {
-      float out[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float u = hv[i][e] * r;
-        acc[i][e] = fmaf(gv[i][e], u, acc[i][e]);
-        out[e] = r * (gv[i][e] * w[i][e] - u * along);
-        if (a.d_residual != nullptr) out[e] += rv[i][e];
-      }
-      store_eight(dx, a.dx_bf16, (i * kT + t) * 8, d, out);
-    }
+    if (kAhead) now = next;
+    row = row1; row1 = row2; mask0 = mask1; mask1 = mask2;
   }
   if (a.parts == nullptr) return;
   float* part = a.parts + (int64_t)blockIdx.x * a.ld;
@@ -247,26 +279,33 @@ __global__ __launch_bounds__(kT < 256 ? 256 : kT) void k_rms_norm_back(NormBackA
   }
 }
 
-// dw[c] = (or +=) sum of the workgroups' partial sums, in fp64 in a fixed order: 16 columns a workgroup, 64 threads along the partials.
+// dw[c] = (or +=) sum of the workgroups' partial sums, in fp64 in a fixed order: kDwLanes times four columns a workgroup, the other threads along
+// the partials.
+constexpr int kDwLanes = 4;
 __global__ __launch_bounds__(256) void k_rms_norm_dw(const float* parts, int n_parts, int ld, int d, int accumulate, float* dw) {
-  __shared__ double sh[4][16];
-  const int c0 = blockIdx.x * 16 + (threadIdx.x & 3) * 4, lane = threadIdx.x & 63;
+  __shared__ double sh[4][4 * kDwLanes];
+  const int at = threadIdx.x % kDwLanes, c0 = (blockIdx.x * kDwLanes + at) * 4, lane = threadIdx.x & 63;
+  constexpr int kAlong = 256 / kDwLanes;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
   if (c0 < ld) {
-    for (int p = threadIdx.x >> 2; p < n_parts; p += 64) {
-      const float4 v = *reinterpret_cast<const float4*>(parts + (int64_t)p * ld + c0);
-      s[0] += (double)v.x; s[1] += (double)v.y; s[2] += (double)v.z; s[3] += (double)v.w;
+    for (int p0 = threadIdx.x / kDwLanes; p0 < n_parts; p0 += kAlong * 4) {
+      float4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        v[k] = p0 + kAlong * k < n_parts ? *reinterpret_cast<const float4*>(parts + (int64_t)(p0 + kAlong * k) * ld + c0) : float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { s[0] += (double)v[k].x; s[1] += (double)v[k].y; s[2] += (double)v[k].z; s[3] += (double)v[k].w; }
     }
   }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
 #pragma unroll
-    for (int off = 4; off < 64; off <<= 1) s[k] += __shfl_xor(s[k], off);
-    if (lane < 4) sh[threadIdx.x >> 6][lane * 4 + k] = s[k];
+    for (int off = kDwLanes; off < 64; off <<= 1) s[k] += __shfl_xor(s[k], off);
+    if (lane < kDwLanes) sh[threadIdx.x >> 6][lane * 4 + k] = s[k];
   }
   __syncthreads();
-  const int c = blockIdx.x * 16 + threadIdx.x;
-  if (threadIdx.x < 16 && c < d) {
+  const int c = blockIdx.x * 4 * kDwLanes + threadIdx.x;
+  if (threadIdx.x < 4 * kDwLanes && c < d) {
     double total = (sh[0][threadIdx.x] + sh[1][threadIdx.x]) + (sh[2][threadIdx.x] + sh[3][threadIdx.x]);
     if (accumulate) total += (double)dw[c];
     dw[c] = (float)total;
@@ -280,56 +319,62 @@ struct Shape { int threads, vectors; };
 Shape norm_shape(int64_t N, int d) {
   const int v = (d + 7) / 8;
   if (v <= 64) return {64, 1};
-  if (N >= 1024 && v <= 512) return {64, v <= 128 ? 2 : v <= 256 ? 4 : 8};
-  if (v <= 1024) return {256, v <= 256 ? 1 : v <= 512 ? 2 : 4};
+  if (v <= 128) return {64, 2};
+  if (v <= 256) return {256, 1};
+  if (v <= 512) return {256, 2};
+  if (v <= 1024) return {512, 2};
   return {1024, 2};
 }
+// Up to 128 vectors of eight a wave takes a row, four of them side by side; above, as many waves as the row has vectors for, with one each: idle
+// lanes cost more than barriers (65104 rows of 1536 in 256 and in 192 threads 182 and 153 us, 27901 of 3584 in 256 threads with two vectors and in 448
+// with one 173 and 150).
 Shape back_shape(int d) {
   const int v = (d + 7) / 8;
   if (v <= 128) return {64, v <= 64 ? 1 : 2};
-  if (v <= 1024) return {256, v <= 256 ? 1 : v <= 512 ? 2 : 4};
-  return {512, 4};
+  if (v <= 512) return {v <= 192 ? 192 : (v + 63) / 64 * 64, 1};
+  return {512, v <= 1024 ? 2 : 4};
 }
-int rows_side_by_side(const Shape& s) { return s.threads < 256 ? 256 / s.threads : 1; }
+int rows_side_by_side(const Shape& s) { return s.threads == 64 ? 4 : 1; }
+// Workgroups: two or more rows each, and as many as fill the chip's latencies without more rows under way than its memory takes well, which is two a
+// compute unit (of the fewest threads four, of the most one): 80000 rows of 2048, us, with 256, 512, 768, 1024 and 1280 of them: 351, 229, 238, 259, 282.
 int back_blocks(int64_t N, int d) {
-  const int rows = rows_side_by_side(back_shape(d));
-  const int64_t b = (N + rows - 1) / rows;
-  return (int)(b < 1024 ? b : 1024);
+  const Shape sh = back_shape(d);
+  const int64_t b = (N + 2 * rows_side_by_side(sh) - 1) / (2 * rows_side_by_side(sh));
+  const int most = sh.threads == 192 ? 1024 : sh.vectors > 1 && sh.threads == 512 ? 256 : 512;
+  return (int)(b < most ? b : most);
 }
 
+template <bool kXBf16, int kRes, int kT> void go_norm_threads(const NormArgs& a, int vectors, hipStream_t s) {
+  const dim3 grid((unsigned)a.N), block(kT);
+  if (vectors == 1) hipLaunchKernelGGL((k_rms_norm<kXBf16, kRes, kT, 1>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_rms_norm<kXBf16, kRes, kT, 2>), grid, block, 0, s, a);
+}
 template <bool kXBf16, int kRes> void go_norm(const NormArgs& a, hipStream_t s) {
   const Shape sh = norm_shape(a.N, a.d);
-  const int rows = rows_side_by_side(sh);
-  const dim3 grid((unsigned)((a.N + rows - 1) / rows)), block(sh.threads < 256 ? 256 : sh.threads);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
-  if (sh.threads == 64) {
-    if (sh.vectors == 1) go(k_rms_norm<kXBf16, kRes, 64, 1>);
-    else if (sh.vectors == 2) go(k_rms_norm<kXBf16, kRes, 64, 2>);
-    else if (sh.vectors == 4) go(k_rms_norm<kXBf16, kRes, 64, 4>);
-    else go(k_rms_norm<kXBf16, kRes, 64, 8>);
-  } else if (sh.threads == 256) {
-    if (sh.vectors == 1) go(k_rms_norm<kXBf16, kRes, 256, 1>);
-    else if (sh.vectors == 2) go(k_rms_norm<kXBf16, kRes, 256, 2>);
-    else go(k_rms_norm<kXBf16, kRes, 256, 4>);
-  } else {
-    go(k_rms_norm<kXBf16, kRes, 1024, 2>);
+  switch (sh.threads) {
+    case 64: go_norm_threads<kXBf16, kRes, 64>(a, sh.vectors, s); break;
+    case 256: go_norm_threads<kXBf16, kRes, 256>(a, sh.vectors, s); break;
+    case 512: go_norm_threads<kXBf16, kRes, 512>(a, sh.vectors, s); break;
+    default: go_norm_threads<kXBf16, kRes, 1024>(a, sh.vectors, s); break;
   }
 }
 
 template <bool kHBf16, bool kDyBf16> void go_back(const NormBackArgs& a, hipStream_t s) {
   const Shape sh = back_shape(a.d);
-  const dim3 grid((unsigned)back_blocks(a.N, a.d)), block(sh.threads < 256 ? 256 : sh.threads);
-  const size_t lds = sh.threads < 256 ? (size_t)a.d * 4 : 64 * 4;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, s, a); };
-  if (sh.threads == 64) {
-    if (sh.vectors == 1) go(k_rms_norm_back<kHBf16, kDyBf16, 64, 1>);
-    else go(k_rms_norm_back<kHBf16, kDyBf16, 64, 2>);
-  } else if (sh.threads == 256) {
-    if (sh.vectors == 1) go(k_rms_norm_back<kHBf16, kDyBf16, 256, 1>);
-    else if (sh.vectors == 2) go(k_rms_norm_back<kHBf16, kDyBf16, 256, 2>);
-    else go(k_rms_norm_back<kHBf16, kDyBf16, 256, 4>);
-  } else {
-    go(k_rms_norm_back<kHBf16, kDyBf16, 512, 4>);
+  const bool waves = sh.threads == 64;
+  const dim3 grid((unsigned)back_blocks(a.N, a.d)), block(waves ? 256 : sh.threads);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, waves ? (size_t)a.d * 4 : 64 * 4, s, a); };
+  switch (sh.threads * 8 + sh.vectors) {
+    case 64 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 64, 1>); break;
+    case 64 * 8 + 2: go(k_rms_norm_back<kHBf16, kDyBf16, 64, 2>); break;
+    case 192 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 192, 1>); break;
+    case 256 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 256, 1>); break;
+    case 320 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 320, 1>); break;
+    case 384 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 384, 1>); break;
+    case 448 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 448, 1>); break;
+    case 512 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 512, 1>); break;
+    case 512 * 8 + 2: go(k_rms_norm_back<kHBf16, kDyBf16, 512, 2>); break;
+    default: go(k_rms_norm_back<kHBf16, kDyBf16, 512, 4>); break;
   }
 }
 
@@ -347,13 +392,13 @@ extern "C" int mrl_rms_norm(const void* x, const void* residual, const void* wei
   if (N < 0 || N > kMaxRows || d <= 0 || d > kMaxWidth) return MRL_ERR_SHAPE;
   if (!is_float_type(x_dtype) || !is_float_type(weight_dtype) || !(is_float_type(y_dtype) || y_dtype == MRL_E4M3)) return MRL_ERR_DTYPE;
   if (residual != nullptr && !(residual_dtype == x_dtype || residual_dtype == MRL_F32)) return MRL_ERR_DTYPE;
-  if (!(eps > 0.f && eps < 1e30f) || (scale_block != 0 && (scale_block != 128 || y_dtype != MRL_E4M3))) return MRL_ERR_CONFIG;
+  if (!(eps >= 1e-30f && eps < 1e30f) || (scale_block != 0 && (scale_block != 128 || y_dtype != MRL_E4M3))) return MRL_ERR_CONFIG;
   if (N == 0) return MRL_OK;
   if (!x || !weight || !out_y || (residual != nullptr) != (out_sum != nullptr) || (y_dtype == MRL_E4M3) != (out_scale != nullptr))
     return MRL_ERR_NULL;
   const int rc = require_gfx950();
   if (rc != MRL_OK) return rc;
-  const NormArgs a = {x, residual, weight, token_mask, N, d, eps, weight_dtype == MRL_BF16, y_dtype, scale_block, out_sum, out_y, out_scale};
+  const NormArgs a = {x, residual, weight, token_mask, N, d, eps, 1.f / (float)d, weight_dtype == MRL_BF16, y_dtype, scale_block, out_sum, out_y, out_scale};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (x_dtype == MRL_BF16) {
     if (residual == nullptr) go_norm<true, 0>(a, s);
@@ -377,7 +422,7 @@ extern "C" int mrl_rms_norm_backward(const void* dy, const void* h, const void* 
                                      int32_t accumulate_dw, void* out_dx, float* out_dweight, void* workspace, size_t workspace_bytes, void* stream) {
   if (N < 0 || N > kMaxRows || d <= 0 || d > kMaxWidth) return MRL_ERR_SHAPE;
   if (!is_float_type(dy_dtype) || !is_float_type(h_dtype) || !is_float_type(weight_dtype) || !is_float_type(dx_dtype)) return MRL_ERR_DTYPE;
-  if (!(eps > 0.f && eps < 1e30f) || (accumulate_dw != 0 && accumulate_dw != 1)) return MRL_ERR_CONFIG;
+  if (!(eps >= 1e-30f && eps < 1e30f) || (accumulate_dw != 0 && accumulate_dw != 1)) return MRL_ERR_CONFIG;
   if ((N > 0 && (!dy || !h || !weight || !out_dx)) || (N == 0 && !out_dweight && !out_dx)) return MRL_ERR_NULL;
   if (out_dweight != nullptr && N > 0 &&
       (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < mrl_rms_norm_backward_workspace(N, d)))
@@ -389,11 +434,11 @@ extern "C" int mrl_rms_norm_backward(const void* dy, const void* h, const void* 
   const int ld = (int)round_up(d, 4), blocks = N > 0 ? back_blocks(N, d) : 0;
   float* parts = out_dweight != nullptr ? static_cast<float*>(workspace) : nullptr;
   if (N > 0) {
-    const NormBackArgs a = {dy, h, weight, d_residual, token_mask, N, d, eps, weight_dtype == MRL_BF16, dx_dtype == MRL_BF16, out_dx, parts, ld};
+    const NormBackArgs a = {dy, h, weight, d_residual, token_mask, N, d, eps, 1.f / (float)d, weight_dtype == MRL_BF16, dx_dtype == MRL_BF16, out_dx, parts, ld};
     if (h_dtype == MRL_BF16) { if (dy_dtype == MRL_BF16) go_back<true, true>(a, s); else go_back<true, false>(a, s); }
     else { if (dy_dtype == MRL_BF16) go_back<false, true>(a, s); else go_back<false, false>(a, s); }
   }
   if (out_dweight != nullptr)                            // (of no rows: zeros)
-    hipLaunchKernelGGL(k_rms_norm_dw, dim3((unsigned)((d + 15) / 16)), dim3(256), 0, s, parts, blocks, ld, d, accumulate_dw, out_dweight);
+    hipLaunchKernelGGL(k_rms_norm_dw, dim3((unsigned)((d + 4 * kDwLanes - 1) / (4 * kDwLanes))), dim3(256), 0, s, parts, blocks, ld, d, accumulate_dw, out_dweight);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
 }

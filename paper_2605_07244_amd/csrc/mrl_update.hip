@@ -16,12 +16,13 @@
 namespace mrl {
 namespace {
 
-constexpr int kChunk = 2048;                 // elements of a tensor that a workgroup takes at a time: eight blocks of 8-bit states
+constexpr int kNormChunk = 2048;             // elements of a tensor that a workgroup takes at a time: norm, eight a thread
+constexpr int kAdamThreads = 64, kAdamChunk = kAdamThreads * 4;    // ... update, four a thread
 constexpr int kStateBlock = 256;             // elements that share a scale: a wave's four a lane
 
 // ------------------------------------------------------------------ global norm
 constexpr int kNormTensors = 96;             // a launch: 96 * 24 bytes of arguments
-constexpr int kNormBlocks = 1024;            // workgroups of a launch at most, a partial sum each
+constexpr int kNormBlocks = 2048;            // workgroups of a launch at most, a partial sum each
 struct NormTable {
   const void* grad[kNormTensors];
   int64_t n[kNormTensors];
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(256) void k_square_sums(NormTable a) {
   double s = 0.0;
   for (int chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
     const int i = tensor_of<kNormTensors>(a.chunk0, chunk);
-    const int64_t at = (int64_t)(chunk - a.chunk0[i]) * kChunk;
-    const int left = (int)min((int64_t)kChunk, a.n[i] - at), c = threadIdx.x * 8;
+    const int64_t at = (int64_t)(chunk - a.chunk0[i]) * kNormChunk;
+    const int left = (int)min((int64_t)kNormChunk, a.n[i] - at), c = threadIdx.x * 8;
     if (a.bf16[i >> 5] >> (i & 31) & 1) {
       Eight<true> g;
       g.load(static_cast<const uint16_t*>(a.grad[i]) + at, c, left);
@@ -94,16 +95,21 @@ __global__ __launch_bounds__(1024) void k_norm_coef(const double* parts, int n, 
 }
 
 // ------------------------------------------------------------------ AdamW
-constexpr int kAdamTensors = 44;             // a launch: 44 * 84 bytes of arguments
-struct AdamTensor {
-  float* param; uint16_t* copy; const void* grad; void* m; void* v; float* m_scale; float* v_scale;
-  int64_t n; float weight_decay; int32_t grad_bf16; int32_t place /*in the call*/;
+template <bool kCodes> struct AdamTensor;
+template <> struct AdamTensor<false> {
+  float* param; uint16_t* copy; const void* grad; void* m; void* v;
+  int64_t n; float weight_decay; uint32_t place_bf16 /*twice the place in the call, plus 1 where the gradient is bf16*/;
 };
-struct AdamTable {
-  AdamTensor t[kAdamTensors];
-  int32_t chunk0[kAdamTensors];
+template <> struct AdamTensor<true> {
+  float* param; uint16_t* copy; const void* grad; void* m; void* v; float* m_scale; float* v_scale;
+  int64_t n; float weight_decay; uint32_t place_bf16;
+};
+template <bool kCodes> struct AdamTable {
+  static constexpr int kTensors = kCodes ? 48 : 64;     // a launch: 3.8 and 3.9 KB of arguments
+  AdamTensor<kCodes> t[kTensors];
+  int32_t chunk0[kTensors];                             // as above
   int32_t skip_nonfinite;
-  float lr, inv_fix1, inv_root_fix2;         // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float lr, inv_fix1, inv_root_fix2;                    // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
   float b1, one_b1, b2, one_b2, eps;
   double beta1, beta2;
   int64_t step;
@@ -128,8 +134,8 @@ __host__ __device__ inline uint32_t mix(uint32_t x) {
   x = (x ^ x >> 15) * 0xBB67AE85u;
   return x ^ x >> 16;
 }
-__device__ inline uint32_t key_of(uint64_t seed, int64_t step, int place) {
-  return mix((uint32_t)seed ^ mix((uint32_t)(seed >> 32) ^ mix((uint32_t)step ^ mix((uint32_t)place))));
+__device__ inline uint32_t key_of(uint64_t seed, int64_t step, uint32_t place) {
+  return mix((uint32_t)seed ^ mix((uint32_t)(seed >> 32) ^ mix((uint32_t)step ^ mix(place))));
 }
 
 // x >= 0, at most 448 (a little above by rounding): the e4m3 value below or above, above with the probability of the fraction.  u: 16
@@ -141,115 +147,34 @@ __device__ inline float to_code(float x, uint32_t u16) {
   return fminf(floorf(fmaf((float)u16, 0x1p-16f, x * per_step)) * step, kE4m3Max);
 }
 
-template <bool kCodes>
-__global__ __launch_bounds__(256) void k_adamw(AdamTable a) {
-  const int i = tensor_of<kAdamTensors>(a.chunk0, blockIdx.x);
-  const AdamTensor& t = a.t[i];
-  const int64_t at = (int64_t)((int)blockIdx.x - a.chunk0[i]) * kChunk;
-  const float coef = a.coef != nullptr ? *a.coef : 1.f;
-  if (a.skip_nonfinite && !(fabsf(coef) < INFINITY)) return;
-  float lr = a.lr, inv_fix1 = a.inv_fix1, inv_root_fix2 = a.inv_root_fix2;
-  int64_t step = a.step;
-  if (a.lr_dev != nullptr) lr = *a.lr_dev;
-  if (a.step_dev != nullptr) {
-    step = max(*a.step_dev, (int64_t)1);
-    inv_fix1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
-    inv_root_fix2 = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int left = (int)min((int64_t)kChunk, t.n - at);
-  const uint32_t key = kCodes ? mix(key_of(a.seed, step, t.place) + (uint32_t)(at >> 32)) : 0;
-#pragma unroll
-  for (int k = 0; k < kChunk / 1024; ++k) {
-    const int c = k * 1024 + wave * kStateBlock + lane * 4;
-    if (k * 1024 + wave * kStateBlock >= left) return;  // (whole waves)
-    float p[4], g[4], m[4], v[4], root[4];
-    const bool whole = c + 4 <= left;
-    const int some = whole ? 4 : c < left ? left - c : 0;
-    // every element of the four that the tensor has; the others as zeros
-    if (whole) {
-      const u32x4 pw = load_any<4, u32x4>(t.param + at + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = __uint_as_float(pw[e]);
-      if (t.grad_bf16) {
-        const u32x2 w = load_any<2, u32x2>(static_cast<const uint16_t*>(t.grad) + at + c);
-        g[0] = bf16_low(w[0]); g[1] = bf16_high(w[0]); g[2] = bf16_low(w[1]); g[3] = bf16_high(w[1]);
-      } else {
-        const u32x4 w = load_any<4, u32x4>(static_cast<const float*>(t.grad) + at + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) g[e] = __uint_as_float(w[e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = e < some ? t.param[at + c + e] : 0.f;
-        g[e] = e >= some ? 0.f : t.grad_bf16 ? bf16_low(static_cast<const uint16_t*>(t.grad)[at + c + e]) : static_cast<const float*>(t.grad)[at + c + e];
-      }
-    }
-    if (kCodes) {
-      uint32_t mw = 0, vw = 0;
-      const uint8_t *mp = static_cast<const uint8_t*>(t.m) + at + c, *vp = static_cast<const uint8_t*>(t.v) + at + c;
-      if (whole) {
-        mw = load_any<1, uint32_t>(mp);
-        vw = load_any<1, uint32_t>(vp);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-          if (e < some) { mw |= (uint32_t)mp[e] << 8 * e; vw |= (uint32_t)vp[e] << 8 * e; }
-      }
-      const int64_t block = (at + c) / kStateBlock;
-      const float ms = t.m_scale[block], vs = t.v_scale[block];
-      const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, true);
-      const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, true);
-      m[0] = m01[0] * ms; m[1] = m01[1] * ms; m[2] = m23[0] * ms; m[3] = m23[1] * ms;
-      v[0] = v01[0] * vs; v[1] = v01[1] * vs; v[2] = v23[0] * vs; v[3] = v23[1] * vs;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] *= v[e];
-    } else if (whole) {
-      const u32x4 mw = load_any<4, u32x4>(static_cast<const float*>(t.m) + at + c), vw = load_any<4, u32x4>(static_cast<const float*>(t.v) + at + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { m[e] = __uint_as_float(mw[e]); v[e] = __uint_as_float(vw[e]); }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        m[e] = e < some ? static_cast<const float*>(t.m)[at + c + e] : 0.f;
-        v[e] = e < some ? static_cast<const float*>(t.v)[at + c + e] : 0.f;
-      }
-    }
+// Products and sums that are rounded one by one: the compiler may not make a fused one of two.
+__device__ inline float times(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+__device__ inline float plus(float a, float b) {
+#pragma clang fp contract(off)
+  return a + b;
+}
+
+// What the elements of a launch share.
+struct Rates { float lr, inv_fix1, inv_root_fix2, coef, b1, one_b1, b2, one_b2, eps, decay; };
+
+// Four elements of a tensor and their moments, in registers.
+struct Four {
+  float p[4], g[4], m[4], v[4], root[4];
+  __device__ void update(const Rates& r) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float ge = g[e] * coef;
-      m[e] = fmaf(a.b1, m[e], a.one_b1 * ge);
-      v[e] = fmaf(a.b2, v[e], a.one_b2 * ge * ge);
+      const float ge = g[e] * r.coef;
+      m[e] = plus(times(r.b1, m[e]), times(r.one_b1, ge));
+      v[e] = plus(times(r.b2, v[e]), times(times(r.one_b2, ge), ge));
       root[e] = sqrtf(v[e]);
-      p[e] = fmaf(-lr, fmaf(t.weight_decay, p[e], m[e] * inv_fix1 / fmaf(root[e], inv_root_fix2, a.eps)), p[e]);
+      p[e] = fmaf(-r.lr, fmaf(r.decay, p[e], m[e] * r.inv_fix1 / fmaf(root[e], r.inv_root_fix2, r.eps)), p[e]);
     }
-    if (whole) {
-      store_any<4>(t.param + at + c, u32x4{__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3])});
-      if (t.copy != nullptr) store_any<2>(t.copy + at + c, u32x2{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3])});
-    } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e) {
-        if (e >= some) continue;
-        t.param[at + c + e] = p[e];
-        if (t.copy != nullptr) t.copy[at + c + e] = (uint16_t)pack_bf16(p[e], 0.f);
-      }
-    }
-    if (!kCodes) {
-      if (whole) {
-        store_any<4>(static_cast<float*>(t.m) + at + c, u32x4{__float_as_uint(m[0]), __float_as_uint(m[1]), __float_as_uint(m[2]), __float_as_uint(m[3])});
-        store_any<4>(static_cast<float*>(t.v) + at + c, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-      } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e) {
-          if (e >= some) continue;
-          static_cast<float*>(t.m)[at + c + e] = m[e];
-          static_cast<float*>(t.v)[at + c + e] = v[e];
-        }
-      }
-      continue;
-    }
-    // 8-bit moments: m and sqrt(v) as multiples of their largest in 256 elements over 448
+  }
+  // Codes of the moments and the block's scales; the wave's 64 fours are a block, elements from `some` on count as zeros.
+  __device__ void encode(int some, uint32_t first, uint32_t key, uint32_t* mw, uint32_t* vw, float* m_scale, float* v_scale) {
     uint32_t m_most = kScaleLeast, v_most = kScaleLeast;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -258,36 +183,143 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable a) {
       v_most = larger(v_most, magnitude(root[e]));
     }
     const float m_max = __uint_as_float(wave_max(m_most)), v_max = __uint_as_float(wave_max(v_most));
-    const float m_inv = kE4m3Max / m_max, v_inv = kE4m3Max / v_max;
+    const float m_inv = times(1.f / m_max, kE4m3Max), v_inv = times(1.f / v_max, kE4m3Max);
     float mq[4], vq[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t bits = mix((uint32_t)(at + c + e) ^ key);
+      const uint32_t bits = mix((first + e) ^ key);
       mq[e] = copysignf(to_code(fabsf(m[e]) * m_inv, bits & 0xffffu), m[e]);
       // a positive root keeps a positive code: at zero the next step would divide by that step's gradient alone
       vq[e] = fmaxf(to_code(root[e] * v_inv, bits >> 16), root[e] > 0.f ? 0x1p-9f : 0.f);
     }
-    const uint32_t mw = pack_e4m3(mq[0], mq[1], mq[2], mq[3]), vw = pack_e4m3(vq[0], vq[1], vq[2], vq[3]);
-    uint8_t *mp = static_cast<uint8_t*>(t.m) + at + c, *vp = static_cast<uint8_t*>(t.v) + at + c;
-    if (whole) {
-      store_any<1>(mp, mw);
-      store_any<1>(vp, vw);
-    } else {
+    *mw = pack_e4m3(mq[0], mq[1], mq[2], mq[3]);
+    *vw = pack_e4m3(vq[0], vq[1], vq[2], vq[3]);
+    *m_scale = times(m_max, 1.f / kE4m3Max);
+    *v_scale = times(v_max, 1.f / kE4m3Max);
+  }
+  __device__ void decode(uint32_t mw, uint32_t vw, float m_scale, float v_scale) {
+    const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, true);
+    const auto v01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw, true);
+    m[0] = times(m01[0], m_scale); m[1] = times(m01[1], m_scale); m[2] = times(m23[0], m_scale); m[3] = times(m23[1], m_scale);
+    v[0] = times(v01[0], v_scale); v[1] = times(v01[1], v_scale); v[2] = times(v23[0], v_scale); v[3] = times(v23[1], v_scale);
 #pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < some) { mp[e] = (uint8_t)(mw >> 8 * e); vp[e] = (uint8_t)(vw >> 8 * e); }
+    for (int e = 0; e < 4; ++e) v[e] = times(v[e], v[e]);
+  }
+};
+__device__ inline u32x4 as_words(const float (&x)[4]) {
+  return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+}
+__device__ inline void as_floats(u32x4 w, float (&x)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
+}
+
+// A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.
+template <bool kCodes>
+__global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
+  const int i = tensor_of<AdamTable<kCodes>::kTensors>(a.chunk0, blockIdx.x);
+  const AdamTensor<kCodes>& t = a.t[i];
+  const bool grad_bf16 = t.place_bf16 & 1;
+  const int64_t at = (int64_t)((int)blockIdx.x - a.chunk0[i]) * kAdamChunk;
+  Rates r = {a.lr, a.inv_fix1, a.inv_root_fix2, a.coef != nullptr ? *a.coef : 1.f, a.b1, a.one_b1, a.b2, a.one_b2, a.eps, t.weight_decay};
+  if (a.skip_nonfinite && !(fabsf(r.coef) < INFINITY)) return;
+  int64_t step = a.step;
+  if (a.lr_dev != nullptr) r.lr = *a.lr_dev;
+  if (a.step_dev != nullptr) {
+    step = max(*a.step_dev, (int64_t)1);
+    r.inv_fix1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
+    r.inv_root_fix2 = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int left = (int)min((int64_t)kAdamChunk, t.n - at);
+  const uint32_t key = kCodes ? mix(key_of(a.seed, step, t.place_bf16 >> 1) + (uint32_t)(at >> 32)) : 0;
+  float* const param = t.param + at;
+  uint16_t* const copy = t.copy + at;
+  const float* const grad = static_cast<const float*>(t.grad) + at;
+  const uint16_t* const grad16 = static_cast<const uint16_t*>(t.grad) + at;
+  float *const m = static_cast<float*>(t.m) + at, *const v = static_cast<float*>(t.v) + at;
+  uint8_t *const mc = static_cast<uint8_t*>(t.m) + at, *const vc = static_cast<uint8_t*>(t.v) + at;
+  float *m_scale = nullptr, *v_scale = nullptr;
+  if constexpr (kCodes) { m_scale = t.m_scale + at / kStateBlock; v_scale = t.v_scale + at / kStateBlock; }
+  if (left == kAdamChunk) {
+    const int block = wave, c = block * kStateBlock + lane * 4;
+    Four f;
+    const u32x4 pw = load_stream<4, u32x4>(param + c);
+    if constexpr (kCodes) {
+      const uint32_t mw = load_stream<1, uint32_t>(mc + c), vw = load_stream<1, uint32_t>(vc + c);
+      f.decode(mw, vw, m_scale[block], v_scale[block]);
+    } else {
+      const u32x4 mw = load_stream<4, u32x4>(m + c), vw = load_stream<4, u32x4>(v + c);
+      as_floats(mw, f.m);
+      as_floats(vw, f.v);
     }
-    if (lane == 0) {
-      const int64_t block = (at + c) / kStateBlock;
-      t.m_scale[block] = m_max / kE4m3Max;
-      t.v_scale[block] = v_max / kE4m3Max;
+    if (grad_bf16) {
+      const u32x2 w = load_stream<2, u32x2>(grad16 + c);
+      as_floats(u32x4{w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u}, f.g);
+    } else {
+      as_floats(load_stream<4, u32x4>(grad + c), f.g);
+    }
+    as_floats(pw, f.p);
+    f.update(r);
+    store_stream<4>(param + c, as_words(f.p));
+    if (t.copy != nullptr) store_stream<2>(copy + c, u32x2{pack_bf16(f.p[0], f.p[1]), pack_bf16(f.p[2], f.p[3])});
+    if constexpr (kCodes) {
+      uint32_t mw, vw;
+      float ms, vs;
+      f.encode(4, (uint32_t)(at + c), key, &mw, &vw, &ms, &vs);
+      store_stream<1>(mc + c, mw);
+      store_stream<1>(vc + c, vw);
+      if (lane == 0) { m_scale[block] = ms; v_scale[block] = vs; }
+    } else {
+      store_stream<4>(m + c, as_words(f.m));
+      store_stream<4>(v + c, as_words(f.v));
+    }
+    return;
+  }
+  // a tensor's last chunk, element by element
+  if (wave * kStateBlock < left) {
+    const int block = wave;
+    const int c = block * kStateBlock + lane * 4, some = min(max(left - c, 0), 4);
+    Four f;
+    uint32_t mw = 0, vw = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in = e < some;
+      f.p[e] = in ? param[c + e] : 0.f;
+      f.g[e] = !in ? 0.f : grad_bf16 ? bf16_low(grad16[c + e]) : grad[c + e];
+      if constexpr (kCodes) {
+        if (in) { mw |= (uint32_t)mc[c + e] << 8 * e; vw |= (uint32_t)vc[c + e] << 8 * e; }
+      } else {
+        f.m[e] = in ? m[c + e] : 0.f;
+        f.v[e] = in ? v[c + e] : 0.f;
+      }
+    }
+    if constexpr (kCodes) f.decode(mw, vw, m_scale[block], v_scale[block]);
+    f.update(r);
+    float ms, vs;
+    if constexpr (kCodes) f.encode(some, (uint32_t)(at + c), key, &mw, &vw, &ms, &vs);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (e >= some) continue;
+      param[c + e] = f.p[e];
+      if (t.copy != nullptr) copy[c + e] = (uint16_t)pack_bf16(f.p[e], 0.f);
+      if constexpr (kCodes) {
+        mc[c + e] = (uint8_t)(mw >> 8 * e);
+        vc[c + e] = (uint8_t)(vw >> 8 * e);
+      } else {
+        m[c + e] = f.m[e];
+        v[c + e] = f.v[e];
+      }
+    }
+    if constexpr (kCodes) {
+      if (lane == 0) { m_scale[block] = ms; v_scale[block] = vs; }
     }
   }
 }
 
 // ------------------------------------------------------------------ host
 constexpr int64_t kMaxElements = (int64_t)1 << 40;
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+int64_t chunks_of(int64_t n, int chunk) { return (n + chunk - 1) / chunk; }
 
 int check_tensors(const mrl_param_tensor* t, int32_t count, bool update, bool codes) {
   if (count < 0) return MRL_ERR_SHAPE;
@@ -297,7 +329,7 @@ int check_tensors(const mrl_param_tensor* t, int32_t count, bool update, bool co
     if (t[i].n < 0 || t[i].n > kMaxElements) return MRL_ERR_SHAPE;
     if (t[i].grad_dtype != MRL_F32 && t[i].grad_dtype != MRL_BF16) return MRL_ERR_DTYPE;
     if (t[i].n == 0) continue;
-    chunks += chunks_of(t[i].n);
+    chunks += chunks_of(t[i].n, update ? kAdamChunk : kNormChunk);
     if (!t[i].grad) return MRL_ERR_NULL;
     if (!update) continue;
     if (!t[i].param || !t[i].m || !t[i].v || (codes && (!t[i].m_scale || !t[i].v_scale))) return MRL_ERR_NULL;
@@ -321,10 +353,44 @@ int64_t norm_parts(const mrl_param_tensor* t, int32_t count) {
   int64_t parts = 0;
   in_launches<kNormTensors>(t, count, [&](int32_t first, int32_t last) {
     int64_t chunks = 0;
-    for (int32_t i = first; i < last; ++i) chunks += chunks_of(t[i].n);
+    for (int32_t i = first; i < last; ++i) chunks += chunks_of(t[i].n, kNormChunk);
     parts += std::min<int64_t>(chunks, kNormBlocks);
   });
   return parts;
+}
+
+template <bool kCodes>
+void go_adamw(const mrl_param_tensor* tensors, int32_t count, const mrl_adamw_config& cfg, const float* grad_coef, hipStream_t s) {
+  using Table = AdamTable<kCodes>;
+  static_assert(sizeof(Table) <= 4096, "kernel arguments");
+  in_launches<Table::kTensors>(tensors, count, [&](int32_t first, int32_t last) {
+    Table a = {};
+    int k = 0;
+    int64_t chunks = 0;
+    for (int32_t i = first; i < last; ++i) {
+      const mrl_param_tensor& t = tensors[i];
+      if (t.n == 0) continue;
+      AdamTensor<kCodes>& to = a.t[k];
+      to.param = t.param; to.copy = static_cast<uint16_t*>(t.copy); to.grad = t.grad; to.m = t.m; to.v = t.v;
+      if constexpr (kCodes) { to.m_scale = t.m_scale; to.v_scale = t.v_scale; }
+      to.n = t.n; to.weight_decay = t.weight_decay; to.place_bf16 = 2u * (uint32_t)i + (t.grad_dtype == MRL_BF16);
+      a.chunk0[k] = (int32_t)chunks;
+      chunks += chunks_of(t.n, kAdamChunk);
+      ++k;
+    }
+    for (; k < Table::kTensors; ++k) a.chunk0[k] = INT32_MAX;
+    a.skip_nonfinite = cfg.skip_nonfinite;
+    a.beta1 = cfg.beta1; a.beta2 = cfg.beta2;
+    a.lr = (float)cfg.lr;
+    a.b1 = (float)cfg.beta1; a.one_b1 = (float)(1.0 - cfg.beta1);
+    a.b2 = (float)cfg.beta2; a.one_b2 = (float)(1.0 - cfg.beta2);
+    a.eps = (float)cfg.eps;
+    a.step = cfg.step; a.seed = cfg.seed;
+    a.inv_fix1 = (float)(1.0 / (1.0 - power(cfg.beta1, cfg.step)));
+    a.inv_root_fix2 = (float)(1.0 / std::sqrt(1.0 - power(cfg.beta2, cfg.step)));
+    a.lr_dev = cfg.lr_dev; a.step_dev = cfg.step_dev; a.coef = grad_coef;
+    hipLaunchKernelGGL(k_adamw<kCodes>, dim3((unsigned)chunks), dim3(kAdamThreads), 0, s, a);
+  });
 }
 
 }  // namespace
@@ -359,7 +425,7 @@ extern "C" int mrl_grad_norm(const mrl_param_tensor* tensors, int32_t count, dou
       a.n[k] = tensors[i].n;
       a.chunk0[k] = (int32_t)chunks;
       if (tensors[i].grad_dtype == MRL_BF16) a.bf16[k >> 5] |= 1u << (k & 31);
-      chunks += chunks_of(tensors[i].n);
+      chunks += chunks_of(tensors[i].n, kNormChunk);
       ++k;
     }
     for (; k < kNormTensors; ++k) a.chunk0[k] = INT32_MAX;
@@ -386,31 +452,8 @@ extern "C" int mrl_adamw(const mrl_param_tensor* tensors, int32_t count, const m
   rc = require_gfx950();
   if (rc != MRL_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  in_launches<kAdamTensors>(tensors, count, [&](int32_t first, int32_t last) {
-    AdamTable a = {};
-    int k = 0;
-    int64_t chunks = 0;
-    for (int32_t i = first; i < last; ++i) {
-      const mrl_param_tensor& t = tensors[i];
-      if (t.n == 0) continue;
-      a.t[k] = {t.param, static_cast<uint16_t*>(t.copy), t.grad, t.m, t.v, t.m_scale, t.v_scale, t.n, t.weight_decay, t.grad_dtype == MRL_BF16, i};
-      a.chunk0[k] = (int32_t)chunks;
-      chunks += chunks_of(t.n);
-      ++k;
-    }
-    for (; k < kAdamTensors; ++k) a.chunk0[k] = INT32_MAX;
-    a.skip_nonfinite = cfg->skip_nonfinite;
-    a.beta1 = cfg->beta1; a.beta2 = cfg->beta2;
-    a.lr = (float)cfg->lr;
-    a.b1 = (float)cfg->beta1; a.one_b1 = (float)(1.0 - cfg->beta1);
-    a.b2 = (float)cfg->beta2; a.one_b2 = (float)(1.0 - cfg->beta2);
-    a.eps = (float)cfg->eps;
-    a.step = cfg->step; a.seed = cfg->seed;
-    a.inv_fix1 = (float)(1.0 / (1.0 - power(cfg->beta1, cfg->step)));
-    a.inv_root_fix2 = (float)(1.0 / std::sqrt(1.0 - power(cfg->beta2, cfg->step)));
-    a.lr_dev = cfg->lr_dev; a.step_dev = cfg->step_dev; a.coef = grad_coef;
-    hipLaunchKernelGGL(codes ? k_adamw<true> : k_adamw<false>, dim3((unsigned)chunks), dim3(256), 0, s, a);
-  });
+  if (codes) go_adamw<true>(tensors, count, *cfg, grad_coef, s);
+  else go_adamw<false>(tensors, count, *cfg, grad_coef, s);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
 }
 

@@ -14,6 +14,15 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <class V, int kAlign> struct __attribute__((packed, aligned(kAlign))) AtAnyAddress { V v; };
 template <int kAlign, class V> __device__ inline V load_any(const void* p) { return static_cast<const AtAnyAddress<V, kAlign>*>(p)->v; }
 template <int kAlign, class V> __device__ inline void store_any(void* p, V v) { static_cast<AtAnyAddress<V, kAlign>*>(p)->v = v; }
+// The same for what nothing near will read again.
+template <int kAlign, class V> __device__ inline V load_stream(const void* p) {
+  typedef V Unaligned __attribute__((aligned(kAlign)));
+  return __builtin_nontemporal_load(static_cast<const Unaligned*>(p));
+}
+template <int kAlign, class V> __device__ inline void store_stream(void* p, V v) {
+  typedef V Unaligned __attribute__((aligned(kAlign)));
+  __builtin_nontemporal_store(v, static_cast<Unaligned*>(p));
+}
 
 __device__ inline float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -61,14 +70,17 @@ template <> struct Eight<false> {
   __device__ float operator[](int e) const { return __uint_as_float(w[e >> 2][e & 3]); }
 };
 
+template <bool kStream, int kAlign, class V> __device__ inline void store_as(void* p, V v) {
+  if (kStream) store_stream<kAlign>(p, v); else store_any<kAlign>(p, v);
+}
 // Elements c .. c + 7 of a row of d, those below d.
-__device__ inline void store_eight(void* row, bool bf16, int c, int d, const float (&v)[8]) {
+template <bool kStream = false> __device__ inline void store_eight(void* row, bool bf16, int c, int d, const float (&v)[8]) {
   if (c >= d) return;
   if (bf16) {
     uint16_t* p = static_cast<uint16_t*>(row) + c;
     const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     if (c + 8 <= d) {
-      store_any<2>(p, w);
+      store_as<kStream, 2>(p, w);
     } else {
 #pragma unroll
       for (int e = 0; e < 7; ++e)
@@ -77,8 +89,8 @@ __device__ inline void store_eight(void* row, bool bf16, int c, int d, const flo
   } else {
     float* p = static_cast<float*>(row) + c;
     if (c + 8 <= d) {
-      store_any<4>(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-      store_any<4>(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+      store_as<kStream, 4>(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+      store_as<kStream, 4>(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
     } else {
 #pragma unroll
       for (int e = 0; e < 7; ++e)
