@@ -154,7 +154,7 @@ _HOST = None
 
 class _NoHost:
     """Takes nothing as it is: every call goes through ctypes."""
-    advantages = align = rms_norm = rms_norm_backward = staticmethod(lambda *args: None)
+    advantages = align = rms_norm = rms_norm_backward = grad_norm = adamw = staticmethod(lambda *args: None)
 
 
 def _load_host():
@@ -170,7 +170,7 @@ def _load_host():
         why = f"was built against torch {module.torch_version}, this is {torch.__version__}"
     except (ImportError, OSError) as e:        # (a file that is not there is an ImportError or FileNotFoundError)
         why = str(e)
-    warnings.warn(f"{path}: {why}; advantages, alignment and norms go through ctypes, which takes 4 - 5 us more a call "
+    warnings.warn(f"{path}: {why}; advantages, alignment, norms and updates go through ctypes, which takes 2 - 6 us more a call "
                   "(`python -m paper_2605_07244_amd.build` builds it)", RuntimeWarning, stacklevel=4)
     return None
 
@@ -551,6 +551,7 @@ class GradPlan:
 
     def _fill(self, count):
         self.count, self.table = count, (_ParamTensor * count)()
+        self.address = ctypes.addressof(self.table)
 
 
 class AdamWPlan(GradPlan):
@@ -611,6 +612,12 @@ def adamw_plan(params, grads, copies=None, m=None, v=None, m_scale=None, v_scale
 def grad_norm(plan: GradPlan, max_norm: float = float("inf"), out=None):
     """mrl_grad_norm: a float32 tensor [norm, clip coefficient] of the plan's gradients (not synchronised)."""
     if out is None:
+        if _native:
+            dev = _get_device()
+            r = (_HOST or _host()).grad_norm(plan.address, plan.count, max_norm, plan.workspace, dev, _raw_stream(dev))
+            if r is not None:
+                _check(r[0], "mrl_grad_norm")
+                return r[1]
         out = torch.empty(2, dtype=torch.float32, device=plan.device)
     elif out.numel() != 2:
         raise ValueError("out must have two entries")
@@ -624,6 +631,12 @@ def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
     """mrl_adamw: updates the plan's params, moments and copies in place.  step counts from 1.  lr and step are numbers or, for graphs that are
     replayed with other values, tensors of one float32 and one int64 on the GPU.  norm_coef: what grad_norm returned, whose coefficient the gradients
     are multiplied by; skip_nonfinite leaves everything as it is where that is not finite."""
+    if _native:
+        dev = _get_device()
+        r = (_HOST or _host()).adamw(plan.address, plan.count, plan.workspace, lr, step, beta1, beta2, eps, norm_coef, seed, skip_nonfinite,
+                                     plan.state_dtype, dev, _raw_stream(dev))
+        if r is not None:
+            return _check(r[0], "mrl_adamw")
     c = _AdamWConfig(0.0, beta1, beta2, eps, 1, int(seed) & 0xFFFFFFFFFFFFFFFF, plan.state_dtype, int(bool(skip_nonfinite)), None, None)
     for name, x, dtype in (("lr", lr, torch.float32), ("step", step, torch.int64)):
         if isinstance(x, torch.Tensor):

@@ -228,11 +228,66 @@ PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// (address of a plan's table, tensors, max_norm, workspace, device, stream) -> (status, [norm, coefficient]) or None
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    int64_t table, device, stream;
+    int32_t count;
+    void* ws;
+    if (n != 6 || !int_arg(a[0], &table) || !int32_arg(a[1], &count) || !PyFloat_CheckExact(a[2]) || !tensor_arg(a[3], at::kByte, false, &ws) ||
+        !int_arg(a[4], &device) || !int_arg(a[5], &stream))
+      Py_RETURN_NONE;
+    const at::Tensor& w = THPVariable_Unpack(a[3]);
+    if (w.get_device() != device) Py_RETURN_NONE;
+    const double max_norm = PyFloat_AS_DOUBLE(a[2]);
+    const size_t bytes = (size_t)w.numel();
+    at::Tensor out = new_like(w, {2}, at::kFloat);
+    float* const out_ptr = static_cast<float*>(out.mutable_data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_grad_norm(reinterpret_cast<const mrl_param_tensor*>(table), count, max_norm, out_ptr, ws, bytes, reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(std::move(out)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// (address of a plan's table, tensors, workspace (which says where the plan is), lr, step, beta1, beta2, eps, norm_coef or None, seed, skip_nonfinite,
+// state_dtype, device, stream) -> (status,) or None
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    int64_t table, device, stream, step, seed;
+    int32_t count, state;
+    void *ws, *coef;
+    if (n != 14 || !int_arg(a[0], &table) || !int32_arg(a[1], &count) || !tensor_arg(a[2], at::kByte, false, &ws) || !PyFloat_CheckExact(a[3]) ||
+        !int_arg(a[4], &step) || !PyFloat_CheckExact(a[5]) || !PyFloat_CheckExact(a[6]) || !PyFloat_CheckExact(a[7]) ||
+        !tensor_arg(a[8], at::kFloat, true, &coef) || !int_arg(a[9], &seed) || (a[10] != Py_True && a[10] != Py_False) || !int32_arg(a[11], &state) ||
+        !int_arg(a[12], &device) || !int_arg(a[13], &stream) || THPVariable_Unpack(a[2]).get_device() != device || seed < 0)
+      Py_RETURN_NONE;
+    if (coef != nullptr && (THPVariable_Unpack(a[8]).numel() != 2 || THPVariable_Unpack(a[8]).get_device() != device)) Py_RETURN_NONE;
+    const mrl_adamw_config c = {PyFloat_AS_DOUBLE(a[3]), PyFloat_AS_DOUBLE(a[5]), PyFloat_AS_DOUBLE(a[6]), PyFloat_AS_DOUBLE(a[7]), step, (uint64_t)seed,
+                                state, a[10] == Py_True, nullptr, nullptr};
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_adamw(reinterpret_cast<const mrl_param_tensor*>(table), count, &c, coef != nullptr ? static_cast<const float*>(coef) + 1 : nullptr,
+                   reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(i)", rc);
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
 PyMethodDef methods[] = {
     {"advantages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(advantages)), METH_FASTCALL, nullptr},
     {"align", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(align)), METH_FASTCALL, nullptr},
     {"rms_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm)), METH_FASTCALL, nullptr},
     {"rms_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm_backward)), METH_FASTCALL, nullptr},
+    {"grad_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(grad_norm)), METH_FASTCALL, nullptr},
+    {"adamw", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "mrl_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -335,12 +335,15 @@ Shape back_shape(int d) {
   return {512, v <= 1024 ? 2 : 4};
 }
 int rows_side_by_side(const Shape& s) { return s.threads == 64 ? 4 : 1; }
-// Workgroups: two or more rows each, and as many as fill the chip's latencies without more rows under way than its memory takes well, which is two a
-// compute unit (of the fewest threads four, of the most one): 80000 rows of 2048, us, with 256, 512, 768, 1024 and 1280 of them: 351, 229, 238, 259, 282.
+// Workgroups: two or more rows each, and as many as cover the latencies of a row without more rows under way than the memory takes well: 80000 rows of 2048,
+// us, with 256, 512, 768, 1024 and 1280 workgroups: 351, 229, 238, 259, 282.  The partial sums of many are worth it to long calls only: rows of 4096 in
+// 512 threads, with 256 and 512 workgroups: 1000 rows 13.8 and 16.2, 4000 28.8 and 31.6, 24414 156 and 154; of 1536 in 192 threads, with 512 and 1024: 4000 rows
+// 17.3 and (768) 18.2, 65104 171 and 157.
 int back_blocks(int64_t N, int d) {
   const Shape sh = back_shape(d);
   const int64_t b = (N + 2 * rows_side_by_side(sh) - 1) / (2 * rows_side_by_side(sh));
-  const int most = sh.threads == 192 ? 1024 : sh.vectors > 1 && sh.threads == 512 ? 256 : 512;
+  const bool is_long = N >= 16384;
+  const int most = sh.threads == 192 && is_long ? 1024 : sh.vectors > 1 && sh.threads == 512 ? 256 : sh.threads >= 384 && !is_long ? 256 : 512;
   return (int)(b < most ? b : most);
 }
 

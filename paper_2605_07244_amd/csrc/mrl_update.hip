@@ -349,14 +349,15 @@ template <int kMost, class F> void in_launches(const mrl_param_tensor* t, int32_
   if (held > 0) f(first, count);
 }
 
-int64_t norm_parts(const mrl_param_tensor* t, int32_t count) {
+// A partial sum for each workgroup of each launch.
+size_t norm_bytes(const mrl_param_tensor* t, int32_t count) {
   int64_t parts = 0;
   in_launches<kNormTensors>(t, count, [&](int32_t first, int32_t last) {
     int64_t chunks = 0;
     for (int32_t i = first; i < last; ++i) chunks += chunks_of(t[i].n, kNormChunk);
     parts += std::min<int64_t>(chunks, kNormBlocks);
   });
-  return parts;
+  return (size_t)round_up(parts * 8 + 8, 256);
 }
 
 template <bool kCodes>
@@ -400,7 +401,7 @@ using namespace mrl;
 
 extern "C" size_t mrl_grad_norm_workspace(const mrl_param_tensor* tensors, int32_t count) {
   if (check_tensors(tensors, count, false, false) != MRL_OK) return 0;
-  return (size_t)round_up(norm_parts(tensors, count) * 8 + 8, 256);
+  return norm_bytes(tensors, count);
 }
 
 extern "C" int mrl_grad_norm(const mrl_param_tensor* tensors, int32_t count, double max_norm, float* out_norm_coef, void* workspace,
@@ -409,7 +410,7 @@ extern "C" int mrl_grad_norm(const mrl_param_tensor* tensors, int32_t count, dou
   if (rc != MRL_OK) return rc;
   if (!out_norm_coef) return MRL_ERR_NULL;
   if (!(max_norm > 0.0)) return MRL_ERR_CONFIG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < mrl_grad_norm_workspace(tensors, count)) return MRL_ERR_WORKSPACE;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < norm_bytes(tensors, count)) return MRL_ERR_WORKSPACE;
   rc = require_gfx950();
   if (rc != MRL_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
