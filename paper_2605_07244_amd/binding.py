@@ -645,7 +645,7 @@ def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
             setattr(c, name + "_dev", _ptr(x, dtype, name))
             _here(x)
         else:
-            setattr(c, name, x)
+            setattr(c, name, float(x) if name == "lr" else int(x))
     if norm_coef is not None and norm_coef.numel() != 2:
         raise ValueError("norm_coef must have two entries")
     coef = None if norm_coef is None else _ptr(norm_coef, torch.float32, "norm_coef") + 4

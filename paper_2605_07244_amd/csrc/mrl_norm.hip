@@ -18,10 +18,10 @@ struct NormArgs {
   void* sum; void* y; float* scale;
 };
 
-// Sum (or maximum) over the kT threads that share a row; `sh`: a slot per wave, used by nothing else between two barriers.
+// Sum (or maximum) over the kT threads that share a row, a part of a wave or some waves; `sh`: a slot per wave, used by nothing else between two barriers.
 template <int kT> __device__ inline float group_sum(float x, float* sh) {
-  x = wave_sum_f32(x);
-  if (kT == 64) return x;
+  x = lanes_sum<(kT < 64 ? kT : 64)>(x);
+  if (kT <= 64) return x;
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
   __syncthreads();
   float s = 0.f;
@@ -30,8 +30,8 @@ template <int kT> __device__ inline float group_sum(float x, float* sh) {
   return s;
 }
 template <int kT> __device__ inline uint32_t group_max(uint32_t x, uint32_t* sh) {
-  x = wave_max(x);
-  if (kT == 64) return x;
+  x = lanes_max<(kT < 64 ? kT : 64)>(x);
+  if (kT <= 64) return x;
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
   __syncthreads();
   uint32_t m = 0;
@@ -40,27 +40,35 @@ template <int kT> __device__ inline uint32_t group_max(uint32_t x, uint32_t* sh)
   return m;
 }
 
-__device__ inline void load_weights(const void* w, bool bf16, int c, int d, float (&out)[8]) {
+// A thread's columns of one row: its i-th eight begin at column (i kT + t) 8.
+template <int kT, bool kBf16> __device__ inline void load_eight(Eight<kBf16>& v, const void* row, const Columns& c, int d) {
+  if (kT == 8 && d < 8) v.load_short(row, d); else v.load(row, c);       // (eight threads take rows of up to 64 columns)
+}
+template <int kT> __device__ inline void load_weights(const void* w, bool bf16, const Columns& c, int d, float (&out)[8]) {
   if (bf16) {
     Eight<true> v;
-    v.load(w, c, d);
+    load_eight<kT>(v, w, c, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = v[e];
   } else {
     Eight<false> v;
-    v.load(w, c, d);
+    load_eight<kT>(v, w, c, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) out[e] = v[e];
   }
 }
 
-// kT threads take a row, each kNV times eight elements, kT * 8 apart.  kRes: 0 no residual, 1 bf16, 2 float.
+// kT threads take a row, each kNV times eight elements; below 64 threads a workgroup of 256 takes several.  kRes: 0 no residual, 1 bf16, 2 float.
+// h is stored past the caches: the next layer reads y, and h is read in the backward pass (7812 rows of 4096 and a kernel that reads y: 71 us with
+// both kept, 66 with h streamed, 67 with both streamed; 15625 rows 137, 136 and 139).
 template <bool kXBf16, int kRes, int kT, int kNV>
-__global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
+__global__ __launch_bounds__(kT < 64 ? 256 : kT) void k_rms_norm(NormArgs a) {
   __shared__ float sh_sum[16];
   __shared__ uint32_t sh_max[16];
-  const int64_t row = blockIdx.x;
-  const int t = threadIdx.x, d = a.d;
+  constexpr int kRows = kT < 64 ? 256 / kT : 1;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + threadIdx.x / kT;
+  if (row >= a.N) return;                               // (all of a row's threads)
+  const int t = threadIdx.x % kT, d = a.d;
   const int scales = a.scale_block ? (d + 127) / 128 : 1;
   const char* x = static_cast<const char*>(a.x) + row * d * (kXBf16 ? 2 : 4);
   const char* res = static_cast<const char*>(a.residual) + row * d * (kRes == 1 ? 2 : 4);
@@ -73,14 +81,16 @@ __global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
     Eight<kRes == 1> rv[kNV];
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-      const int c = (i * kT + t) * 8;
-      xv[i].load(x, c, d);
-      if (kRes) rv[i].load(res, c, d);
+      const Columns c((i * kT + t) * 8, d);
+      load_eight<kT>(xv[i], x, c, d);
+      if (kRes) load_eight<kT>(rv[i], res, c, d);
     }
 #pragma unroll
-    for (int i = 0; i < kNV; ++i)
+    for (int i = 0; i < kNV; ++i) {
+      const Columns c((i * kT + t) * 8, d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[i][e] = kRes ? xv[i][e] + rv[i][e] : xv[i][e];
+      for (int e = 0; e < 8; ++e) h[i][e] = e < c.skip ? 0.f : kRes ? xv[i][e] + rv[i][e] : xv[i][e];
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kNV; ++i)
@@ -92,20 +102,21 @@ __global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
   for (int i = 0; i < kNV; ++i) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) s = fmaf(h[i][e], h[i][e], s);
-    if (kRes) store_eight<true>(sum, kRes == 1, (i * kT + t) * 8, d, h[i]);
+    if (kRes) store_eight<true>(sum, kRes == 1, Columns((i * kT + t) * 8, d), d, h[i]);
   }
   s = group_sum<kT>(s, sh_sum);
   const float r = __builtin_amdgcn_rsqf(fmaf(s, a.inv_d, a.eps));      // (the instruction is good to a step of fp32)
 #pragma unroll
   for (int i = 0; i < kNV; ++i) {
+    const Columns c((i * kT + t) * 8, d);
     float w[8];
-    load_weights(a.w, a.w_bf16, (i * kT + t) * 8, d, w);
+    load_weights<kT>(a.w, a.w_bf16, c, d, w);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[i][e] = scored ? h[i][e] * r * w[e] : 0.f;
+    for (int e = 0; e < 8; ++e) h[i][e] = scored && e >= c.skip ? h[i][e] * r * w[e] : 0.f;
   }
   if (a.y_type != MRL_E4M3) {
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) store_eight(y, a.y_type == MRL_BF16, (i * kT + t) * 8, d, h[i]);
+    for (int i = 0; i < kNV; ++i) store_eight(y, a.y_type == MRL_BF16, Columns((i * kT + t) * 8, d), d, h[i]);
     return;
   }
   uint32_t most[kNV];
@@ -115,10 +126,10 @@ __global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) most[i] = larger(most[i], magnitude(h[i][e]));
   }
-  if (a.scale_block) {                                  // 128 columns are 16 lanes
+  if (kT > 8 && a.scale_block) {                        // 128 columns are 16 lanes (and a row of up to 64 is one block)
 #pragma unroll
     for (int i = 0; i < kNV; ++i) {
-      most[i] = row16_max(most[i]);
+      most[i] = lanes_max<16>(most[i]);
       const int block = (i * kT + t) / 16;
       if ((t & 15) == 0 && block < scales) a.scale[row * scales + block] = __uint_as_float(most[i]) / kE4m3Max;
     }
@@ -135,7 +146,7 @@ __global__ __launch_bounds__(kT) void k_rms_norm(NormArgs a) {
     const float inverse = kE4m3Max / __uint_as_float(most[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) h[i][e] *= inverse;
-    store_eight_e4m3(y, (i * kT + t) * 8, d, h[i]);
+    store_eight_e4m3(y, Columns((i * kT + t) * 8, d), d, h[i]);
   }
 }
 
@@ -160,33 +171,34 @@ template <bool kHBf16, bool kDyBf16, int kT, int kNV> struct BackRow {
     if (is_scored) {
 #pragma unroll
       for (int i = 0; i < kNV; ++i) {
-        h[i].load(h_row, (i * kT + t) * 8, a.d);
-        dy[i].load(dy_row, (i * kT + t) * 8, a.d);
+        const Columns c((i * kT + t) * 8, a.d);
+        load_eight<kT>(h[i], h_row, c, a.d);
+        load_eight<kT>(dy[i], dy_row, c, a.d);
       }
     }
     if (a.d_residual != nullptr) {
 #pragma unroll
-      for (int i = 0; i < kNV; ++i) res[i].load(res_row, (i * kT + t) * 8, a.d);
+      for (int i = 0; i < kNV; ++i) load_eight<kT>(res[i], res_row, Columns((i * kT + t) * 8, a.d), a.d);
     }
   }
 };
 
-// The rows of a workgroup one after the other (kT = 64: four waves side by side), the next one's elements on their way while one is
+// The rows of a workgroup one after the other (up to 64 threads a row: several side by side), the next one's elements on their way while one is
 // worked on, and the mask of the one behind it; the columns' sums of dy u stay in registers until the last row.  Then the rows that were
 // side by side are added in LDS, in their order, and the workgroup writes one row of partial sums.
 // In round k the workgroups take consecutive rows, turned by k times a golden section of their number: sequences of as many slots as there are
 // workgroups, whose heads are scored and whose tails are not, would else give some of them scored rows only.
 template <bool kHBf16, bool kDyBf16, int kT, int kNV>
-__global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackArgs a) {
-  extern __shared__ float lds[];                        // kT = 64: [d] sums; else two sets of two sums a wave
-  constexpr int kRows = kT == 64 ? 4 : 1;
+__global__ __launch_bounds__(kT <= 64 ? 256 : kT) void k_rms_norm_back(NormBackArgs a) {
+  extern __shared__ float lds[];                        // kT <= 64: [d] sums; else two sets of two sums a wave
+  constexpr int kRows = kT <= 64 ? 256 / kT : 1;
   const int t = threadIdx.x % kT, side = threadIdx.x / kT, d = a.d;
   const int slots = (int)gridDim.x * kRows, slot = (int)blockIdx.x * kRows + side;
   const int turn_by = (int)(slots * 0.618f), rounds = (int)((a.N + slots - 1) / slots);
   float acc[kNV][8], w[kNV][8];                         // (weights stay in registers, too: every row needs them twice)
 #pragma unroll
   for (int i = 0; i < kNV; ++i) {
-    load_weights(a.w, a.w_bf16, (i * kT + t) * 8, d, w[i]);
+    load_weights<kT>(a.w, a.w_bf16, Columns((i * kT + t) * 8, d), d, w[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
   }
@@ -204,12 +216,13 @@ __global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackA
   BackRow<kHBf16, kDyBf16, kT, kNV> now, next;
   int64_t row = next_row(), row1 = next_row();
   int mask0 = mask_of(row), mask1 = mask_of(row1), turn = 0;
-  if (kAhead && row >= 0) now.load(a, row, __builtin_amdgcn_readfirstlane(mask0) != 0, t);
+  auto is_scored = [](int m) { return (kT < 64 ? m : __builtin_amdgcn_readfirstlane(m)) != 0; };     // (one row a wave: a scalar condition)
+  if (kAhead && row >= 0) now.load(a, row, is_scored(mask0), t);
   for (int k = 0; k < rounds; ++k) {
     const int64_t row2 = next_row();
     const int mask2 = mask_of(row2);
-    if (kAhead && row1 >= 0) next.load(a, row1, __builtin_amdgcn_readfirstlane(mask1) != 0, t);
-    if (!kAhead && row >= 0) now.load(a, row, __builtin_amdgcn_readfirstlane(mask0) != 0, t);
+    if (kAhead && row1 >= 0) next.load(a, row1, is_scored(mask1), t);
+    if (!kAhead && row >= 0) now.load(a, row, is_scored(mask0), t);
     if (row >= 0) {                                     // (with more waves than one a row, the workgroup is of one mind)
       char* dx = static_cast<char*>(a.dx) + row * d * (a.dx_bf16 ? 2 : 4);
       float r = 0.f, along = 0.f;
@@ -217,14 +230,16 @@ __global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackA
         float hh = 0.f, gh = 0.f;
 #pragma unroll
         for (int i = 0; i < kNV; ++i) {
+          const Columns c((i * kT + t) * 8, d);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
+            if (e < c.skip) continue;                   // (a column of another thread)
             hh = fmaf(now.h[i][e], now.h[i][e], hh);
             gh = fmaf(now.dy[i][e] * w[i][e], now.h[i][e], gh);
           }
         }
-        hh = wave_sum_f32(hh);
-        gh = wave_sum_f32(gh);
+        hh = lanes_sum<(kT < 64 ? kT : 64)>(hh);
+        gh = lanes_sum<(kT < 64 ? kT : 64)>(gh);
         if (kT > 64) {                                  // (two sets of slots in turn from one scored row to the next: one barrier each)
           float* sh = lds + turn * 32;
           turn ^= 1;
@@ -250,7 +265,7 @@ __global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackA
           }
           if (a.d_residual != nullptr) out[e] += now.res[i][e];
         }
-        store_eight(dx, a.dx_bf16, (i * kT + t) * 8, d, out);
+        store_eight(dx, a.dx_bf16, Columns((i * kT + t) * 8, d), d, out);
       }
     }
     if (kAhead) now = next;
@@ -258,24 +273,33 @@ __global__ __launch_bounds__(kT == 64 ? 256 : kT) void k_rms_norm_back(NormBackA
   }
   if (a.parts == nullptr) return;
   float* part = a.parts + (int64_t)blockIdx.x * a.ld;
-  if (kRows > 1) {
-    for (int s = 0; s < kRows; ++s) {
-      if (side == s) {
+  if (kT > 64) {
 #pragma unroll
-        for (int i = 0; i < kNV; ++i)
+    for (int i = 0; i < kNV; ++i) store_eight(part, false, Columns((i * kT + t) * 8, d), d, acc[i]);
+    return;
+  }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int c = (i * kT + t) * 8 + e;
-            if (c >= d) continue;
-            const float sum = s > 0 ? lds[c] + acc[i][e] : acc[i][e];
-            if (s < kRows - 1) lds[c] = sum; else part[c] = sum;
-          }
-      }
-      __syncthreads();
+  for (int i = 0; i < kNV; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int off = kT; off < 64; off <<= 1) acc[i][e] += __shfl_xor(acc[i][e], off);
     }
-  } else {
+  const int wave = threadIdx.x >> 6;
+  for (int v = 0; v < 4; ++v) {
+    if (wave == v && (threadIdx.x & 63) < kT) {
 #pragma unroll
-    for (int i = 0; i < kNV; ++i) store_eight(part, false, (i * kT + t) * 8, d, acc[i]);
+      for (int i = 0; i < kNV; ++i) {
+        const Columns c((i * kT + t) * 8, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (!c.own(e, d)) continue;
+          const float sum = v > 0 ? lds[c.at + e] + acc[i][e] : acc[i][e];
+          if (v < 3) lds[c.at + e] = sum; else part[c.at + e] = sum;
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -316,25 +340,25 @@ constexpr int kMaxWidth = 16384;                         // 1024 threads, 16 ele
 
 // Threads that share a row, and how many times eight elements each takes.
 struct Shape { int threads, vectors; };
-Shape norm_shape(int64_t N, int d) {
+Shape norm_shape(int d) {
   const int v = (d + 7) / 8;
-  if (v <= 64) return {64, 1};
+  if (v <= 64) return {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, 1};
   if (v <= 128) return {64, 2};
   if (v <= 256) return {256, 1};
   if (v <= 512) return {256, 2};
   if (v <= 1024) return {512, 2};
   return {1024, 2};
 }
-// Up to 128 vectors of eight a wave takes a row, four of them side by side; above, as many waves as the row has vectors for, with one each: idle
+// Up to 128 vectors of eight a wave or a part of one takes a row, several of them side by side; above, as many waves as the row has vectors for, with one each: idle
 // lanes cost more than barriers (65104 rows of 1536 in 256 and in 192 threads 182 and 153 us, 27901 of 3584 in 256 threads with two vectors and in 448
 // with one 173 and 150).
 Shape back_shape(int d) {
   const int v = (d + 7) / 8;
-  if (v <= 128) return {64, v <= 64 ? 1 : 2};
+  if (v <= 128) return {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, v <= 64 ? 1 : 2};
   if (v <= 512) return {v <= 192 ? 192 : (v + 63) / 64 * 64, 1};
   return {512, v <= 1024 ? 2 : 4};
 }
-int rows_side_by_side(const Shape& s) { return s.threads == 64 ? 4 : 1; }
+int rows_side_by_side(const Shape& s) { return s.threads <= 64 ? 256 / s.threads : 1; }
 // Workgroups: two or more rows each, and as many as cover the latencies of a row without more rows under way than the memory takes well: 80000 rows of 2048,
 // us, with 256, 512, 768, 1024 and 1280 workgroups: 351, 229, 238, 259, 282.  The partial sums of many are worth it to long calls only: rows of 4096 in
 // 512 threads, with 256 and 512 workgroups: 1000 rows 13.8 and 16.2, 4000 28.8 and 31.6, 24414 156 and 154; of 1536 in 192 threads, with 512 and 1024: 4000 rows
@@ -347,27 +371,37 @@ int back_blocks(int64_t N, int d) {
   return (int)(b < most ? b : most);
 }
 
-template <bool kXBf16, int kRes, int kT> void go_norm_threads(const NormArgs& a, int vectors, hipStream_t s) {
-  const dim3 grid((unsigned)a.N), block(kT);
-  if (vectors == 1) hipLaunchKernelGGL((k_rms_norm<kXBf16, kRes, kT, 1>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_rms_norm<kXBf16, kRes, kT, 2>), grid, block, 0, s, a);
+constexpr int64_t kMostWide = 1 << 21;                   // workgroups along x: a launch has fewer than 2^32 threads there
+
+template <bool kXBf16, int kRes, int kT, int kNV> void go_norm_shape(const NormArgs& a, hipStream_t s) {
+  constexpr int kRows = kT < 64 ? 256 / kT : 1;
+  const int64_t groups = (a.N + kRows - 1) / kRows, wide = groups < kMostWide ? groups : kMostWide;
+  hipLaunchKernelGGL((k_rms_norm<kXBf16, kRes, kT, kNV>), dim3((unsigned)wide, (unsigned)((groups + wide - 1) / wide)), dim3(kT < 64 ? 256 : kT), 0, s, a);
 }
 template <bool kXBf16, int kRes> void go_norm(const NormArgs& a, hipStream_t s) {
-  const Shape sh = norm_shape(a.N, a.d);
-  switch (sh.threads) {
-    case 64: go_norm_threads<kXBf16, kRes, 64>(a, sh.vectors, s); break;
-    case 256: go_norm_threads<kXBf16, kRes, 256>(a, sh.vectors, s); break;
-    case 512: go_norm_threads<kXBf16, kRes, 512>(a, sh.vectors, s); break;
-    default: go_norm_threads<kXBf16, kRes, 1024>(a, sh.vectors, s); break;
+  const Shape sh = norm_shape(a.d);
+  switch (sh.threads * 8 + sh.vectors) {
+    case 8 * 8 + 1: go_norm_shape<kXBf16, kRes, 8, 1>(a, s); break;
+    case 16 * 8 + 1: go_norm_shape<kXBf16, kRes, 16, 1>(a, s); break;
+    case 32 * 8 + 1: go_norm_shape<kXBf16, kRes, 32, 1>(a, s); break;
+    case 64 * 8 + 1: go_norm_shape<kXBf16, kRes, 64, 1>(a, s); break;
+    case 64 * 8 + 2: go_norm_shape<kXBf16, kRes, 64, 2>(a, s); break;
+    case 256 * 8 + 1: go_norm_shape<kXBf16, kRes, 256, 1>(a, s); break;
+    case 256 * 8 + 2: go_norm_shape<kXBf16, kRes, 256, 2>(a, s); break;
+    case 512 * 8 + 2: go_norm_shape<kXBf16, kRes, 512, 2>(a, s); break;
+    default: go_norm_shape<kXBf16, kRes, 1024, 2>(a, s); break;
   }
 }
 
 template <bool kHBf16, bool kDyBf16> void go_back(const NormBackArgs& a, hipStream_t s) {
   const Shape sh = back_shape(a.d);
-  const bool waves = sh.threads == 64;
+  const bool waves = sh.threads <= 64;
   const dim3 grid((unsigned)back_blocks(a.N, a.d)), block(waves ? 256 : sh.threads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, waves ? (size_t)a.d * 4 : 64 * 4, s, a); };
   switch (sh.threads * 8 + sh.vectors) {
+    case 8 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 8, 1>); break;
+    case 16 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 16, 1>); break;
+    case 32 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 32, 1>); break;
     case 64 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 64, 1>); break;
     case 64 * 8 + 2: go(k_rms_norm_back<kHBf16, kDyBf16, 64, 2>); break;
     case 192 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 192, 1>); break;

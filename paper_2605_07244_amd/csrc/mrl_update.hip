@@ -66,17 +66,26 @@ __global__ __launch_bounds__(256) void k_square_sums(NormTable a) {
     const int i = tensor_of<kNormTensors>(a.chunk0, chunk);
     const int64_t at = (int64_t)(chunk - a.chunk0[i]) * kNormChunk;
     const int left = (int)min((int64_t)kNormChunk, a.n[i] - at), c = threadIdx.x * 8;
-    if (a.bf16[i >> 5] >> (i & 31) & 1) {
-      Eight<true> g;
-      g.load(static_cast<const uint16_t*>(a.grad[i]) + at, c, left);
+    float g[8];
+    const bool bf16 = a.bf16[i >> 5] >> (i & 31) & 1;
+    const uint16_t* g16 = static_cast<const uint16_t*>(a.grad[i]) + at + c;
+    const float* g32 = static_cast<const float*>(a.grad[i]) + at + c;
+    if (left == kNormChunk) {
+      if (bf16) {
+        const u32x4 w = load_any<2, u32x4>(g16);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+        for (int e = 0; e < 8; ++e) g[e] = e & 1 ? bf16_high(w[e >> 1]) : bf16_low(w[e >> 1]);
+      } else {
+        const u32x4 w0 = load_any<4, u32x4>(g32), w1 = load_any<4, u32x4>(g32 + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = __uint_as_float(e < 4 ? w0[e & 3] : w1[e & 3]);
+      }
     } else {
-      Eight<false> g;
-      g.load(static_cast<const float*>(a.grad[i]) + at, c, left);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
+      for (int e = 0; e < 8; ++e) g[e] = c + e >= left ? 0.f : bf16 ? bf16_low(g16[e]) : g32[e];
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fma((double)g[e], (double)g[e], s);
   }
   s = block_sum_f64<4>(s, sh);
   if (threadIdx.x == 0) a.parts[blockIdx.x] = s;
@@ -108,7 +117,7 @@ template <bool kCodes> struct AdamTable {
   static constexpr int kTensors = kCodes ? 48 : 64;     // a launch: 3.8 and 3.9 KB of arguments
   AdamTensor<kCodes> t[kTensors];
   int32_t chunk0[kTensors];                             // as above
-  int32_t skip_nonfinite;
+  int32_t chunks, skip_nonfinite;
   float lr, inv_fix1, inv_root_fix2;                    // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
   float b1, one_b1, b2, one_b2, eps;
   double beta1, beta2;
@@ -182,7 +191,7 @@ struct Four {
       m_most = larger(m_most, magnitude(m[e]));
       v_most = larger(v_most, magnitude(root[e]));
     }
-    const float m_max = __uint_as_float(wave_max(m_most)), v_max = __uint_as_float(wave_max(v_most));
+    const float m_max = __uint_as_float(lanes_max<64>(m_most)), v_max = __uint_as_float(lanes_max<64>(v_most));
     const float m_inv = times(1.f / m_max, kE4m3Max), v_inv = times(1.f / v_max, kE4m3Max);
     float mq[4], vq[4];
 #pragma unroll
@@ -217,10 +226,12 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
 // A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.
 template <bool kCodes>
 __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
-  const int i = tensor_of<AdamTable<kCodes>::kTensors>(a.chunk0, blockIdx.x);
+  const int chunk = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  if (chunk >= a.chunks) return;
+  const int i = tensor_of<AdamTable<kCodes>::kTensors>(a.chunk0, chunk);
   const AdamTensor<kCodes>& t = a.t[i];
   const bool grad_bf16 = t.place_bf16 & 1;
-  const int64_t at = (int64_t)((int)blockIdx.x - a.chunk0[i]) * kAdamChunk;
+  const int64_t at = (int64_t)(chunk - a.chunk0[i]) * kAdamChunk;
   Rates r = {a.lr, a.inv_fix1, a.inv_root_fix2, a.coef != nullptr ? *a.coef : 1.f, a.b1, a.one_b1, a.b2, a.one_b2, a.eps, t.weight_decay};
   if (a.skip_nonfinite && !(fabsf(r.coef) < INFINITY)) return;
   int64_t step = a.step;
@@ -318,6 +329,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
 }
 
 // ------------------------------------------------------------------ host
+constexpr int64_t kMostWide = 1 << 25;
 constexpr int64_t kMaxElements = (int64_t)1 << 40;
 int64_t chunks_of(int64_t n, int chunk) { return (n + chunk - 1) / chunk; }
 
@@ -390,7 +402,10 @@ void go_adamw(const mrl_param_tensor* tensors, int32_t count, const mrl_adamw_co
     a.inv_fix1 = (float)(1.0 / (1.0 - power(cfg.beta1, cfg.step)));
     a.inv_root_fix2 = (float)(1.0 / std::sqrt(1.0 - power(cfg.beta2, cfg.step)));
     a.lr_dev = cfg.lr_dev; a.step_dev = cfg.step_dev; a.coef = grad_coef;
-    hipLaunchKernelGGL(k_adamw<kCodes>, dim3((unsigned)chunks), dim3(kAdamThreads), 0, s, a);
+    a.chunks = (int32_t)chunks;
+    // (a launch has fewer than 2^32 threads along x)
+    const int64_t wide = std::min<int64_t>(chunks, kMostWide);
+    hipLaunchKernelGGL(k_adamw<kCodes>, dim3((unsigned)wide, (unsigned)((chunks + wide - 1) / wide)), dim3(kAdamThreads), 0, s, a);
   });
 }
 

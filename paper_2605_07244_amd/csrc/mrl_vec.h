@@ -36,36 +36,43 @@ __device__ inline uint32_t pack_e4m3(float a, float b, float c, float d) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
-// Elements c .. c + 7 of a row of d as they lie in memory, zeros from d on.  Nothing behind the row is read.
+// The eight columns of a row of d that a thread looks at.  Its own are c .. c + 7 as far as the row reaches; at the row's end it looks at the last
+// eight of it, of which the first `skip` are other threads' (all eight where c is behind the row).  So every load is whole, inside the row and behind
+// no branch: a branch that some lanes take waits for the loads in flight (166666 rows of 384 by 64 lanes, a quarter of them idle: a backward
+// pass of 215 us with such branches, 107 without).  Rows of fewer than eight columns are loaded one by one.
+struct Columns {
+  int at, skip;
+  __device__ Columns(int c, int d) : at(max(min(c, d - 8), 0)), skip(c - at) {}
+  __device__ bool own(int e, int d) const { return e >= skip && at + e < d; }
+};
+
+// Those columns as they lie in memory.
 template <bool kBf16> struct Eight;
 template <> struct Eight<true> {
   u32x4 w;
-  __device__ void load(const void* row, int c, int d) {
-    const uint16_t* p = static_cast<const uint16_t*>(row) + c;
+  __device__ void load(const void* row, const Columns& c) { w = load_any<2, u32x4>(static_cast<const uint16_t*>(row) + c.at); }
+  __device__ void load_short(const void* row, int d) {
+    const uint16_t* p = static_cast<const uint16_t*>(row);
     w = u32x4{0, 0, 0, 0};
-    if (c + 8 <= d) {
-      w = load_any<2, u32x4>(p);
-    } else if (c < d) {
 #pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (c + e < d) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-    }
+    for (int e = 0; e < 7; ++e)
+      if (e < d) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
   }
   __device__ float operator[](int e) const { return e & 1 ? bf16_high(w[e >> 1]) : bf16_low(w[e >> 1]); }
 };
 template <> struct Eight<false> {
   u32x4 w[2];
-  __device__ void load(const void* row, int c, int d) {
-    const uint32_t* p = static_cast<const uint32_t*>(row) + c;
+  __device__ void load(const void* row, const Columns& c) {
+    const float* p = static_cast<const float*>(row) + c.at;
+    w[0] = load_any<4, u32x4>(p);
+    w[1] = load_any<4, u32x4>(p + 4);
+  }
+  __device__ void load_short(const void* row, int d) {
+    const uint32_t* p = static_cast<const uint32_t*>(row);
     w[0] = w[1] = u32x4{0, 0, 0, 0};
-    if (c + 8 <= d) {
-      w[0] = load_any<4, u32x4>(p);
-      w[1] = load_any<4, u32x4>(p + 4);
-    } else if (c < d) {
 #pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (c + e < d) w[e >> 2][e & 3] = p[e];
-    }
+    for (int e = 0; e < 7; ++e)
+      if (e < d) w[e >> 2][e & 3] = p[e];
   }
   __device__ float operator[](int e) const { return __uint_as_float(w[e >> 2][e & 3]); }
 };
@@ -73,76 +80,70 @@ template <> struct Eight<false> {
 template <bool kStream, int kAlign, class V> __device__ inline void store_as(void* p, V v) {
   if (kStream) store_stream<kAlign>(p, v); else store_any<kAlign>(p, v);
 }
-// Elements c .. c + 7 of a row of d, those below d.
-template <bool kStream = false> __device__ inline void store_eight(void* row, bool bf16, int c, int d, const float (&v)[8]) {
-  if (c >= d) return;
+// The thread's own ones of those columns, of a row of d.
+template <bool kStream = false> __device__ inline void store_eight(void* row, bool bf16, const Columns& c, int d, const float (&v)[8]) {
   if (bf16) {
-    uint16_t* p = static_cast<uint16_t*>(row) + c;
+    uint16_t* p = static_cast<uint16_t*>(row) + c.at;
     const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    if (c + 8 <= d) {
+    if (c.skip == 0 && d >= 8) {
       store_as<kStream, 2>(p, w);
-    } else {
+    } else if (c.skip < 8) {
 #pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (c + e < d) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+      for (int e = 0; e < 8; ++e)
+        if (c.own(e, d)) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
     }
   } else {
-    float* p = static_cast<float*>(row) + c;
-    if (c + 8 <= d) {
+    float* p = static_cast<float*>(row) + c.at;
+    if (c.skip == 0 && d >= 8) {
       store_as<kStream, 4>(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
       store_as<kStream, 4>(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
-    } else {
+    } else if (c.skip < 8) {
 #pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (c + e < d) p[e] = v[e];
+      for (int e = 0; e < 8; ++e)
+        if (c.own(e, d)) p[e] = v[e];
     }
   }
 }
-__device__ inline void store_eight_e4m3(void* row, int c, int d, const float (&v)[8]) {
-  if (c >= d) return;
-  uint8_t* p = static_cast<uint8_t*>(row) + c;
+__device__ inline void store_eight_e4m3(void* row, const Columns& c, int d, const float (&v)[8]) {
+  uint8_t* p = static_cast<uint8_t*>(row) + c.at;
   const u32x2 w = {pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
-  if (c + 8 <= d) {
+  if (c.skip == 0 && d >= 8) {
     store_any<1>(p, w);
-  } else {
+  } else if (c.skip < 8) {
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (c + e < d) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+    for (int e = 0; e < 8; ++e)
+      if (c.own(e, d)) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
   }
 }
 
-// Over the 16 lanes of a row by rotation, then over the wave's four rows through scalar registers.  Lanes that a step pairs
-// add the same two numbers, so all lanes end with the same bits.
-template <int kRotate> __device__ inline uint32_t rotated(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + kRotate, 0xf, 0xf, true);
+// Over neighbouring lanes, 8, 16, 32 or all 64 of a wave.  Lanes that a step pairs add the same two numbers, so all lanes end with the same bits.
+template <int kControl> __device__ inline uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kControl, 0xf, 0xf, true);
 }
-__device__ inline float row16_sum(float x) {
-  x += __uint_as_float(rotated<8>(__float_as_uint(x)));
-  x += __uint_as_float(rotated<4>(__float_as_uint(x)));
-  x += __uint_as_float(rotated<2>(__float_as_uint(x)));
-  return x + __uint_as_float(rotated<1>(__float_as_uint(x)));
+constexpr int kSwapOne = 0xB1, kSwapTwo = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;      // quads permuted; 8 and 16 lanes reversed
+template <int kLanes, class T, class F> __device__ inline T over_lanes(T x, F join) {
+  auto with = [&](uint32_t other) { x = join(x, __builtin_bit_cast(T, other)); };
+  with(moved<kSwapOne>(__builtin_bit_cast(uint32_t, x)));
+  with(moved<kSwapTwo>(__builtin_bit_cast(uint32_t, x)));
+  with(moved<kHalfMirror>(__builtin_bit_cast(uint32_t, x)));
+  if (kLanes >= 16) with(moved<kMirror>(__builtin_bit_cast(uint32_t, x)));
+  if (kLanes == 32) with(__shfl_xor(__builtin_bit_cast(uint32_t, x), 16));
+  if (kLanes == 64) {
+    T part[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[k] = __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 16 * k));
+    x = join(join(part[0], part[1]), join(part[2], part[3]));
+  }
+  return x;
 }
-__device__ inline float wave_sum_f32(float x) {
-  const int s = __float_as_int(row16_sum(x));
-  const float a = __int_as_float(__builtin_amdgcn_readlane(s, 0)), b = __int_as_float(__builtin_amdgcn_readlane(s, 16));
-  const float c = __int_as_float(__builtin_amdgcn_readlane(s, 32)), d = __int_as_float(__builtin_amdgcn_readlane(s, 48));
-  return (a + b) + (c + d);
+template <int kLanes> __device__ inline float lanes_sum(float x) {
+  return over_lanes<kLanes>(x, [](float a, float b) { return a + b; });
 }
 // Maxima of absolute values as their bits, whose order is that of the values, with infinity above all numbers and NaN above
 // infinity: a NaN is kept, where a maximum of floats would drop it.
 __device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 __device__ inline uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
-__device__ inline uint32_t row16_max(uint32_t x) {
-  x = larger(x, rotated<8>(x));
-  x = larger(x, rotated<4>(x));
-  x = larger(x, rotated<2>(x));
-  return larger(x, rotated<1>(x));
-}
-__device__ inline uint32_t wave_max(uint32_t x) {
-  const int m = (int)row16_max(x);
-  return larger(larger((uint32_t)__builtin_amdgcn_readlane(m, 0), (uint32_t)__builtin_amdgcn_readlane(m, 16)),
-                larger((uint32_t)__builtin_amdgcn_readlane(m, 32), (uint32_t)__builtin_amdgcn_readlane(m, 48)));
-}
+template <int kLanes> __device__ inline uint32_t lanes_max(uint32_t x) { return over_lanes<kLanes>(x, larger); }
 
 // Scales of e4m3 values: the largest magnitude, at least 2^-100 (whose inverse times 448 still is a number), maps to 448.
 constexpr float kE4m3Max = 448.f;

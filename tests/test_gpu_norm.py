@@ -17,7 +17,7 @@ U = 2.0 ** -24
 F32, BF16, E4M3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
 HALF = {F32: U, BF16: 2.0 ** -8}
 EPS = 1e-5
-WIDTHS = [1, 2, 7, 8, 63, 100, 128, 129, 512, 513, 712, 1024, 1025, 1536, 2048, 2049, 3584, 4096, 4100, 8191, 8192, 8200, 16384]
+WIDTHS = [1, 2, 7, 8, 9, 15, 16, 63, 64, 65, 71, 100, 128, 129, 136, 255, 256, 257, 512, 513, 712, 1024, 1025, 1536, 2048, 2049, 3584, 4096, 4100, 8191, 8192, 8200, 16384]
 
 
 @pytest.fixture(scope="module")
@@ -310,12 +310,29 @@ def test_more_than_2_31_elements(mrl):
     y, h, s = mrl.rms_norm(x, w, EPS, residual=x, token_mask=mask, out_dtype=E4M3)
     y0, h0, s0 = mrl.rms_norm(tail, w, EPS, residual=tail, out_dtype=E4M3)
     assert torch.equal(h[-300:], h0) and bool((h[:1000] == 0).all())
-    # (few rows and many are taken by different kernels: a code may round the other way)
-    assert float((y[-300:].float() * s[-300:, None] - y0.float() * s0[:, None]).norm() / (y0.float() * s0[:, None]).norm()) < 1e-3
+    assert torch.equal(y[-300:].float(), y0.float()) and torch.equal(s[-300:], s0)
     del y, h
     dx, dw = mrl.rms_norm_backward(x, x, w, EPS, token_mask=mask)
     dx0, dw0 = mrl.rms_norm_backward(tail, tail, w, EPS)
     assert torch.equal(dx[-300:], dx0) and torch.allclose(dw, dw0, rtol=1e-5, atol=1e-4)
+
+
+@pytest.mark.parametrize("N,d", [(2 ** 21 + 77, 264), (2 ** 25 + 4097, 9)])
+def test_more_rows_than_a_launch_is_wide(mrl, N, d):
+    """More workgroups than go along x; rows of few columns, several to a wave, among them."""
+    x = torch.zeros((N, d), device="cuda", dtype=BF16)
+    head, tail = _rand((100, d), BF16, 1), _rand((300, d), BF16, 2)
+    x[:100], x[-300:] = head, tail
+    w = 1 + _rand((d,), F32, 3, 0.2)
+    y, _, _ = mrl.rms_norm(x, w, EPS)
+    assert torch.equal(y[:100], mrl.rms_norm(head, w, EPS)[0]) and torch.equal(y[-300:], mrl.rms_norm(tail, w, EPS)[0])
+    assert not bool(y[100:-300].any())
+    dx, dw = mrl.rms_norm_backward(x, x, w, EPS)
+    ends = torch.cat([head, tail])
+    dx0, dw0 = mrl.rms_norm_backward(ends, ends, w, EPS)
+    assert torch.equal(dx[:100], dx0[:100]) and torch.equal(dx[-300:], dx0[100:])
+    # zeros beside them change no sum, only its order: 4 + 400 additions
+    assert torch.all((dw - dw0).abs() <= 404 * U * (ends.double().square() / (ends.double().square().mean(1, keepdim=True) + EPS).sqrt()).sum(0))
 
 
 def test_no_rows(mrl):
@@ -328,6 +345,20 @@ def test_no_rows(mrl):
     kept = torch.full((16,), 3.0, device="cuda")
     _, dw = mrl.rms_norm_backward(x, x, w, EPS, out_dweight=kept, accumulate=True)
     assert bool((dw == 3).all())
+
+
+def test_another_device_is_refused(mrl, monkeypatch):
+    """Tensors that are not on the current device, whose stream the call would use."""
+    from paper_2605_07244_amd import binding
+    x, w = _rand((4, 16), BF16, 1), torch.ones(16, device="cuda")
+    p, g = torch.zeros(10, device="cuda"), torch.zeros(10, device="cuda")
+    plan = mrl.adamw_plan([p], [g])
+    monkeypatch.setattr(binding, "_native", False)
+    monkeypatch.setattr(binding.torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: mrl.rms_norm(x, w), lambda: mrl.rms_norm_backward(x, x, w), lambda: mrl.grad_norm(plan, 1.0), lambda: mrl.adamw_step(plan, 1e-3, 1),
+                 lambda: mrl.grad_plan([g])):
+        with pytest.raises(ValueError, match="current device"):
+            call()
 
 
 def test_refusals(mrl):

@@ -287,9 +287,10 @@ def test_numbers_from_the_device_and_replays(mrl):
             assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.all(), b.all())), t
 
 
-def test_more_than_2_32_elements(mrl):
-    """One tensor whose offsets pass 32 bits: its end is updated as a tensor of its own would be, with the random bits of its places."""
-    n, k = 2 ** 32 + 3 * 2048 + 301, 5000
+def test_more_than_2_33_elements(mrl):
+    """One tensor whose offsets pass 32 bits, and whose workgroups pass what a launch takes along x: its end is updated as a tensor of its own would be, with
+    the random bits of its places."""
+    n, k = 2 ** 33 + 3 * 2048 + 301, 5000
     p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
     m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2))
     ms, vs = (torch.zeros(-(-n // 256), device="cuda") for _ in range(2))
