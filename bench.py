@@ -5,7 +5,7 @@ One step = one pass of the whole hot path over one synthetic batch already
 resident in HBM: group advantages, then the fused LM-head + log-softmax + GRPO
 loss forward and backward (dH, dW).  Prints ONE JSON line.
 
-    python bench.py [--gpus 1] [--steps K] [--warmup W] [--config 5] [--full-length]
+    python bench.py [--gpus 1] [--steps K] [--warmup W] [--config 5] [--full-length] [--update f32|e4m3]
 """
 from __future__ import annotations
 
@@ -110,6 +110,43 @@ def thl_alignment_leg(mrl, synth, torch, with_cpu, B=2048, S_src=1180, S_tgt=153
     return leg
 
 
+def training_leg(mrl, torch, batch, mask, loss, out_dH, out_dW, states, reps=2):
+    """A whole training step of head and final norm around the scoring step: norm with the residual's addition, loss forward and backward on its
+    output, the norm's backward pass, clipping and the AdamW update.  `loss(hidden)` is the scoring step; times are medians of HIP events."""
+    N, d, V = batch["N"], batch["d"], batch["V"]
+    kind = {"f32": torch.float32, "e4m3": torch.float8_e4m3fn}[states]
+    residual = torch.randn((N, d), device="cuda", dtype=torch.bfloat16)
+    gain = torch.ones(d, device="cuda")
+    params, copies = [batch["W"].float(), gain], [batch["W"].clone(), gain.bfloat16()]
+    dgain = torch.empty(d, device="cuda")
+    plan = mrl.adamw_plan(params, [out_dW, dgain], copies, state_dtype=kind, weight_decay=[0.01, 0.0])
+    names = ("norm", "loss", "norm_backward", "grad_norm", "adamw")
+    times = {k: [] for k in names}
+    for rep in range(reps + 1):
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(len(names) + 1)]
+        ev[0].record()
+        hidden, total, _ = mrl.rms_norm(batch["H"], copies[1], residual=residual, token_mask=mask)
+        ev[1].record()
+        loss(hidden, copies[0])
+        ev[2].record()
+        mrl.rms_norm_backward(out_dH, total, copies[1], d_residual=None, token_mask=mask, out_dweight=dgain)
+        ev[3].record()
+        coef = mrl.grad_norm(plan, 1.0)
+        ev[4].record()
+        mrl.adamw_step(plan, 1e-6, rep + 1, norm_coef=coef, seed=1, skip_nonfinite=True)
+        ev[5].record()
+        torch.cuda.synchronize()
+        if rep > 0:
+            for k, name in enumerate(names):
+                times[name].append(ev[k].elapsed_time(ev[k + 1]))
+    med = {k: sorted(v)[len(v) // 2] for k, v in times.items()}
+    scored, state = int(mask.sum().item()), 1 + 4 / 256 if states == "e4m3" else 4
+    gb = dict(norm=d * (4 * scored + 4 * N), norm_backward=d * (4 * scored + 2 * N), grad_norm=4 * (V + 1) * d,
+              adamw=(V + 1) * d * (4 + 8 + 4 * state + 2))
+    return dict(moments=states, ms_per_call={k: round(v, 3) for k, v in med.items()}, ms_per_step=round(sum(med.values()), 2),
+                achieved_GBps={k: round(b / (med[k] * 1e-3) / 1e9, 1) for k, b in gb.items()}, grad_norm=float(coef[0]))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -126,6 +163,8 @@ def main():
                          "used for kernel profiles so that only the step's launches are in the trace")
     ap.add_argument("--calib-copy", action="store_true",
                     help="also run one plain 1 GiB device copy (calibration of the HBM traffic counters)")
+    ap.add_argument("--update", choices=("f32", "e4m3"), help="also time a whole training step of head and final norm, with AdamW moments in 32 "
+                    "or 8 bits (not part of `value`)")
     args = ap.parse_args()
     if args.gpus != 1:
         sys.exit("bench.py: this build measures one GPU only (no collectives, no sharding); run with --gpus 1")
@@ -268,6 +307,17 @@ def main():
                        tokens_per_s=round(n_scored / dt_f, 1),
                        pct_bf16_mfma_peak=round(100.0 * 2.0 * n_scored * d * V / dt_f / (MFMA_BF16_PEAK_TFLOPS * 1e12), 2))
 
+    train_leg = None
+    if args.update:
+        log("timing a whole training step")
+
+        def loss(hidden, head):
+            adv, _, _, _ = mrl.group_advantages(batch["rewards_all"], batch["group_all"], G, batch["in_stats"], batch["scored"], batch["is_own"])
+            seq_adv = adv if adv.numel() == B else synth.seq_adv_from(adv, batch)
+            mrl.grpo_loss_fwd_bwd(hidden, head, batch["targets"], mask, batch["behav"], batch["ref"], seq_adv, batch["seq_group"], batch["seq_kind"],
+                                  B, T, G, cfg, out_dH=out_dH, out_dW=out_dW, workspace=ws, out_logp=out_logp, out_stats=out_stats)
+        train_leg = training_leg(mrl, torch, batch, mask, loss, out_dH, out_dW, args.update)
+
     base = None
     if not args.no_cpu_baseline:
         log("timing the CPU oracle on a bounded sample")
@@ -282,6 +332,7 @@ def main():
                 pct_bf16_mfma_peak=round(pct_peak, 2), flop_per_token=flop_per_token,
                 roofline=roofline, measured_mfma_peak=measured_peak, kernel_classes=classes,
                 hbm_passes=hbm_passes, thl_word_align=thl_leg, scoring_forward_only=fwd_leg, cpu_baseline=base,
+                **({} if train_leg is None else dict(training_step=train_leg)),
                 loss=dict(total=stats["loss_total"], clip_frac=stats["n_clipped_tokens"] / max(n_scored, 1),
                           mean_ratio=stats["mean_ratio"]))
     print(json.dumps(line), flush=True)
