@@ -19,7 +19,7 @@ extern "C" {
 
 /* ------------------------------------------------------------------------
  * Per-kernel-class timing for benchmarks.  When enabled, every kernel launch
- * of the entry points of mrl.h is bracketed by HIP events on the launch stream.
+ * of calls (1) to (3) of mrl.h is bracketed by HIP events on the launch stream.
  * mrl_profile_collect synchronises the device, adds up the elapsed time and
  * launch count per class since the last collect, and resets the log.
  * Arrays are HOST memory of MRL_PROF_NCLASS entries.

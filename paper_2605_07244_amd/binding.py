@@ -578,6 +578,8 @@ class AdamWPlan(GradPlan):
             raise ValueError("params and grads must be as many, and of the same sizes")
         self.copies = None if copies is None else of(copies, torch.bfloat16, sizes, "copies")
         self.m, self.v = of(m, state_dtype, sizes, "m"), of(v, state_dtype, sizes, "v")
+        if codes and ((m is None) != (m_scale is None) or (v is None) != (v_scale is None)):
+            raise ValueError("8-bit moments and their scales are given together")
         blocks = [-(-n // STATE_BLOCK) for n in sizes]
         self.m_scale, self.v_scale = (of(x, torch.float32, blocks, name) if codes else None for x, name in ((m_scale, "m_scale"), (v_scale, "v_scale")))
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * self.count

@@ -320,7 +320,9 @@ def test_refusals(mrl):
             bad()
     for bad in (lambda: mrl.adamw_plan([p], [g[:9]]), lambda: mrl.adamw_plan([p, p], [g]), lambda: mrl.adamw_plan([p], [g], weight_decay=[0.1, 0.1]),
                 lambda: mrl.adamw_plan([p], [g], m=[]), lambda: mrl.grad_plan([torch.zeros(8, 8, device="cuda").t()]),
-                lambda: mrl.adamw_plan([p], [g], state_dtype=E4M3, m_scale=[torch.zeros(2, device="cuda")])):
+                lambda: mrl.adamw_plan([p], [g], state_dtype=E4M3, m_scale=[torch.zeros(2, device="cuda")]),
+                lambda: mrl.adamw_plan([p], [g], m=[torch.zeros(10, device="cuda").to(E4M3)]),
+                lambda: mrl.adamw_plan([p], [g], m=[torch.zeros(10, device="cuda").to(E4M3)], m_scale=[torch.zeros(2, device="cuda")])):
         with pytest.raises(ValueError):
             bad()
     plan = mrl.adamw_plan([p], [g])
