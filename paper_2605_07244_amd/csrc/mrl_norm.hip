@@ -363,11 +363,16 @@ int rows_side_by_side(const Shape& s) { return s.threads <= 64 ? 256 / s.threads
 // us, with 256, 512, 768, 1024 and 1280 workgroups: 351, 229, 238, 259, 282.  The partial sums of many are worth it to long calls only: rows of 4096 in
 // 512 threads, with 256 and 512 workgroups: 1000 rows 13.8 and 16.2, 4000 28.8 and 31.6, 24414 156 and 154; of 1536 in 192 threads, with 512 and 1024: 4000 rows
 // 17.3 and (768) 18.2, 65104 171 and 157.
-int back_blocks(int64_t N, int d) {
+// A long call without d_residual, which has fewer bytes under way for each of them, takes twice as many below 512 threads: 78125 rows of 2048 211 and 185 us, 62500 of 2560
+// 207 and 187; with d_residual 229 and 258, 235 and 260; 39062 rows of 4096 184 and 198 without.
+int back_blocks(int64_t N, int d, bool has_residual) {
   const Shape sh = back_shape(d);
   const int64_t b = (N + 2 * rows_side_by_side(sh) - 1) / (2 * rows_side_by_side(sh));
   const bool is_long = N >= 16384;
-  const int most = sh.threads == 192 && is_long ? 1024 : sh.vectors > 1 && sh.threads == 512 ? 256 : sh.threads >= 384 && !is_long ? 256 : 512;
+  int most = 512;
+  if (sh.threads == 512 && sh.vectors > 1) most = 256;
+  else if (!is_long) most = sh.threads >= 384 ? 256 : 512;
+  else if (sh.threads == 192 || (sh.threads > 64 && sh.threads < 512 && !has_residual)) most = 1024;
   return (int)(b < most ? b : most);
 }
 
@@ -396,7 +401,7 @@ template <bool kXBf16, int kRes> void go_norm(const NormArgs& a, hipStream_t s) 
 template <bool kHBf16, bool kDyBf16> void go_back(const NormBackArgs& a, hipStream_t s) {
   const Shape sh = back_shape(a.d);
   const bool waves = sh.threads <= 64;
-  const dim3 grid((unsigned)back_blocks(a.N, a.d)), block(waves ? 256 : sh.threads);
+  const dim3 grid((unsigned)back_blocks(a.N, a.d, a.d_residual != nullptr)), block(waves ? 256 : sh.threads);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, waves ? (size_t)a.d * 4 : 64 * 4, s, a); };
   switch (sh.threads * 8 + sh.vectors) {
     case 8 * 8 + 1: go(k_rms_norm_back<kHBf16, kDyBf16, 8, 1>); break;
@@ -451,7 +456,7 @@ extern "C" int mrl_rms_norm(const void* x, const void* residual, const void* wei
 
 extern "C" size_t mrl_rms_norm_backward_workspace(int64_t N, int32_t d) {
   if (N < 0 || N > kMaxRows || d <= 0 || d > kMaxWidth) return 0;
-  return (size_t)round_up((int64_t)back_blocks(N, d) * round_up(d, 4) * 4, 256);
+  return (size_t)round_up((int64_t)back_blocks(N, d, false) * round_up(d, 4) * 4, 256);     // (no fewer than with d_residual)
 }
 
 extern "C" int mrl_rms_norm_backward(const void* dy, const void* h, const void* weight, const void* d_residual, const uint8_t* token_mask,
@@ -468,7 +473,7 @@ extern "C" int mrl_rms_norm_backward(const void* dy, const void* h, const void* 
   const int rc = require_gfx950();
   if (rc != MRL_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int ld = (int)round_up(d, 4), blocks = N > 0 ? back_blocks(N, d) : 0;
+  const int ld = (int)round_up(d, 4), blocks = N > 0 ? back_blocks(N, d, d_residual != nullptr) : 0;
   float* parts = out_dweight != nullptr ? static_cast<float*>(workspace) : nullptr;
   if (N > 0) {
     const NormBackArgs a = {dy, h, weight, d_residual, token_mask, N, d, eps, 1.f / (float)d, weight_dtype == MRL_BF16, dx_dtype == MRL_BF16, out_dx, parts, ld};
