@@ -344,7 +344,7 @@ Shape norm_shape(int d) {
   const int v = (d + 7) / 8;
   if (v <= 64) return {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, 1};
   if (v <= 128) return {64, 2};
-  if (v <= 256) return {256, 1};
+  if (v <= 256) return {v <= 192 ? 192 : 256, 1};
   if (v <= 512) return {256, 2};
   if (v <= 1024) return {512, 2};
   return {1024, 2};
@@ -391,6 +391,7 @@ template <bool kXBf16, int kRes> void go_norm(const NormArgs& a, hipStream_t s) 
     case 32 * 8 + 1: go_norm_shape<kXBf16, kRes, 32, 1>(a, s); break;
     case 64 * 8 + 1: go_norm_shape<kXBf16, kRes, 64, 1>(a, s); break;
     case 64 * 8 + 2: go_norm_shape<kXBf16, kRes, 64, 2>(a, s); break;
+    case 192 * 8 + 1: go_norm_shape<kXBf16, kRes, 192, 1>(a, s); break;
     case 256 * 8 + 1: go_norm_shape<kXBf16, kRes, 256, 1>(a, s); break;
     case 256 * 8 + 2: go_norm_shape<kXBf16, kRes, 256, 2>(a, s); break;
     case 512 * 8 + 2: go_norm_shape<kXBf16, kRes, 512, 2>(a, s); break;

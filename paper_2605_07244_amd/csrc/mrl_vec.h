@@ -80,39 +80,58 @@ template <> struct Eight<false> {
 template <bool kStream, int kAlign, class V> __device__ inline void store_as(void* p, V v) {
   if (kStream) store_stream<kAlign>(p, v); else store_any<kAlign>(p, v);
 }
-// The thread's own ones of those columns, of a row of d.
+// The thread's own ones of those columns, of a row of d.  The end of a row, the last n = 8 - skip of the eight, goes out as four, two and one of
+// them, as n has bits: what is left below the four or the two begins at an odd element, if it is one.
 template <bool kStream = false> __device__ inline void store_eight(void* row, bool bf16, const Columns& c, int d, const float (&v)[8]) {
+  const int n = 8 - c.skip;
+  const bool four = n & 4;
   if (bf16) {
     uint16_t* p = static_cast<uint16_t*>(row) + c.at;
     const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     if (c.skip == 0 && d >= 8) {
       store_as<kStream, 2>(p, w);
-    } else if (c.skip < 8) {
+    } else if (d < 8) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 7; ++e)
         if (c.own(e, d)) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    } else if (n > 0) {
+      if (four) store_any<2>(p + 4, u32x2{w[2], w[3]});
+      if (n & 2) store_any<2>(p + (four ? 2 : 6), four ? w[1] : w[3]);
+      if (n & 1) p[c.skip] = (uint16_t)((c.skip < 4 ? c.skip < 2 ? w[0] : w[1] : c.skip < 6 ? w[2] : w[3]) >> 16);
     }
   } else {
     float* p = static_cast<float*>(row) + c.at;
+    const u32x4 lo = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    const u32x4 hi = {__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
     if (c.skip == 0 && d >= 8) {
-      store_as<kStream, 4>(p, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-      store_as<kStream, 4>(p + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
-    } else if (c.skip < 8) {
+      store_as<kStream, 4>(p, lo);
+      store_as<kStream, 4>(p + 4, hi);
+    } else if (d < 8) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 7; ++e)
         if (c.own(e, d)) p[e] = v[e];
+    } else if (n > 0) {
+      if (four) store_any<4>(p + 4, hi);
+      if (n & 2) store_any<4>(p + (four ? 2 : 6), four ? u32x2{lo[2], lo[3]} : u32x2{hi[2], hi[3]});
+      if (n & 1) store_any<4>(p + c.skip, c.skip < 4 ? c.skip < 2 ? lo[1] : lo[3] : c.skip < 6 ? hi[1] : hi[3]);
     }
   }
 }
 __device__ inline void store_eight_e4m3(void* row, const Columns& c, int d, const float (&v)[8]) {
   uint8_t* p = static_cast<uint8_t*>(row) + c.at;
   const u32x2 w = {pack_e4m3(v[0], v[1], v[2], v[3]), pack_e4m3(v[4], v[5], v[6], v[7])};
+  const int n = 8 - c.skip;
+  const bool four = n & 4;
   if (c.skip == 0 && d >= 8) {
     store_any<1>(p, w);
-  } else if (c.skip < 8) {
+  } else if (d < 8) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < 7; ++e)
       if (c.own(e, d)) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+  } else if (n > 0) {
+    if (four) store_any<1>(p + 4, w[1]);
+    if (n & 2) store_any<1>(p + (four ? 2 : 6), (uint16_t)((four ? w[0] : w[1]) >> 16));
+    if (n & 1) p[c.skip] = (uint8_t)((c.skip < 4 ? w[0] : w[1]) >> (8 * (c.skip & 3)));
   }
 }
 
