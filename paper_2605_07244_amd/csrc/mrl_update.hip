@@ -226,7 +226,7 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
 // A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.
 template <bool kCodes>
 __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
-  const int chunk = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  const int chunk = (int)(blockIdx.y * gridDim.x + blockIdx.x);       // (at most 2^30 and the rest of a row of workgroups)
   if (chunk >= a.chunks) return;
   const int i = tensor_of<AdamTable<kCodes>::kTensors>(a.chunk0, chunk);
   const AdamTensor<kCodes>& t = a.t[i];
@@ -347,7 +347,7 @@ int check_tensors(const mrl_param_tensor* t, int32_t count, bool update, bool co
     if (!t[i].param || !t[i].m || !t[i].v || (codes && (!t[i].m_scale || !t[i].v_scale))) return MRL_ERR_NULL;
     if (!(t[i].weight_decay >= 0.f && t[i].weight_decay < INFINITY)) return MRL_ERR_CONFIG;
   }
-  return chunks < (int64_t)1 << 31 ? MRL_OK : MRL_ERR_SHAPE;
+  return chunks <= (int64_t)1 << 30 ? MRL_OK : MRL_ERR_SHAPE;            // (256 elements each: more than a device holds)
 }
 
 // Calls f(first, last) for the tensors of each launch: at most kMost of them that are not empty.
