@@ -335,6 +335,18 @@ def test_more_rows_than_a_launch_is_wide(mrl, N, d):
     assert torch.all((dw - dw0).abs() <= 404 * U * (ends.double().square() / (ends.double().square().mean(1, keepdim=True) + EPS).sqrt()).sum(0))
 
 
+def test_mask_in_the_shape_of_the_batch(mrl):
+    """A mask [B, T] serves the rows [B * T, d], as it does the scoring step."""
+    B, T, d = 5, 37, 200
+    x, w = _rand((B * T, d), BF16, 1), _rand((d,), BF16, 2)
+    mask = (torch.arange(T, device="cuda")[None] < torch.tensor([0, 1, 17, 36, 37], device="cuda")[:, None]).to(torch.uint8)
+    for a, b in zip(mrl.rms_norm(x, w, EPS, x, mask, E4M3), mrl.rms_norm(x, w, EPS, x, mask.reshape(-1), E4M3)):
+        assert torch.equal(a.float(), b.float())
+    _check_backward(mrl, x, x, w, None, mask.reshape(-1))
+    for a, b in zip(mrl.rms_norm_backward(x, x, w, EPS, None, mask), mrl.rms_norm_backward(x, x, w, EPS, None, mask.reshape(-1))):
+        assert torch.equal(a, b)
+
+
 def test_no_rows(mrl):
     w = torch.ones(16, device="cuda")
     x = torch.empty((0, 16), device="cuda")

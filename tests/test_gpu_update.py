@@ -1,7 +1,7 @@
 """Gradient norm and AdamW against 64 bits: sizes around lanes, blocks and chunks, many tensors, both kinds of moments, and a whole training step of
 head and norm.
 
-Bounds.  U = 2^-24.  m is two products and a fused addition of numbers known to U: 3 U of its terms; v has one more product.  The update's
+Bounds.  U = 2^-24.  m is two products and a sum of numbers known to U: 4 U of its terms; v has one more product.  The update's
 quotient adds the root (half of v's error, one rounding), a product, the addition of eps and the division: 10 U of itself; p itself is rounded once."""
 import numpy as np
 import pytest
@@ -309,6 +309,42 @@ def test_more_than_2_33_elements(mrl):
     uo.check_codes("m", m[first:], ms[first // 256:], m1, bits & 0xFFFF, False)
     uo.check_codes("sqrt(v)", v[first:], vs[first // 256:], np.sqrt(v1), bits >> 16, True)
     assert not bool(p[:2 ** 20].any()) and not bool(p[2 ** 31 - 1000:2 ** 31 + 1000].any())
+
+
+def test_threads_on_streams_of_their_own(mrl):
+    """Calls of several host threads at once, each on its own stream and data, give what the same calls give one after the other."""
+    import threading
+
+    def work(k, out):
+        g = torch.Generator("cuda").manual_seed(k)
+        N, d = 700 + 300 * k, 513 + 64 * k
+        x, w = torch.randn((N, d), device="cuda", generator=g), 1 + 0.1 * torch.randn(d, device="cuda", generator=g)
+        p, grad = [w.clone(), x.reshape(-1).clone()], [torch.empty(d, device="cuda"), torch.empty(N * d, device="cuda")]
+        plan = mrl.adamw_plan(p, grad, state_dtype=E4M3 if k % 2 else F32)
+        for t in range(1, 6):
+            y, h, _ = mrl.rms_norm(p[1].view(N, d), p[0], 1e-5, x)
+            dx, _ = mrl.rms_norm_backward(y, h, p[0], 1e-5, out_dweight=grad[0])
+            grad[1].copy_(dx.reshape(-1))
+            mrl.adamw_step(plan, 1e-3, t, norm_coef=mrl.grad_norm(plan, 1.0), seed=k)
+        torch.cuda.current_stream().synchronize()
+        out[k] = [x.clone() for x in (*p, *plan.m, *plan.v)]
+
+    alone, together = {}, {}
+    for k in range(4):
+        work(k, alone)
+
+    def on_a_stream(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            work(k, together)
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=on_a_stream, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for k in range(4):
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(alone[k], together[k])), k
 
 
 def test_refusals(mrl):
