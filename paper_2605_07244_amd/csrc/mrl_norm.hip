@@ -382,7 +382,8 @@ int rows_side_by_side(const Shape& s) { return s.threads <= 64 ? 256 / s.threads
 // 512 threads, with 256 and 512 workgroups: 1000 rows 13.8 and 16.2, 4000 28.8 and 31.6, 24414 156 and 154; of 1536 in 192 threads, with 512 and 1024: 4000 rows
 // 17.3 and (768) 18.2, 65104 171 and 157.
 // A long call without d_residual, which has fewer bytes under way for each of them, takes twice as many below 512 threads: 78125 rows of 2048 211 and 185 us, 62500 of 2560
-// 207 and 187; with d_residual 229 and 258, 235 and 260; 39062 rows of 4096 184 and 198 without.
+// 207 and 187, 468750 of 128 111 and 81; with d_residual 229 and 258, 235 and 260; 39062 rows of 4096 184 and 198 without.  Rows that share a wave take three a compute
+// unit with it (468750 of 128 with 512, 768 and 1024: 120, 101, 104).
 int back_blocks(int64_t N, int d, bool has_residual) {
   const Shape sh = back_shape(d);
   const int64_t b = (N + 2 * rows_side_by_side(sh) - 1) / (2 * rows_side_by_side(sh));
@@ -390,7 +391,8 @@ int back_blocks(int64_t N, int d, bool has_residual) {
   int most = 512;
   if (sh.threads == 512 && sh.vectors > 1) most = 256;
   else if (!is_long) most = sh.threads >= 384 ? 256 : 512;
-  else if (sh.threads == 192 || (sh.threads > 64 && sh.threads < 512 && !has_residual)) most = 1024;
+  else if (sh.threads == 192 || (sh.threads < 512 && sh.vectors == 1 && !has_residual)) most = 1024;
+  else if (sh.threads < 64) most = 768;
   return (int)(b < most ? b : most);
 }
 
