@@ -59,6 +59,8 @@ template <int kWaves> __device__ inline double block_sum_f64(double x, double* s
   return s;
 }
 
+// A partial sum of squares for each workgroup, which takes every gridDim.x-th chunk.  A chunk that is squared and added in fp64 (exact squares of float and
+// bf16) costs less than its read: 233 M floats in 151 us, 6.2 TB/s; with 1024 and 4096 workgroups in place of 2048 163 and 154.
 __global__ __launch_bounds__(256) void k_square_sums(NormTable a) {
   __shared__ double sh[4];
   double s = 0.0;
@@ -223,7 +225,10 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
   for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
 }
 
-// A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.
+// A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.  Memory bounds it: 30 bytes an element with 32-bit moments
+// (233 M in 1156 us, 6.06 TB/s), 18 with 8-bit ones (263 M in 770 us, 6.2 TB/s), where the hash, the roots and the quotients fit beside the loads.  Everything passes
+// the caches: nothing is read again before all the rest has gone through them (kept 1315 us, loads or stores streamed 1303 and 1311, both 1252, then in
+// workgroups of one wave and 256 elements 1161; of 128, 512 and 1024 threads 1182, 1249, 1230).
 template <bool kCodes>
 __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
   const int chunk = (int)(blockIdx.y * gridDim.x + blockIdx.x);       // (at most 2^30 and the rest of a row of workgroups)
