@@ -343,7 +343,7 @@ int mrl_thl_word_align(const float* src_logp /*[B,S_src] dev*/, const uint8_t* s
  *   out_y [N, d], y_dtype MRL_F32, MRL_BF16 or MRL_E4M3.  MRL_E4M3: out_y holds codes q and out_scale
  *   the floats they are multiplied by, scale = max(max |y|, 2^-100) / 448 over the row
  *   (scale_block = 0, out_scale [N]) or over every 128 columns (scale_block = 128,
- *   out_scale [N, ceil(d / 128)]), q = y / scale (taken as y (448 / max)) rounded to nearest even.  A NaN among them makes the scale
+ *   out_scale [N, ceil(d / 128)]), q = y / scale rounded to nearest even.  A NaN among them makes the scale
  *   NaN, an infinity makes it infinite.  Other types: out_scale NULL, scale_block 0.
  *   token_mask [N] or NULL: rows with mask 0 are not read; their h and y are zero, their scales
  *   those of a zero row.

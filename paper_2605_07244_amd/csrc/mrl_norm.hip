@@ -58,6 +58,13 @@ template <int kT> __device__ inline void load_weights(const void* w, bool bf16, 
   }
 }
 
+// Largest magnitude / 448, rounded as the division is: a product and a step that corrects it.
+__device__ inline float scale_of(uint32_t most) {
+  constexpr float kInverse = 1.f / kE4m3Max;
+  const float x = __uint_as_float(most), q = x * kInverse;
+  return x < INFINITY ? fmaf(fmaf(-q, kE4m3Max, x), kInverse, q) : x;
+}
+
 // kT threads take a row, each kNV times eight elements; below 64 threads a workgroup of 256 takes several.  kRes: 0 no residual, 1 bf16, 2 float.
 // Memory bounds it: 65536 rows of 2048 with a residual, bf16, 178 us, 6.0 TB/s; 500000 of 128 86 us, 5.9; 32768 of 4096, a third scored, 133 us, 5.4.  Two
 // vectors a thread at most, and a workgroup to a row: 5000 rows of 4096 in a wave each 34 us, in 128, 256 and 512 threads 32, 28 and 29.
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(kT < 64 ? 256 : kT) void k_rms_norm(NormArgs a) {
       if (a.y_type == MRL_E4M3) store_eight_e4m3(y, c, d, zero); else store_eight(y, a.y_type == MRL_BF16, c, d, zero);
     }
     if (a.y_type == MRL_E4M3)
-      for (int k = t; k < scales; k += kT) a.scale[row * scales + k] = __uint_as_float(kScaleLeast) / kE4m3Max;
+      for (int k = t; k < scales; k += kT) a.scale[row * scales + k] = scale_of(kScaleLeast);
     return;
   }
   float h[kNV][8], w[kNV][8];
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(kT < 64 ? 256 : kT) void k_rms_norm(NormArgs a) {
     for (int i = 0; i < kNV; ++i) {
       most[i] = lanes_max<16>(most[i]);
       const int block = (i * kT + t) / 16;
-      if ((t & 15) == 0 && block < scales) a.scale[row * scales + block] = __uint_as_float(most[i]) / kE4m3Max;
+      if ((t & 15) == 0 && block < scales) a.scale[row * scales + block] = scale_of(most[i]);
     }
   } else {
 #pragma unroll
@@ -159,13 +166,19 @@ __global__ __launch_bounds__(kT < 64 ? 256 : kT) void k_rms_norm(NormArgs a) {
     most[0] = group_max<kT>(most[0], sh_max);
 #pragma unroll
     for (int i = 1; i < kNV; ++i) most[i] = most[0];
-    if (t == 0) a.scale[row] = __uint_as_float(most[0]) / kE4m3Max;
+    if (t == 0) a.scale[row] = scale_of(most[0]);
   }
 #pragma unroll
   for (int i = 0; i < kNV; ++i) {
-    const float inverse = kE4m3Max / __uint_as_float(most[i]);
+    // y / scale: a product with the reciprocal and a step that corrects it, as exact as a division and a third of its instructions (the product alone is
+    // off by another half a step of fp32, and twice as many codes fall on the other side of a rounding as need be).  Infinite scales: reciprocal and
+    // divisor zero leave finite values at zero.
+    const float scale = scale_of(most[i]), inverse = __builtin_amdgcn_rcpf(scale), divisor = scale < INFINITY ? scale : 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[i][e] *= inverse;
+    for (int e = 0; e < 8; ++e) {
+      const float q = h[i][e] * inverse;
+      h[i][e] = fmaf(fmaf(-q, divisor, h[i][e]), inverse, q);
+    }
     store_eight_e4m3(y, Columns((i * kT + t) * 8, d), d, h[i]);
   }
 }
