@@ -281,7 +281,7 @@ def test_slices_at_any_address(mrl):
         assert bool((guard[:off] == 7).all()) and bool((guard[off + N * d:] == 7).all()) and gw[0] == 7 and gw[-1] == 7
 
 
-@pytest.mark.parametrize("N,d", [(3, 100), (1200, 1536), (2, 9000)])
+@pytest.mark.parametrize("N,d", [(3, 100), (700, 9), (50, 1001), (1200, 1536), (700, 1537), (300, 4099), (2, 9000), (20, 12345)])
 def test_outputs_in_the_inputs_buffers(mrl, N, d):
     x, r, w = _rand((N, d), BF16, 1), _rand((N, d), BF16, 2), _rand((d,), BF16, 3)
     y, h, _ = mrl.rms_norm(x, w, EPS, r)
