@@ -371,6 +371,7 @@ int mrl_rms_norm(const void* x /*[N,d] dev*/, const void* residual /*[N,d] dev |
  *   out_dx is d_residual, or zero.
  *   out_dweight [d] float, or NULL to skip it; accumulate_dw = 1 adds into it.  Sums over rows have a fixed
  *   order: bit-reproducible.  The workspace is needed with out_dweight only; a smaller one is refused.
+ *   N = 0 needs no pointer but out_dweight, where it is wanted: zeros, or what it held.
  *   out_dx may be the buffer of dy, h or d_residual where the types have the same size.
  * ---------------------------------------------------------------------- */
 size_t mrl_rms_norm_backward_workspace(int64_t N, int32_t d);

@@ -503,7 +503,7 @@ extern "C" int mrl_rms_norm_backward(const void* dy, const void* h, const void* 
   if (N < 0 || N > kMaxRows || d <= 0 || d > kMaxWidth) return MRL_ERR_SHAPE;
   if (!is_float_type(dy_dtype) || !is_float_type(h_dtype) || !is_float_type(weight_dtype) || !is_float_type(dx_dtype)) return MRL_ERR_DTYPE;
   if (!(eps >= 1e-30f && eps < 1e30f) || (accumulate_dw != 0 && accumulate_dw != 1)) return MRL_ERR_CONFIG;
-  if ((N > 0 && (!dy || !h || !weight || !out_dx)) || (N == 0 && !out_dweight && !out_dx)) return MRL_ERR_NULL;
+  if (N > 0 && (!dy || !h || !weight || !out_dx)) return MRL_ERR_NULL;
   if (out_dweight != nullptr && N > 0 &&
       (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < mrl_rms_norm_backward_workspace(N, d)))
     return MRL_ERR_WORKSPACE;

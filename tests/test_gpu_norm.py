@@ -465,3 +465,12 @@ def test_captured_and_replayed(mrl):
         dx1, _ = mrl.rms_norm_backward(dy, h1, w, EPS, out_dweight=total, accumulate=True)
         assert torch.equal(y, y1) and torch.equal(h, h1) and torch.equal(q.float(), q1.float()) and torch.equal(s, s1)
         assert torch.equal(dx, dx1) and torch.equal(dw, total), k
+
+
+def test_no_rows_without_a_weight_gradient(mrl):
+    w = torch.ones(16, device="cuda")
+    for x_type in (F32, BF16):
+        x = torch.empty((0, 16), device="cuda", dtype=x_type)
+        for mask in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+            dx, dw = mrl.rms_norm_backward(x, x, w, EPS, x, mask, want_dweight=False)
+            assert dx.shape == (0, 16) and dx.dtype == x_type and dw is None

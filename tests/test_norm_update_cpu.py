@@ -190,3 +190,10 @@ def test_codes_of_the_oracle():
     assert abs(np.corrcoef(a, b)[0, 1]) < 5 / np.sqrt(n)
     for other in (dict(seed=78, step=3, place=2), dict(seed=77, step=4, place=2), dict(seed=77, step=3, place=3), dict(seed=77 + (1 << 32), step=3, place=2)):
         assert np.mean(uo.random_bits(n, **other) == bits) < 1e-3
+
+
+def test_no_rows_need_no_pointers():
+    """An empty tensor has no device pointer: a call of no rows that asks for no weight gradient has none at all."""
+    for pointers in (dict(dx=None), dict(dx=None, dy=None, h=None, w=None, ws=None, ws_bytes=0)):
+        assert _back(N=0, dw=None, **pointers) == 0, pointers
+    assert _back(N=0, dw=None, dx=None, d=0) == -2 and _back(N=0, dw=None, dx=None, eps=0.0) == -7
