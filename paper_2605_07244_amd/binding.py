@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib.util
+import operator
 import os
 import warnings
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
@@ -456,6 +457,13 @@ def _shaped(t, shape, name):
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
 
 
+def _fits(n, bits, name):
+    """ctypes cuts a number to the bits that the C interface has for it; one that needs more is refused here."""
+    if not -(1 << bits - 1) <= n < 1 << bits - 1:
+        raise ValueError(f"{name} does not fit in {bits} bits: {n}")
+    return n
+
+
 def rms_norm(x, weight, eps=1e-6, residual=None, token_mask=None, out_dtype=None, scale_block=0):
     """mrl_rms_norm: (y [N, d], h [N, d] or None, scale or None) of x [N, d].  h = x + residual is returned with a residual, in
     its type; out_dtype float8_e4m3fn (None: the type of x) makes y codes, to be multiplied by scale [N] or, with
@@ -473,6 +481,8 @@ def rms_norm(x, weight, eps=1e-6, residual=None, token_mask=None, out_dtype=None
     if x.dim() != 2:
         raise ValueError("x must be [N, d]")
     N, d = x.shape
+    _fits(d, 32, "the number of columns")
+    scale_block = _fits(operator.index(scale_block), 32, "scale_block")
     _shaped(weight, (d,), "weight")
     _shaped(residual, (N, d), "residual")
     if token_mask is not None and token_mask.numel() != N:
@@ -484,7 +494,7 @@ def rms_norm(x, weight, eps=1e-6, residual=None, token_mask=None, out_dtype=None
     y = torch.empty((N, d), dtype=out_dtype, device=x.device)
     h = torch.empty((N, d), dtype=residual.dtype, device=x.device) if residual is not None else None
     scale = torch.empty((N, -(-d // scale_block)) if scale_block > 0 else (N,), dtype=torch.float32, device=x.device) if out_dtype == torch.float8_e4m3fn else None
-    _check(lib().mrl_rms_norm(*args, N, d, float(eps), xt, rt, wt, codes[out_dtype], int(scale_block), _ptr(h), _ptr(y), _ptr(scale), _stream()),
+    _check(lib().mrl_rms_norm(*args, N, d, float(eps), xt, rt, wt, codes[out_dtype], scale_block, _ptr(h), _ptr(y), _ptr(scale), _stream()),
            "mrl_rms_norm")
     return y, h, scale
 
@@ -507,6 +517,7 @@ def rms_norm_backward(dy, h, weight, eps=1e-6, d_residual=None, token_mask=None,
     if h.dim() != 2:
         raise ValueError("h must be [N, d]")
     N, d = h.shape
+    _fits(d, 32, "the number of columns")
     _shaped(dy, (N, d), "dy")
     _shaped(weight, (d,), "weight")
     _shaped(d_residual, (N, d), "d_residual")
@@ -647,7 +658,7 @@ def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
             setattr(c, name + "_dev", _ptr(x, dtype, name))
             _here(x)
         else:
-            setattr(c, name, float(x) if name == "lr" else int(x))
+            setattr(c, name, float(x) if name == "lr" else _fits(int(x), 64, name))
     if norm_coef is not None and norm_coef.numel() != 2:
         raise ValueError("norm_coef must have two entries")
     coef = None if norm_coef is None else _ptr(norm_coef, torch.float32, "norm_coef") + 4

@@ -197,3 +197,26 @@ def test_no_rows_need_no_pointers():
     for pointers in (dict(dx=None), dict(dx=None, dy=None, h=None, w=None, ws=None, ws_bytes=0)):
         assert _back(N=0, dw=None, **pointers) == 0, pointers
     assert _back(N=0, dw=None, dx=None, d=0) == -2 and _back(N=0, dw=None, dx=None, eps=0.0) == -7
+
+
+def test_numbers_past_32_bits_are_refused(monkeypatch):
+    """The C interface takes widths and scale blocks in 32 bits.  Cut to them, 2^32 + 128 would be a block of 128 next to an output with one scale a
+    row, and a row of 2^32 + 16 columns one of 16.  (Tensors that are not on a GPU: these are checked before anything needs one.)"""
+    x, w = torch.zeros(4, 256), torch.zeros(256)
+    for block in ((1 << 32) + 128, 1 << 32, -(1 << 32), 1 << 31, 1 << 70):
+        with pytest.raises(ValueError, match="scale_block"):
+            m.rms_norm(x, w, out_dtype=torch.float8_e4m3fn, scale_block=block)
+    for d in (1 << 31, (1 << 32) + 16):
+        x, w = torch.empty((1, d), device="meta"), torch.empty(d, device="meta")
+        with pytest.raises(ValueError, match="columns"):
+            m.rms_norm(x, w)
+        with pytest.raises(ValueError, match="columns"):
+            m.rms_norm_backward(x, x, w)
+    # a step is counted in 64 bits
+    monkeypatch.setattr(binding, "_native", False)
+    plan = object.__new__(m.AdamWPlan)
+    for name, value in dict(address=0, count=0, workspace=torch.zeros(1, dtype=torch.uint8), state_dtype=binding.F32, table=None).items():
+        setattr(plan, name, value)
+    for step in (1 << 63, (1 << 64) + 5):
+        with pytest.raises(ValueError, match="step"):
+            m.adamw_step(plan, 1e-3, step)
