@@ -424,7 +424,8 @@ int mrl_grad_norm(const mrl_param_tensor* tensors /*host*/, int32_t count, doubl
  *      mix(lo(i) ^ mix(key + hi(i))), key = mix(lo(seed) ^ mix(hi(seed) ^ mix(lo(t) ^ mix(j)))), with
  *      mix(x): x = (x ^ x >> 16) * 0x6A09E667, x = (x ^ x >> 15) * 0xBB67AE85, x ^ x >> 16 on 32 bits, lo and hi the
  *      32-bit halves; the low 16 bits serve m, the high 16 sqrt(v).  The same seed gives the same bits.
- *      A gradient that is not finite makes its block of 8-bit moments NaN; with 32-bit moments its element.
+ *      A gradient that is not finite makes its block of 8-bit moments NaN, and one whose (1 - b2) g^2 fp32 does not hold that of sqrt(v); with 32-bit
+ *      moments those of its own element are no longer finite.
  *      The buffers of all tensors are updated in place and must not overlap: mrl_adamw_check says whether they do. */
 typedef struct {
   double lr, beta1, beta2, eps;  /* lr >= 0; 0 <= beta < 1; eps >= 1e-30 */

@@ -168,6 +168,10 @@ __device__ inline float plus(float a, float b) {
   return a + b;
 }
 
+// The scale of a block with this largest magnitude.  x - x is zero, or NaN where x is infinite: under an infinite scale sqrt(v) would decode to infinity
+// and hold the block's weights where they are for good.
+__device__ inline float scale_or_nan(float x) { return plus(times(x, 1.f / kE4m3Max), plus(x, -x)); }
+
 // What the elements of a launch share.
 struct Rates { float lr, inv_fix1, inv_root_fix2, coef, b1, one_b1, b2, one_b2, eps, decay; };
 
@@ -205,8 +209,8 @@ struct Four {
     }
     *mw = pack_e4m3(mq[0], mq[1], mq[2], mq[3]);
     *vw = pack_e4m3(vq[0], vq[1], vq[2], vq[3]);
-    *m_scale = times(m_max, 1.f / kE4m3Max);
-    *v_scale = times(v_max, 1.f / kE4m3Max);
+    *m_scale = scale_or_nan(m_max);
+    *v_scale = scale_or_nan(v_max);
   }
   __device__ void decode(uint32_t mw, uint32_t vw, float m_scale, float v_scale) {
     const auto m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)mw, true);

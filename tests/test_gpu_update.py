@@ -423,3 +423,35 @@ def test_a_training_step_of_head_and_norm(mrl):
             p_o, m_o, v_o = uo.adamw(f64(p_old).reshape(-1), gc, 0 * gc, 0 * gc, 1e-3, 1, decay=decay)
             assert np.all(np.abs(f64(p_new).reshape(-1) - p_o) <= U * np.abs(p_o) + 1e-3 * 24 * U)
             assert torch.equal(c16, p_new.to(BF16))
+
+
+@pytest.mark.parametrize("n", [700, 512, 256, 3])
+@pytest.mark.parametrize("odd", [float("inf"), -float("inf"), float("nan"), 1e21])
+def test_8_bit_moments_of_no_numbers(mrl, n, odd):
+    """A gradient that is not finite makes both 8-bit moments of its block NaN, one whose square is not (1e-3 * 1e42 is above 3.4e38) the second: a scale
+    that is infinite instead would leave v infinite, and an infinite v holds the block's weights where they are, for good and without a sign of it.  Other blocks do not see it."""
+    at = n - 1 if n < 512 else 300
+    block = slice(at // 256 * 256, min(at // 256 * 256 + 256, n))
+    g = _rand(n, 2, 1e-3)
+    sets = []
+    for spoiled in (False, True):
+        m, v, ms, vs = _moments(n, 5, E4M3)
+        grad = g.clone()
+        if spoiled:
+            grad[at] = odd
+        p = _rand(n, 1, 0.02)
+        sets.append((p, grad, mrl.adamw_plan([p], [grad], None, [m], [v], [ms], [vs])))
+    for t in (5, 6):
+        for p, grad, plan in sets:
+            mrl.adamw_step(plan, 1e-3, t, seed=3)
+        torch.cuda.synchronize()
+        (p0, _, clean), (p1, _, plan) = sets
+        m, root = uo.decode(plan.m[0], plan.m_scale[0]), uo.decode(plan.v[0], plan.v_scale[0])
+        assert np.all(np.isnan(root[block])), (t, int(np.isinf(root).sum()))
+        assert np.all(np.isnan(m[block])) if not np.isfinite(odd) else np.all(np.isfinite(m[block]))
+        rest = np.ones(n, dtype=bool)
+        rest[block] = False
+        assert np.array_equal(m[rest], uo.decode(clean.m[0], clean.m_scale[0])[rest]) and np.array_equal(root[rest], uo.decode(clean.v[0], clean.v_scale[0])[rest])
+        assert np.array_equal(f64(p1)[rest], f64(p0)[rest])
+        if t == 6:
+            assert np.all(np.isnan(f64(p1)[block]))
