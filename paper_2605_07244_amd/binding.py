@@ -547,12 +547,20 @@ def rms_norm_backward(dy, h, weight, eps=1e-6, d_residual=None, token_mask=None,
 STATE_BLOCK = 256              # elements of a tensor that share the scales of 8-bit moments
 
 
+def _tensors(given, name, optional=False):
+    given = list(given)
+    for t in given:
+        if not (isinstance(t, torch.Tensor) or (optional and t is None)):
+            raise TypeError(f"{name} must hold tensors{' or None' if optional else ''}, got {type(t).__name__}")
+    return given
+
+
 class GradPlan:
     """The gradients of a set of tensors, laid out for grad_norm: built once, good for as long as the tensors keep their memory (which the
     plan holds on to).  Calls with one plan share its workspace: they belong on one stream, or must be ordered."""
 
     def __init__(self, grads):
-        self.grads = list(grads)
+        self.grads = _tensors(grads, "grads")
         self._fill(len(self.grads))
         for row, g in zip(self.table, self.grads):
             row.n, row.grad, row.grad_dtype = g.numel(), _ptr(g, name="grad"), _float_code(g, "grad")
@@ -574,20 +582,20 @@ class AdamWPlan(GradPlan):
         if state_dtype not in (torch.float32, torch.float8_e4m3fn):
             raise TypeError(f"state_dtype must be float32 or float8_e4m3fn, got {state_dtype}")
         codes = state_dtype == torch.float8_e4m3fn
-        self.state_dtype, self.params = E4M3 if codes else F32, list(params)
+        self.state_dtype, self.params = E4M3 if codes else F32, _tensors(params, "params")
         sizes = [g.numel() for g in self.grads]
 
-        def of(given, dtype, sizes, name):
+        def of(given, dtype, sizes, name, optional=False):
             if given is None:
                 return [torch.zeros(n, dtype=dtype, device=self.device) for n in sizes]
-            given = list(given)
-            if [t.numel() for t in given] != sizes:
+            given = _tensors(given, name, optional)
+            if len(given) != len(sizes) or any(t is not None and t.numel() != n for t, n in zip(given, sizes)):
                 raise ValueError(f"{name} must hold a tensor for each of {len(sizes)}, of their sizes")
             return given
 
         if [p.numel() for p in self.params] != sizes:
             raise ValueError("params and grads must be as many, and of the same sizes")
-        self.copies = None if copies is None else of(copies, torch.bfloat16, sizes, "copies")
+        self.copies = None if copies is None else of(copies, torch.bfloat16, sizes, "copies", optional=True)
         self.m, self.v = of(m, state_dtype, sizes, "m"), of(v, state_dtype, sizes, "v")
         if codes and ((m is None) != (m_scale is None) or (v is None) != (v_scale is None)):
             raise ValueError("8-bit moments and their scales are given together")
@@ -614,10 +622,10 @@ def grad_plan(grads) -> GradPlan:
 
 def adamw_plan(params, grads, copies=None, m=None, v=None, m_scale=None, v_scale=None, state_dtype=None, weight_decay=0.01) -> AdamWPlan:
     """A plan for adamw_step: params float32 tensors, grads (float32 or bfloat16) the buffers that their gradients are written to, copies
-    the bfloat16 tensors that new weights are copied to, or None.  Moments that are not given start at zero, in state_dtype: float32 (the default, or that
+    the bfloat16 tensors that new weights are copied to, None for tensors without one or for all.  Moments that are not given start at zero, in state_dtype: float32 (the default, or that
     of m) or float8_e4m3fn.  weight_decay: a number, or one for each tensor."""
     if state_dtype is None:
-        m = None if m is None else list(m)
+        m = None if m is None else _tensors(m, "m")
         state_dtype = m[0].dtype if m else torch.float32
     return AdamWPlan(params, grads, copies, m, v, m_scale, v_scale, state_dtype, weight_decay)
 

@@ -455,3 +455,24 @@ def test_8_bit_moments_of_no_numbers(mrl, n, odd):
         assert np.array_equal(f64(p1)[rest], f64(p0)[rest])
         if t == 6:
             assert np.all(np.isnan(f64(p1)[block]))
+
+
+def test_copies_of_some_tensors(mrl):
+    """None in a list of copies: that tensor has none, the others' are written, and the weights are those of a plan without any."""
+    sizes = [5, 300, 1000]
+    for states in (F32, E4M3):
+        a, b = Set(mrl, sizes, F32, states, copy=False), Set(mrl, sizes, F32, states, copy=False)
+        copies = [None, torch.empty(300, dtype=BF16, device="cuda"), None]
+        plan = mrl.adamw_plan(a.p, a.g, copies, a.m, a.v, a.ms, a.vs, weight_decay=0.01)
+        mrl.adamw_step(plan, 1e-3, 2, seed=8)
+        mrl.adamw_step(b.plan, 1e-3, 2, seed=8)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.all(), b.all()))
+        assert torch.equal(copies[1], a.p[1].to(BF16))
+        with pytest.raises(ValueError):
+            mrl.adamw_plan(a.p, a.g, copies[:2], a.m, a.v, a.ms, a.vs)
+        with pytest.raises(ValueError):
+            mrl.adamw_plan(a.p, a.g, [None, copies[1][:299], None], a.m, a.v, a.ms, a.vs)
+        for bad in (dict(params=[a.p[0], None, a.p[2]]), dict(v=[a.v[0], None, a.v[2]])):
+            with pytest.raises(TypeError, match="must hold tensors"):
+                mrl.adamw_plan(**(dict(params=a.p, grads=a.g, m=a.m, v=a.v, m_scale=a.ms, v_scale=a.vs) | bad))

@@ -220,3 +220,12 @@ def test_numbers_past_32_bits_are_refused(monkeypatch):
     for step in (1 << 63, (1 << 64) + 5):
         with pytest.raises(ValueError, match="step"):
             m.adamw_step(plan, 1e-3, step)
+
+
+def test_plans_of_no_tensors_are_refused():
+    """A parameter without a gradient has None in its place; so have lists that do not hold what they should."""
+    w = torch.zeros(8)
+    for bad in (lambda: m.grad_plan([None]), lambda: m.grad_plan([w, None]), lambda: m.adamw_plan([w], [None]), lambda: m.grad_plan([1.0]),
+                lambda: m.adamw_plan([w], [w], m=[None]), lambda: m.adamw_plan([w], [w], m=["m"])):
+        with pytest.raises(TypeError, match="must hold tensors"):
+            bad()
