@@ -556,8 +556,9 @@ def _tensors(given, name, optional=False):
 
 
 class GradPlan:
-    """The gradients of a set of tensors, laid out for grad_norm: built once, good for as long as the tensors keep their memory (which the
-    plan holds on to).  Calls with one plan share its workspace: they belong on one stream, or must be ordered."""
+    """The gradients of a set of tensors, laid out for grad_norm: built once, good for as long as the tensors keep their memory.  (The plan holds on to that
+    memory, so that one whose tensors were given other memory, by `t.data = ...` or a new entry in its lists, still writes to the old.)  Calls with one plan share its workspace: they belong on one stream,
+    the one that was current when the plan was made, or must be ordered; a captured call needs the plan for as long as it is replayed."""
 
     def __init__(self, grads):
         self.grads = _tensors(grads, "grads")
@@ -565,6 +566,7 @@ class GradPlan:
         for row, g in zip(self.table, self.grads):
             row.n, row.grad, row.grad_dtype = g.numel(), _ptr(g, name="grad"), _float_code(g, "grad")
         _here(*self.grads)
+        self._memory = [g.untyped_storage() for g in self.grads]
         self.device = self.grads[0].device if self.grads else torch.device("cuda", torch.cuda.current_device())
         self.workspace = _workspace(lib().mrl_grad_norm_workspace(self.table, self.count), self.device)
 
@@ -611,7 +613,9 @@ class AdamWPlan(GradPlan):
             if codes:
                 row.m_scale, row.v_scale = (_ptr(t[i], torch.float32, name) for t, name in ((self.m_scale, "m_scale"), (self.v_scale, "v_scale")))
             row.weight_decay = decay[i]
-        _here(*self.params, *(self.copies or []), *self.m, *self.v, *(self.m_scale or []), *(self.v_scale or []))
+        held = [*self.params, *(self.copies or []), *self.m, *self.v, *(self.m_scale or []), *(self.v_scale or [])]
+        _here(*held)
+        self._memory += [t.untyped_storage() for t in held if t is not None]
         _check(lib().mrl_adamw_check(self.table, self.count, self.state_dtype), "mrl_adamw_check")
 
 

@@ -476,3 +476,24 @@ def test_copies_of_some_tensors(mrl):
         for bad in (dict(params=[a.p[0], None, a.p[2]]), dict(v=[a.v[0], None, a.v[2]])):
             with pytest.raises(TypeError, match="must hold tensors"):
                 mrl.adamw_plan(**(dict(params=a.p, grads=a.g, m=a.m, v=a.v, m_scale=a.ms, v_scale=a.vs) | bad))
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_a_plan_holds_on_to_its_memory(mrl, states):
+    """Tensors that were given other memory since, and moments replaced in the plan's lists: what the plan still writes to belongs to nobody else."""
+    n = 3 << 20                                          # (large enough for blocks of their own, which the allocator would hand out again)
+    s = Set(mrl, [n], F32, states)
+    plan = s.plan
+    lists = [x for x in (plan.params, plan.grads, plan.copies, plan.m, plan.v, plan.m_scale, plan.v_scale) if x]
+    old = [x[0].data_ptr() for x in lists]
+    for k, x in enumerate(lists):
+        if k % 2:
+            x[0].data = x[0].clone()
+        x[0] = x[0].clone()
+    del s
+    torch.cuda.synchronize()
+    others = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for size in (4 * n, 2 * n, n, n // 64) for _ in range(8)]
+    assert not {x.data_ptr() for x in others} & set(old)
+    mrl.adamw_step(plan, 1e-3, 1, norm_coef=mrl.grad_norm(plan, 1.0), seed=1)
+    torch.cuda.synchronize()
+    assert all(bool((x == 7).all()) for x in others)
