@@ -358,7 +358,7 @@ int mrl_rms_norm(const void* x /*[N,d] dev*/, const void* residual /*[N,d] dev |
                  void* out_sum /*[N,d] dev | NULL*/, void* out_y /*[N,d] dev*/, float* out_scale /*dev | NULL*/, void* stream);
 
 /* ------------------------------------------------------------------------
- * (6) Backward pass of call (5), from out_dH of call (3) as a rule.
+ * (6) Backward pass of call (5), from out_dH of call (3) as a rule; what a mask means for it is said below.
  *
  *   g = dy * weight,  r = 1 / sqrt(mean h^2 + eps),  u = h r
  *   out_dx = r (g - u mean(g u)) + d_residual      the gradient of x and of residual alike
@@ -367,8 +367,11 @@ int mrl_rms_norm(const void* x /*[N,d] dev*/, const void* residual /*[N,d] dev |
  *   h: what was normalised, out_sum or, without a residual, x.  r is taken from it again (a sum
  *   over values in registers; no statistic is kept).  d_residual [N, d], h's type, or NULL: what the residual stream
  *   brings to h from further on.  dy_dtype, h_dtype, weight_dtype, dx_dtype: MRL_F32 or MRL_BF16 each.
- *   token_mask: rows with mask 0 add nothing to out_dweight and neither dy nor h is read there; their
- *   out_dx is d_residual, or zero.
+ *   token_mask: the rows whose y was used.  In the others dy counts as zero: they add nothing to out_dweight, neither dy nor h is
+ *   read there, and their out_dx is d_residual, or zero.  This is the gradient where h = x + residual runs through every row and only
+ *   some are scored, so of call (5) WITHOUT a mask.  With one, call (5) makes h a constant zero in the other rows and the gradient there is zero: so
+ *   is out_dx without d_residual, and with one that is zero there, as out_dx of calls with the same mask is.  A d_residual from
+ *   anything else behind a masked call (5) has to be cleared in those rows first.
  *   out_dweight [d] float, or NULL to skip it; accumulate_dw = 1 adds into it.  Sums over rows have a fixed
  *   order: bit-reproducible.  The workspace is needed with out_dweight only; a smaller one is refused.
  *   N = 0 needs no pointer but out_dweight, where it is wanted: zeros, or what it held.

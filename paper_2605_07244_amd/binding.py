@@ -502,7 +502,8 @@ def rms_norm(x, weight, eps=1e-6, residual=None, token_mask=None, out_dtype=None
 def rms_norm_backward(dy, h, weight, eps=1e-6, d_residual=None, token_mask=None, dx_dtype=None, out_dweight=None, accumulate=False,
                       want_dweight=True, workspace=None):
     """mrl_rms_norm_backward: (dx [N, d] in dx_dtype (None: the type of h), dweight [d] float32 or None).  h is what rms_norm returned as h
-    or, without a residual, its x; accumulate adds into out_dweight."""
+    or, without a residual, its x; accumulate adds into out_dweight.  Rows with mask 0 are those whose y was not used: dx is d_residual there, or zero.  (Behind an
+    rms_norm that had the mask too, h does not depend on x there: d_residual must be zero in those rows, as this call's dx is without one.)"""
     if dx_dtype is None:
         dx_dtype = h.dtype
     if _native and type(h) is torch.Tensor and h.is_cuda:

@@ -474,3 +474,39 @@ def test_no_rows_without_a_weight_gradient(mrl):
         for mask in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
             dx, dw = mrl.rms_norm_backward(x, x, w, EPS, x, mask, want_dweight=False)
             assert dx.shape == (0, 16) and dx.dtype == x_type and dw is None
+
+
+def test_masked_gradient_against_differences(mrl):
+    """Differences of the forward pass, with its bound in test_gradient_against_differences: without a mask where only some rows' y are used, and of two masked
+    norms, one behind the other along the residual stream."""
+    N, d = 7, 77
+    x, r, b = (_rand((N, d), F32, k) for k in (1, 2, 3))
+    w, w2 = 1 + _rand((d,), F32, 4, 0.2), 1 + _rand((d,), F32, 5, 0.2)
+    dy, dh = _rand((N, d), F32, 6), _rand((N, d), F32, 7)
+    mask = (torch.arange(N, device="cuda") % 3 != 1).to(torch.uint8)
+    on = mask.double()[:, None]
+
+    def unmasked(x, r, w):
+        y, h, _ = mrl.rms_norm(x, w, EPS, r)
+        return float((y.double() * dy.double() * on).sum() + (h.double() * dh.double()).sum())
+
+    def masked(x, r, w):
+        y, h, _ = mrl.rms_norm(x, w, EPS, r, mask)
+        y2, _, _ = mrl.rms_norm(b, w2, EPS, h, mask)
+        return float((y.double() * dy.double()).sum() + (y2.double() * dh.double()).sum())
+    _, h, _ = mrl.rms_norm(x, w, EPS, r)
+    one = mrl.rms_norm_backward(dy, h, w, EPS, dh, mask)
+    _, h, _ = mrl.rms_norm(x, w, EPS, r, mask)
+    _, h2, _ = mrl.rms_norm(b, w2, EPS, h, mask)
+    back, _ = mrl.rms_norm_backward(dh, h2, w2, EPS, None, mask)
+    two = mrl.rms_norm_backward(dy, h, w, EPS, back, mask)
+    assert not bool(back[mask == 0].any()) and not bool(two[0][mask == 0].any())
+    for value, (dx, dw) in ((unmasked, one), (masked, two)):
+        for seed in range(3):
+            for k, grad in ((0, dx), (1, dx), (2, dw)):
+                at = [x, r, w]
+                step = 1e-2 * _rand(at[k].shape, F32, 10 + seed)
+                up, down = list(at), list(at)
+                up[k], down[k] = at[k] + step, at[k] - step
+                got = float((grad.double() * step.double()).sum())
+                assert abs((value(*up) - value(*down)) / 2 - got) <= 1e-3 * float((grad.double() * step.double()).norm() * np.sqrt(step.numel())), (value, seed, k)

@@ -229,3 +229,47 @@ def test_plans_of_no_tensors_are_refused():
                 lambda: m.adamw_plan([w], [w], m=[None]), lambda: m.adamw_plan([w], [w], m=["m"])):
         with pytest.raises(TypeError, match="must hold tensors"):
             bad()
+
+
+def _differences(value, x, step=1e-6):
+    out = np.zeros_like(x)
+    for i in np.ndindex(x.shape):
+        up, down = x.copy(), x.copy()
+        up[i] += step
+        down[i] -= step
+        out[i] = (value(up) - value(down)) / (2 * step)
+    return out
+
+
+def test_masked_backward_and_the_forwards_it_belongs_to():
+    """In 64 bits: steps of 1e-6 leave 1e-12 of third derivatives and 1e-16 / 1e-6 of rounding, both times the terms' size (10)."""
+    rng = np.random.default_rng(1)
+    N, d = 6, 5
+    x, r, w, w2 = rng.normal(size=(N, d)), rng.normal(size=(N, d)), 1 + 0.2 * rng.normal(size=d), 1 + 0.2 * rng.normal(size=d)
+    dy, dh, b = (rng.normal(size=(N, d)) for _ in range(3))
+    mask = np.array([1, 0, 1, 1, 0, 1])
+
+    # the residual stream runs through every row, the loss reads y of the scored ones
+    def unmasked(x):
+        y, h = uo.rms_norm(x, w, 1e-5, r)
+        return np.sum((y * dy)[mask == 1]) + np.sum(h * dh)
+    dx = uo.rms_norm_backward(dy, x + r, w, 1e-5, dh, mask)[0]
+    assert np.max(np.abs(_differences(unmasked, x) - dx)) < 1e-8
+
+    # two masked norms, the second one's residual stream the first one's h: the gradient that comes back along it is zero in the other rows
+    def masked(x):
+        y, h = uo.rms_norm(x, w, 1e-5, r, mask)
+        y2, _ = uo.rms_norm(b, w2, 1e-5, h, mask)
+        return np.sum(y * dy) + np.sum(y2 * dh)
+    _, h = uo.rms_norm(x, w, 1e-5, r, mask)
+    _, h2 = uo.rms_norm(b, w2, 1e-5, h, mask)
+    back = uo.rms_norm_backward(dh, h2, w2, 1e-5, None, mask)[0]
+    dx = uo.rms_norm_backward(dy, h, w, 1e-5, back, mask)[0]
+    assert not back[mask == 0].any() and not dx[mask == 0].any()
+    assert np.max(np.abs(_differences(masked, x) - dx)) < 1e-8
+    # and one that does not come from such a call is not its gradient there, until it is cleared
+    dx = uo.rms_norm_backward(dy, h, w, 1e-5, dh, mask)[0]
+    want = _differences(lambda x: np.sum(uo.rms_norm(x, w, 1e-5, r, mask)[0] * dy) + np.sum(uo.rms_norm(x, w, 1e-5, r, mask)[1] * dh), x)
+    assert np.array_equal((np.abs(want - dx) > 1e-8).any(axis=1), mask == 0)
+    dx = uo.rms_norm_backward(dy, h, w, 1e-5, dh * mask[:, None], mask)[0]
+    assert np.max(np.abs(want - dx)) < 1e-8
