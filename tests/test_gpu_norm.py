@@ -510,3 +510,63 @@ def test_masked_gradient_against_differences(mrl):
                 up[k], down[k] = at[k] + step, at[k] - step
                 got = float((grad.double() * step.double()).sum())
                 assert abs((value(*up) - value(*down)) / 2 - got) <= 1e-3 * float((grad.double() * step.double()).norm() * np.sqrt(step.numel())), (value, seed, k)
+
+
+@pytest.mark.parametrize("d", [128, 1536, 2048, 3584])
+@pytest.mark.parametrize("N", [16384, 20001])
+@pytest.mark.parametrize("types", [(BF16, BF16, BF16), (F32, F32, F32)])
+def test_backward_of_long_calls(mrl, N, d, types):
+    """Calls long enough for the most workgroups, with data in every row, against 64 bits (on the GPU): with and without d_residual, which are other counts
+    of workgroups, every row scored, and sequences of 512 slots with scored heads, a period that divides those counts.
+
+    A workgroup's register adds its rows one after the other.  The workspace holds a row of partial sums for each workgroup of a call without
+    d_residual; with one there are at least half as many.  Then at most 6 additions join lanes and waves, the rest is fp64 and one rounding; u is off by 52 U."""
+    h_type, dy_type, w_type = types
+    dy, h, w = _rand((N, d), dy_type, 1, 0.01), _rand((N, d), h_type, 2, 2.0), 1 + _rand((d,), w_type, 3, 0.2)
+    res = _rand((N, d), h_type, 4, 0.01)
+    lengths = torch.randint(0, 513, (N // 512 + 1, 1), device="cuda", generator=torch.Generator("cuda").manual_seed(5))
+    heads = (torch.arange(512, device="cuda")[None] < lengths).to(torch.uint8).reshape(-1)[:N].contiguous()
+    groups = mrl.lib().mrl_rms_norm_backward_workspace(N, d) // (4 * d)
+    for d_res in (None, res):
+        rows = -(-N // groups) * (1 if d_res is None else 2)
+        for mask in (None, heads):
+            dx, dw = mrl.rms_norm_backward(dy, h, w, EPS, d_res, mask)
+            on = torch.ones(N, 1, device="cuda", dtype=torch.float64) if mask is None else mask.double()[:, None]
+            h64, g64 = h.double() * on, dy.double() * on
+            r = 1 / torch.sqrt((h64 * h64).mean(1, keepdim=True) + EPS)
+            u, g = h64 * r, g64 * w.double()
+            want = r * (g - u * (g * u).mean(1, keepdim=True))
+            size = r * (g.abs() + u.abs() * (g * u).abs().mean(1, keepdim=True))
+            if d_res is not None:
+                want, size = want + d_res.double(), size + d_res.double().abs()
+            bound = HALF[h_type] * want.abs() + 160 * U * size + 1e-38
+            assert bool(((dx.double() - want).abs() <= bound).all()), (d_res is None, mask is None)
+            err, bound = (dw.double() - (g64 * u).sum(0)).abs(), (52 + rows + 6 + 1) * U * (g64 * u).abs().sum(0)
+            print("dweight: worst error over its bound", float((err / bound).max()))
+            assert bool((err <= bound).all()), (d_res is None, mask is None)
+            again = mrl.rms_norm_backward(dy, h, w, EPS, d_res, mask)
+            assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+
+
+def test_codes_differ_at_borders_only(mrl):
+    """8-bit codes are those of the exact quotient, but where it lies at the border of two of them: y is off by 52 U, the scale by 54 U and the quotient by
+    2 roundings.  They are the same bits again in outputs that hold something else before."""
+    for N, d, block in ((2047, 3584, 0), (1000, 700, 128)):
+        x, r, w = _rand((N, d), BF16, 1), _rand((N, d), BF16, 2, 3.0), 1 + _rand((d,), BF16, 3, 0.2)
+        y, h, s = mrl.rms_norm(x, w, EPS, r, out_dtype=E4M3, scale_block=block)
+        for fill in (0x55, 0xFF):
+            junk = [torch.full((N * d * size,), fill, dtype=torch.uint8, device="cuda") for size in (1, 2)]
+            del junk
+            again = mrl.rms_norm(x, w, EPS, r, out_dtype=E4M3, scale_block=block)
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip((y, h, s), again))
+        h64 = x.double() + r.double()
+        y64 = h64 / torch.sqrt((h64 * h64).mean(1, keepdim=True) + EPS) * w.double()
+        scale = torch.stack([part.abs().amax(1) for part in y64.split(block or d, dim=1)], dim=1) / 448
+        z = (y64 / scale.repeat_interleave(block or d, dim=1)[:, :d]).abs()
+        step = torch.exp2(torch.floor(torch.log2(z.clamp(min=2.0 ** -6))) - 3)
+        want = torch.round(z / step) * step * torch.sign(y64)
+        other = y.double() != want
+        border = (torch.abs(torch.frac(z / step) - 0.5) * step)[other]
+        print("codes off the exact ones:", int(other.sum()), "of", N * d)
+        assert bool((border <= 108 * U * z[other]).all())
+        assert bool(((y.double() - want).abs() <= step)[other].all())
