@@ -497,3 +497,31 @@ def test_a_plan_holds_on_to_its_memory(mrl, states):
     mrl.adamw_step(plan, 1e-3, 1, norm_coef=mrl.grad_norm(plan, 1.0), seed=1)
     torch.cuda.synchronize()
     assert all(bool((x == 7).all()) for x in others)
+
+
+def test_scatter_of_8_bit_moments(mrl):
+    """sqrt(v) in codes against 32 bits after 3000 steps of steady gradients: not only the mean is held, so that errors of two halves do not cancel.
+
+    Relative to r = sqrt(v), a step moves it by 5e-4 (z^2 - 1), z normal, and the block's scale moves by as much of another element; codes lie s = 1/16 to 1/8 of r
+    apart, 0.090 in the mean over the logarithm.  A value that lies f steps off a code is rounded with a variance of f s^2 at most, f s = 5e-4 |z1^2 - z2^2|, whose
+    mean is 5e-4 * 4 / pi = 6.4e-4.  A root that is off by x is pulled back by 1e-3 x a step: the variance settles at 6.4e-4 s / (2 * 1e-3) = 0.32 s, a deviation of 0.17
+    (0.20 where s is 1/8).  Held: a deviation below 0.22 and above 0.12, and 99 % of the values within 0.7, 3.5 times the larger of the two.
+    The mean moves with the variance alone, by (1.5 times) it at most: 0.05 (pulled back are squares), and by 5 / sqrt(16384) * 0.2 of chance."""
+    n = 256 * 64
+    sigma = 1e-3 * torch.exp(1.5 * _rand(n, 21))
+    g = torch.empty(n, device="cuda")
+    gen = torch.Generator("cuda").manual_seed(23)
+    plans = [mrl.adamw_plan([torch.zeros(n, device="cuda")], [g], state_dtype=t, weight_decay=0.0) for t in (F32, E4M3)]
+    for t in range(1, 3001):
+        torch.randn(n, device="cuda", generator=gen, out=g)
+        g.mul_(sigma)
+        for plan in plans:
+            mrl.adamw_step(plan, 1e-3, t, seed=31)
+    root = f64(plans[0].v[0]) ** 0.5
+    got = uo.decode(plans[1].v[0], plans[1].v_scale[0])
+    large = root > 1e-3 * np.repeat(uo.block_max(root), 256)          # (well inside the normal codes)
+    off = got[large] / root[large] - 1
+    far = np.quantile(np.abs(off), 0.99)
+    print(f"{large.sum()} values: mean {off.mean():.4f} deviation {off.std():.4f} 99 % within {far:.3f}")
+    assert large.sum() > n // 2
+    assert abs(off.mean()) <= 0.06 and 0.12 <= off.std() <= 0.22 and far <= 0.7
