@@ -17,11 +17,11 @@ namespace mrl {
 namespace {
 
 constexpr int kNormChunk = 2048;             // elements of a tensor that a workgroup takes at a time: norm, eight a thread
-constexpr int kAdamThreads = 64, kAdamChunk = kAdamThreads * 4;    // ... update, four a thread
-constexpr int kStateBlock = 256;             // elements that share a scale: a wave's four a lane
+constexpr int kAdamThreads = 64, kAdamChunk = kAdamThreads * 4;    // ... update, a wave and four a lane
+constexpr int kStateBlock = kAdamChunk;      // elements that share a scale of 8-bit states
 
 // ------------------------------------------------------------------ global norm
-constexpr int kNormTensors = 96;             // a launch: 96 * 24 bytes of arguments
+constexpr int kNormTensors = 96;             // a launch: 1.9 KB of arguments
 constexpr int kNormBlocks = 2048;            // workgroups of a launch at most, a partial sum each
 struct NormTable {
   const void* grad[kNormTensors];
@@ -229,7 +229,7 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
   for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
 }
 
-// A workgroup takes a chunk of a tensor, each wave 256 elements, which are a block of 8-bit states.  Memory bounds it: 30 bytes an element with 32-bit moments
+// A workgroup of one wave takes 256 elements of a tensor, which are a block of 8-bit states.  Memory bounds it: 30 bytes an element with 32-bit moments
 // (233 M in 1156 us, 6.06 TB/s), 18 with 8-bit ones (263 M in 770 us, 6.2 TB/s), where the hash, the roots and the quotients fit beside the loads.  Everything passes
 // the caches: nothing is read again before all the rest has gone through them (kept 1315 us, loads or stores streamed 1303 and 1311, both 1252, then in
 // workgroups of one wave and 256 elements 1161; of 128, 512 and 1024 threads 1182, 1249, 1230).
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
     r.inv_fix1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
     r.inv_root_fix2 = (float)(1.0 / sqrt(1.0 - power(a.beta2, step)));
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x, c = lane * 4;
   const int left = (int)min((int64_t)kAdamChunk, t.n - at);
   const uint32_t key = kCodes ? mix(key_of(a.seed, step, t.place_bf16 >> 1) + (uint32_t)(at >> 32)) : 0;
   float* const param = t.param + at;
@@ -262,12 +262,11 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
   float *m_scale = nullptr, *v_scale = nullptr;
   if constexpr (kCodes) { m_scale = t.m_scale + at / kStateBlock; v_scale = t.v_scale + at / kStateBlock; }
   if (left == kAdamChunk) {
-    const int block = wave, c = block * kStateBlock + lane * 4;
     Four f;
     const u32x4 pw = load_stream<4, u32x4>(param + c);
     if constexpr (kCodes) {
       const uint32_t mw = load_stream<1, uint32_t>(mc + c), vw = load_stream<1, uint32_t>(vc + c);
-      f.decode(mw, vw, m_scale[block], v_scale[block]);
+      f.decode(mw, vw, *m_scale, *v_scale);
     } else {
       const u32x4 mw = load_stream<4, u32x4>(m + c), vw = load_stream<4, u32x4>(v + c);
       as_floats(mw, f.m);
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
       f.encode(4, (uint32_t)(at + c), key, &mw, &vw, &ms, &vs);
       store_stream<1>(mc + c, mw);
       store_stream<1>(vc + c, vw);
-      if (lane == 0) { m_scale[block] = ms; v_scale[block] = vs; }
+      if (lane == 0) { *m_scale = ms; *v_scale = vs; }
     } else {
       store_stream<4>(m + c, as_words(f.m));
       store_stream<4>(v + c, as_words(f.v));
@@ -297,43 +296,40 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamTable<kCodes> a) {
     return;
   }
   // a tensor's last chunk, element by element
-  if (wave * kStateBlock < left) {
-    const int block = wave;
-    const int c = block * kStateBlock + lane * 4, some = min(max(left - c, 0), 4);
-    Four f;
-    uint32_t mw = 0, vw = 0;
+  const int some = min(max(left - c, 0), 4);
+  Four f;
+  uint32_t mw = 0, vw = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in = e < some;
-      f.p[e] = in ? param[c + e] : 0.f;
-      f.g[e] = !in ? 0.f : grad_bf16 ? bf16_low(grad16[c + e]) : grad[c + e];
-      if constexpr (kCodes) {
-        if (in) { mw |= (uint32_t)mc[c + e] << 8 * e; vw |= (uint32_t)vc[c + e] << 8 * e; }
-      } else {
-        f.m[e] = in ? m[c + e] : 0.f;
-        f.v[e] = in ? v[c + e] : 0.f;
-      }
-    }
-    if constexpr (kCodes) f.decode(mw, vw, m_scale[block], v_scale[block]);
-    f.update(r);
-    float ms, vs;
-    if constexpr (kCodes) f.encode(some, (uint32_t)(at + c), key, &mw, &vw, &ms, &vs);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (e >= some) continue;
-      param[c + e] = f.p[e];
-      if (t.copy != nullptr) copy[c + e] = (uint16_t)pack_bf16(f.p[e], 0.f);
-      if constexpr (kCodes) {
-        mc[c + e] = (uint8_t)(mw >> 8 * e);
-        vc[c + e] = (uint8_t)(vw >> 8 * e);
-      } else {
-        m[c + e] = f.m[e];
-        v[c + e] = f.v[e];
-      }
-    }
+  for (int e = 0; e < 4; ++e) {
+    const bool in = e < some;
+    f.p[e] = in ? param[c + e] : 0.f;
+    f.g[e] = !in ? 0.f : grad_bf16 ? bf16_low(grad16[c + e]) : grad[c + e];
     if constexpr (kCodes) {
-      if (lane == 0) { m_scale[block] = ms; v_scale[block] = vs; }
+      if (in) { mw |= (uint32_t)mc[c + e] << 8 * e; vw |= (uint32_t)vc[c + e] << 8 * e; }
+    } else {
+      f.m[e] = in ? m[c + e] : 0.f;
+      f.v[e] = in ? v[c + e] : 0.f;
     }
+  }
+  if constexpr (kCodes) f.decode(mw, vw, *m_scale, *v_scale);
+  f.update(r);
+  float ms, vs;
+  if constexpr (kCodes) f.encode(some, (uint32_t)(at + c), key, &mw, &vw, &ms, &vs);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= some) continue;
+    param[c + e] = f.p[e];
+    if (t.copy != nullptr) copy[c + e] = (uint16_t)pack_bf16(f.p[e], 0.f);
+    if constexpr (kCodes) {
+      mc[c + e] = (uint8_t)(mw >> 8 * e);
+      vc[c + e] = (uint8_t)(vw >> 8 * e);
+    } else {
+      m[c + e] = f.m[e];
+      v[c + e] = f.v[e];
+    }
+  }
+  if constexpr (kCodes) {
+    if (lane == 0) { *m_scale = ms; *v_scale = vs; }
   }
 }
 
