@@ -426,7 +426,8 @@ int mrl_grad_norm(const mrl_param_tensor* tensors /*host*/, int32_t count, doubl
  *      The random bits of element i of tensor j (its place in `tensors`) are
  *      mix(lo(i) ^ mix(key + hi(i))), key = mix(lo(seed) ^ mix(hi(seed) ^ mix(lo(t) ^ mix(j)))), with
  *      mix(x): x = (x ^ x >> 16) * 0x6A09E667, x = (x ^ x >> 15) * 0xBB67AE85, x ^ x >> 16 on 32 bits, lo and hi the
- *      32-bit halves; the low 16 bits serve m, the high 16 sqrt(v).  The same seed gives the same bits.
+ *      32-bit halves; the low 16 bits serve m, the high 16 sqrt(v).  The same seed gives the same bits: calls for other tensors at the same step, whose places are
+ *      the same, need a seed of their own to have bits of their own, and a captured call draws others in each replay only with step_dev.
  *      A gradient that is not finite makes its block of 8-bit moments NaN, and one whose (1 - b2) g^2 fp32 does not hold that of sqrt(v); with 32-bit
  *      moments those of its own element are no longer finite.
  *      The buffers of all tensors are updated in place and must not overlap: mrl_adamw_check says whether they do. */

@@ -656,7 +656,8 @@ def grad_norm(plan: GradPlan, max_norm: float = float("inf"), out=None):
 def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm_coef=None, seed=0, skip_nonfinite=False):
     """mrl_adamw: updates the plan's params, moments and copies in place.  step counts from 1.  lr and step are numbers or, for graphs that are
     replayed with other values, tensors of one float32 and one int64 on the GPU.  norm_coef: what grad_norm returned, whose coefficient the gradients
-    are multiplied by; skip_nonfinite leaves everything as it is where that is not finite."""
+    are multiplied by; skip_nonfinite leaves everything as it is where that is not finite.  seed and step make the roundings of 8-bit moments: plans
+    that are stepped side by side need a seed each, and a graph step as a tensor that it counts up, or every replay rounds alike."""
     if _native:
         dev = _get_device()
         r = (_HOST or _host()).adamw(plan.address, plan.count, plan.workspace, lr, step, beta1, beta2, eps, norm_coef, seed, skip_nonfinite,
