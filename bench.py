@@ -110,7 +110,7 @@ def thl_alignment_leg(mrl, synth, torch, with_cpu, B=2048, S_src=1180, S_tgt=153
     return leg
 
 
-def training_leg(mrl, torch, batch, mask, loss, out_dH, out_dW, states, reps=2):
+def training_leg(mrl, torch, batch, mask, loss, out_dH, out_dW, states, reps=3):
     """A whole training step of head and final norm around the scoring step: norm with the residual's addition, loss forward and backward on its
     output, the norm's backward pass, clipping and the AdamW update.  `loss(hidden)` is the scoring step; times are medians of HIP events."""
     N, d, V = batch["N"], batch["d"], batch["V"]
