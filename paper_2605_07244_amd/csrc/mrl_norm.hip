@@ -220,7 +220,7 @@ template <bool kHBf16, bool kDyBf16, int kT, int kNV> struct BackRow {
 // worked on, and the mask of the one behind it; the columns' sums of dy u stay in registers until the last row.  Then the rows that were
 // side by side are added in LDS, in their order, and the workgroup writes one row of partial sums.
 // Memory bounds it in long calls (80000 rows of 2048 with d_residual 229 us, 5.7 TB/s; 500000 of 128 104 us, 4.9), in short ones the latency of a workgroup's rows
-// (400 of 1536 in 5.1 us).
+// (400 of 1536 in 5.1 us; 3001 of 713 in 12.4, of which the waves' sums in LDS are a part: they go in one after the other, a column at a time, and a lane waits for each).
 // In round k the workgroups take consecutive rows, turned by k times a golden section of their number: sequences of as many slots as there are
 // workgroups, whose heads are scored and whose tails are not, would else give some of them scored rows only.
 template <bool kHBf16, bool kDyBf16, int kT, int kNV>
@@ -394,6 +394,8 @@ Shape back_shape(int d) {
   return {512, v <= 1024 ? 2 : 4};
 }
 int rows_side_by_side(const Shape& s) { return s.threads <= 64 ? 256 / s.threads : 1; }
+// Rows above 8192 columns, a workgroup's one row under way at a time: 134 M elements as rows of 4096, 8192, 12288 and 16384 in bf16 162, 164, 201 and 182 us (at 5.9 TB/s 137), with
+// d_residual 200, 199, 230 and 221 (182); float 307, 302, 304 and 317 (273).  Calls of few such rows wait for them: 300 of 16384 22 us, 2000 50 (33).
 // Workgroups: two or more rows each, and as many as cover the latencies of a row without more rows under way than the memory takes well: 80000 rows of 2048,
 // us, with 256, 512, 768, 1024 and 1280 workgroups: 351, 229, 238, 259, 282.  The partial sums of many are worth it to long calls only: rows of 4096 in
 // 512 threads, with 256 and 512 workgroups: 1000 rows 13.8 and 16.2, 4000 28.8 and 31.6, 24414 156 and 154; of 1536 in 192 threads, with 512 and 1024: 4000 rows

@@ -60,7 +60,9 @@ template <int kWaves> __device__ inline double block_sum_f64(double x, double* s
 }
 
 // A partial sum of squares for each workgroup, which takes every gridDim.x-th chunk.  A chunk that is squared and added in fp64 (exact squares of float and
-// bf16) costs less than its read: 233 M floats in 151 us, 6.2 TB/s; with 1024 and 4096 workgroups in place of 2048 163 and 154.
+// bf16) costs less than its read: 233 M floats in 151 us, 6.2 TB/s; with 1024 and 4096 workgroups in place of 2048 163 and 154.  (A kernel that only reads 4 GiB reaches
+// 5.3 - 6.3 TB/s with plain loads and 5.7 - 7.1 with streamed ones, by its number of workgroups.)  A tensor's last chunk loads element by element, behind branches: of
+// 57 small tensors, whose 164 chunks hold 57 such, 4.3 us.
 __global__ __launch_bounds__(256) void k_square_sums(NormTable a) {
   __shared__ double sh[4];
   double s = 0.0;
@@ -230,7 +232,8 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
 }
 
 // A workgroup of one wave takes 256 elements of a tensor, which are a block of 8-bit states.  Memory bounds it: 30 bytes an element with 32-bit moments
-// (233 M in 1156 us, 6.06 TB/s), 18 with 8-bit ones (263 M in 770 us, 6.2 TB/s), where the hash, the roots and the quotients fit beside the loads.  Everything passes
+// (233 M in 1140 - 1180 us from card to card, 6.0 - 6.1 TB/s), 18 with 8-bit ones (263 M in 755 - 805 us, 5.9 - 6.3 TB/s), where the hash, the roots and the quotients fit beside
+// the loads.  With the step on the device each wave computes its two corrections before its first load: 32-bit moments take no longer (1154), 8-bit ones 919 - 986.  Everything passes
 // the caches: nothing is read again before all the rest has gone through them (kept 1315 us, loads or stores streamed 1303 and 1311, both 1252, then in
 // workgroups of one wave and 256 elements 1161; of 128, 512 and 1024 threads 1182, 1249, 1230).
 template <bool kCodes>
