@@ -349,7 +349,7 @@ int mrl_thl_word_align(const float* src_logp /*[B,S_src] dev*/, const uint8_t* s
  *   those of a zero row.
  *   Any d from 1 to 16384, any alignment that the types have.  N = 0 is a no-op.  The mean square is
  *   taken in fp32: entries beyond 1e19 overflow it.
- *   out_sum may be the buffer of residual or x, out_y that of x, where the types have the same size.
+ *   out_sum may be the buffer of residual or x, out_y that of x, where the types have the same size; never both one buffer.
  *   A row's results do not depend on what other rows hold.  eps >= 1e-30.
  * ---------------------------------------------------------------------- */
 int mrl_rms_norm(const void* x /*[N,d] dev*/, const void* residual /*[N,d] dev | NULL*/, const void* weight /*[d] dev*/,

@@ -525,3 +525,40 @@ def test_scatter_of_8_bit_moments(mrl):
     print(f"{large.sum()} values: mean {off.mean():.4f} deviation {off.std():.4f} 99 % within {far:.3f}")
     assert large.sum() > n // 2
     assert abs(off.mean()) <= 0.06 and 0.12 <= off.std() <= 0.22 and far <= 0.7
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+@pytest.mark.parametrize("b1,b2", [(0.9, 0.999), (0.0, 0.0), (0.0, 0.95)])
+def test_gradients_of_both_types_in_one_plan(mrl, states, b1, b2):
+    """Tensors with float and bfloat16 gradients side by side, more of them than a word of their flags has bits; betas of zero, under which a moment is its gradient."""
+    sizes = [1 + (97 * i) % 700 for i in range(70)]
+    s = Set(mrl, sizes, F32, states)
+    s.g = [g.to(BF16) if i % 3 == 1 else g for i, g in enumerate(s.g)]
+    s.plan = mrl.adamw_plan(s.p, s.g, s.copies, s.m, s.v, s.ms, s.vs, weight_decay=0.01)
+    s.keep()
+    norm, c = uo.grad_norm(s.old["g"], 1e-3)
+    got = mrl.grad_norm(s.plan, 1e-3)
+    assert abs(float(got[0]) - norm) <= 1.001 * U * norm and abs(float(got[1]) - c) <= 1.001 * U * c
+    mrl.adamw_step(s.plan, 1e-3, 3, beta1=b1, beta2=b2, norm_coef=got, seed=6)
+    s.check(1e-3, 3, coef=float(got[1]), seed=6, b1=b1, b2=b2)
+
+
+@pytest.mark.parametrize("states", [F32, E4M3])
+def test_a_number_beside_one_from_the_device(mrl, states):
+    """Learning rate or step alone from the device, and steps below 1 there, which count as 1: the same bits as with numbers."""
+    def after(lr, step):
+        s = Set(mrl, [300, 1000], F32, states)
+        mrl.adamw_step(s.plan, lr, step, seed=9)
+        torch.cuda.synchronize()
+        return s.all()
+    lr = torch.full((1,), 1e-3, device="cuda")
+    rate = float(lr)                                     # (what the tensor holds, to the bit)
+    for step in (1, 2, 1000, (1 << 32) + 3):
+        want = after(rate, step)
+        on_device = torch.full((1,), step, dtype=torch.int64, device="cuda")
+        for got in (after(lr, step), after(rate, on_device), after(lr, on_device)):
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(want, got)), step
+    want = after(rate, 1)
+    for step in (0, -1, -(1 << 40)):
+        got = after(lr, torch.full((1,), step, dtype=torch.int64, device="cuda"))
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(want, got)), step
