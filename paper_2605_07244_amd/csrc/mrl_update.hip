@@ -232,7 +232,7 @@ __device__ inline void as_floats(u32x4 w, float (&x)[4]) {
 }
 
 // A workgroup of one wave takes 256 elements of a tensor, which are a block of 8-bit states.  Memory bounds it: 30 bytes an element with 32-bit moments
-// (233 M in 1140 - 1180 us from card to card, 6.0 - 6.1 TB/s), 18 with 8-bit ones (263 M in 755 - 805 us, 5.9 - 6.3 TB/s), where the hash, the roots and the quotients fit beside
+// (233 M in 1140 - 1180 us from card to card, 5.9 - 6.1 TB/s), 18 with 8-bit ones (263 M in 755 - 805 us, 5.9 - 6.3 TB/s), where the hash, the roots and the quotients fit beside
 // the loads.  With the step on the device each wave computes its two corrections before its first load: 32-bit moments take no longer (1154), 8-bit ones 919 - 986.  Everything passes
 // the caches: nothing is read again before all the rest has gone through them (kept 1315 us, loads or stores streamed 1303 and 1311, both 1252, then in
 // workgroups of one wave and 256 elements 1161; of 128, 512 and 1024 threads 1182, 1249, 1230).
