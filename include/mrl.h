@@ -448,6 +448,50 @@ int mrl_adamw(const mrl_param_tensor* tensors /*host*/, int32_t count, const mrl
  * (MRL_ERR_CONFIG).  Host only, once for a set of tensors: it sorts them, which takes longer than a small update. */
 int mrl_adamw_check(const mrl_param_tensor* tensors /*host*/, int32_t count, int32_t state_dtype);
 
+/* ------------------------------------------------------------------------
+ * (9) Top alternatives of given logits, with the log-probs of given tokens and the entropy: what a sampler reports
+ *     for a decoding step, and how a teacher's logits become the targets of call (10).  (Where hidden states are at hand and no
+ *     alternatives are wanted, call (1b) scores tokens without any logits in memory.)
+ *
+ *   s = logits[n, :] / temperature,  lse = log sum_v exp s_v
+ *   out_top_logp[n, j] = s[out_ids[n, j]] - lse, out_ids[n, :] the k ids of the largest logits, largest first, equal ones by the lower id
+ *   out_logp[n] = s[target_ids[n]] - lse,  out_entropy[n] = lse - sum_v p_v s_v,  out_lse[n] = lse
+ *
+ *   logits: MRL_F32 or MRL_BF16, row n from logits + n * row_stride elements on (row_stride >= V; any alignment that the type has).
+ *   k from 0 to 256, at most V.  Any of the outputs may be NULL, but not all; out_logp needs target_ids, and is 0 where an id is
+ *   outside [0, V).  token_mask [N] or NULL: rows with mask 0 are not read; their ids are -1, the other outputs 0.
+ *   -infinity is a logit like others (probability 0).  A row that holds NaN or +infinity, or nothing above -infinity, has no
+ *   distribution: its lse, log-probs and entropy are NaN; its ids are in order all the same, NaN before everything, zeros of either sign alike.
+ *   The sums have a fixed order: bit-reproducible.  temperature from 1e-4 to 1e4.  N = 0 is a no-op.
+ *   The workspace is needed where few rows are split over several workgroups each; a query of 256 means that none is.
+ * ---------------------------------------------------------------------- */
+size_t mrl_top_logprobs_workspace(int64_t N, int32_t V, int32_t k);
+int mrl_top_logprobs(const void* logits /*[N, row_stride] dev*/, int64_t row_stride, const int32_t* target_ids /*[N] dev | NULL*/,
+                     const uint8_t* token_mask /*[N] dev | NULL*/, int64_t N, int32_t V, int32_t k, int32_t dtype, float temperature,
+                     int32_t* out_ids /*[N,k] dev | NULL*/, float* out_top_logp /*[N,k] dev | NULL*/, float* out_logp /*[N] dev | NULL*/,
+                     float* out_lse /*[N] dev | NULL*/, float* out_entropy /*[N] dev | NULL*/, void* workspace /*dev*/, size_t workspace_bytes,
+                     void* stream);
+
+/* ------------------------------------------------------------------------
+ * (11), (12) Embedding lookup with a scale, and its gradient: the input end of a model whose head shares the table (accumulate = 1 adds
+ *     into the out_dW of call (3) or (10)) or has its own.
+ *
+ *   (11) out_y[n, :] = scale * table[ids[n], :]
+ *   (12) out_dtable[v, :] = (or +=) scale * sum over n with ids[n] = v of dy[n, :]
+ *
+ *   table, y, dy, dtable: MRL_F32 or MRL_BF16 each; products and sums are in fp32 and rounded once.  accumulate = 1 needs a float
+ *   out_dtable.  A token with an id outside [0, V) (-1 for none, say) or with mask 0 is none: its row of y is zero, its row of dy is not
+ *   read and adds nothing.  Any d from 1 to 2^20, any alignment that the types have; V to 2^24.  N = 0: (11) is a no-op, (12) clears the table or
+ *   leaves it.  N to 2^30 in (11), to 2^24 in (12) (more tokens: several calls, all but the first with accumulate).
+ *   (12) adds the rows of a token in the order of n, in a fixed grouping: bit-reproducible.  out_dtable must not overlap dy.
+ * ---------------------------------------------------------------------- */
+int mrl_embedding(const void* table /*[V,d] dev*/, const int32_t* ids /*[N] dev*/, const uint8_t* token_mask /*[N] dev | NULL*/, int64_t N,
+                  int32_t d, int32_t V, float scale, int32_t table_dtype, int32_t y_dtype, void* out_y /*[N,d] dev*/, void* stream);
+size_t mrl_embedding_backward_workspace(int64_t N, int32_t d, int32_t V);
+int mrl_embedding_backward(const void* dy /*[N,d] dev*/, const int32_t* ids /*[N] dev*/, const uint8_t* token_mask /*[N] dev | NULL*/, int64_t N,
+                           int32_t d, int32_t V, float scale, int32_t dy_dtype, int32_t out_dtype, int32_t accumulate, void* out_dtable /*[V,d] dev*/,
+                           void* workspace /*dev*/, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

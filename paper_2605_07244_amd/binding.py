@@ -138,6 +138,16 @@ def lib() -> ctypes.CDLL:
     L.mrl_adamw.argtypes = [POINTER(_ParamTensor), c_int32, POINTER(_AdamWConfig), c_void_p, c_void_p]
     L.mrl_adamw_check.restype = c_int
     L.mrl_adamw_check.argtypes = [POINTER(_ParamTensor), c_int32, c_int32]
+    L.mrl_top_logprobs_workspace.restype = c_size_t
+    L.mrl_top_logprobs_workspace.argtypes = [c_int64, c_int32, c_int32]
+    L.mrl_top_logprobs.restype = c_int
+    L.mrl_top_logprobs.argtypes = [c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_int32, c_float] + [c_void_p] * 6 + [c_size_t, c_void_p]
+    L.mrl_embedding.restype = c_int
+    L.mrl_embedding.argtypes = [c_void_p] * 3 + [c_int64, c_int32, c_int32, c_float, c_int32, c_int32, c_void_p, c_void_p]
+    L.mrl_embedding_backward_workspace.restype = c_size_t
+    L.mrl_embedding_backward_workspace.argtypes = [c_int64, c_int32, c_int32]
+    L.mrl_embedding_backward.restype = c_int
+    L.mrl_embedding_backward.argtypes = [c_void_p] * 3 + [c_int64, c_int32, c_int32, c_float] + [c_int32] * 3 + [c_void_p] * 2 + [c_size_t, c_void_p]
     L.mrl_diag_dw_tail_plan.restype = c_int
     L.mrl_diag_dw_tail_plan.argtypes = [c_int32, c_int32, POINTER(c_int32)]
     L.mrl_diag_gemm_cut.restype = c_int
@@ -678,3 +688,97 @@ def adamw_step(plan: AdamWPlan, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
     coef = None if norm_coef is None else _ptr(norm_coef, torch.float32, "norm_coef") + 4
     _here(norm_coef, plan.workspace)
     _check(lib().mrl_adamw(plan.table, plan.count, ctypes.byref(c), coef, _stream()), "mrl_adamw")
+
+
+def _mask(t, N):
+    if t is not None and t.numel() != N:
+        raise ValueError("token_mask must have N entries")
+    return _ptr(t, torch.uint8, "token_mask")
+
+
+def _rows(t, n, name):
+    """A tensor of one int32 for each row."""
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return _ptr(t, torch.int32, name)
+
+
+def top_logprobs(logits, k, target_ids=None, token_mask=None, temperature=1.0, want_lse=True, want_entropy=True, workspace=None):
+    """mrl_top_logprobs of logits [N, V], float32 or bfloat16, whose rows may lie apart (a slice of wider rows): dict(ids [N, k] int32, top_logp [N, k],
+    logp [N] of target_ids, lse [N], entropy [N]), with None for what is not asked for; ids and top_logp are None with k = 0."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [N, V]")
+    N, V = logits.shape
+    k = _fits(operator.index(k), 32, "k")
+    _fits(V, 32, "the vocabulary")
+    dt = _float_code(logits, "logits")
+    if not logits.is_cuda:
+        raise TypeError("logits must be a GPU torch tensor")
+    if N > 0 and V > 0 and (logits.stride(1) != 1 and V > 1 or logits.stride(0) < V and N > 1):
+        raise ValueError("logits must have rows of adjacent elements that do not overlap")
+    args = [_rows(target_ids, N, "target_ids"), _mask(token_mask, N)]
+    _here(logits, target_ids, token_mask, workspace)
+    dev, out = logits.device, torch.float32
+    r = dict(ids=torch.empty((N, k), dtype=torch.int32, device=dev) if k > 0 else None, top_logp=torch.empty((N, k), dtype=out, device=dev) if k > 0 else None,
+             logp=torch.empty(N, dtype=out, device=dev) if target_ids is not None else None, lse=torch.empty(N, dtype=out, device=dev) if want_lse else None,
+             entropy=torch.empty(N, dtype=out, device=dev) if want_entropy else None)
+    need = lib().mrl_top_logprobs_workspace(N, V, k)
+    if workspace is None and need > 256:
+        workspace = _workspace(need, dev)
+    _check(lib().mrl_top_logprobs(logits.data_ptr(), max(logits.stride(0), V) if N > 1 else V, *args, N, V, k, dt, float(temperature), _ptr(r["ids"]), _ptr(r["top_logp"]),
+                                  _ptr(r["logp"]), _ptr(r["lse"]), _ptr(r["entropy"]), _ptr(workspace, torch.uint8, "workspace"),
+                                  workspace.numel() if workspace is not None else 0, _stream()), "mrl_top_logprobs")
+    return r
+
+
+def embedding(table, ids, scale=1.0, token_mask=None, out_dtype=None, out=None):
+    """mrl_embedding: scale * table[ids], [N, d] in out_dtype (None: the type of table), of ids [N] int32.  Ids outside the table, and tokens with mask 0, give zero rows."""
+    if table.dim() != 2 or ids.dim() != 1:
+        raise ValueError("table must be [V, d] and ids [N]")
+    V, d = table.shape
+    N = ids.numel()
+    if out is None:
+        out_dtype = table.dtype if out_dtype is None else out_dtype
+        if out_dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"out_dtype must be float32 or bfloat16, got {out_dtype}")
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError(f"out must have dtype {out_dtype}, got {out.dtype}")
+    _fits(V, 32, "the vocabulary")
+    _fits(d, 32, "the number of columns")
+    _shaped(out, (N, d), "out")
+    args = [_ptr(table, name="table"), _rows(ids, N, "ids"), _mask(token_mask, N)]
+    tt = _float_code(table, "table")
+    _here(table, ids, token_mask, out)
+    if out is None:
+        out = torch.empty((N, d), dtype=out_dtype, device=table.device)
+    _check(lib().mrl_embedding(*args, N, d, V, float(scale), tt, _float_code(out, "out"), _ptr(out, name="out"), _stream()), "mrl_embedding")
+    return out
+
+
+def embedding_backward(dy, ids, V, scale=1.0, token_mask=None, out_dtype=None, out=None, accumulate=False, workspace=None):
+    """mrl_embedding_backward: the gradient [V, d] of the table of an embedding whose output's gradient is dy [N, d], in out_dtype (None: float32).  accumulate
+    adds into out (float32), the gradient of a head that shares the table, say; without it every row of out is written."""
+    if dy.dim() != 2 or ids.dim() != 1:
+        raise ValueError("dy must be [N, d] and ids [N]")
+    N, d = dy.shape
+    V = _fits(operator.index(V), 32, "V")
+    _fits(d, 32, "the number of columns")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    if out is None:
+        out_dtype = torch.float32 if out_dtype is None else out_dtype
+        if out_dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"out_dtype must be float32 or bfloat16, got {out_dtype}")
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError(f"out must have dtype {out_dtype}, got {out.dtype}")
+    _shaped(out, (V, d), "out")
+    args = [_ptr(dy, name="dy"), _rows(ids, N, "ids"), _mask(token_mask, N)]
+    yt = _float_code(dy, "dy")
+    _here(dy, ids, token_mask, out, workspace)
+    if out is None:
+        out = torch.empty((max(V, 0), d), dtype=out_dtype, device=dy.device)
+    if workspace is None:
+        workspace = _workspace(lib().mrl_embedding_backward_workspace(N, d, V), dy.device)
+    _check(lib().mrl_embedding_backward(*args, N, d, V, float(scale), yt, _float_code(out, "out"), int(bool(accumulate)), _ptr(out, name="out"),
+                                        _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "mrl_embedding_backward")
+    return out

@@ -1,0 +1,431 @@
+// Top alternatives of given logits, with the log-probs of given tokens and the entropy.  Row n of [N, V], s2 = log2(e) / T:
+//   u_v = z_v s2 - m s2,  S = sum 2^u,  E = sum 2^u u     (m: the largest logit met; all in the log2 domain)
+//   lse = (m s2 + log2 S) ln 2,  entropy = (log2 S - E / S) ln 2,  log-prob = z / T - lse
+//   alternatives: the k largest by (logit, then the lower id first), exactly those
+// One pass over the logits, which are read once.  The alternatives come out of the same pass: the k-th largest of the threads'
+// running maxima is a lower bound of the k-th largest logit (each maximum is another element), so a thread looks at its tile's elements one by one
+// only where their maximum reaches that bound, and what reaches it goes to a list in LDS.  With random logits the list gets about
+// k (1 + log2(tiles)) entries; where it overflows (sorted or constant rows), and for rows with NaN, the workgroup selects by digits of the whole
+// key instead, in at most six further passes.
+// Few rows are split over several workgroups each, whose lists and sums a second launch joins.
+#include "../../include/mrl.h"
+#include "mrl_internal.h"
+#include "mrl_vec.h"
+
+namespace mrl {
+namespace {
+
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kPer = 16;                               // logits of a thread in a tile
+constexpr int kTileLogits = kThreads * kPer;
+constexpr int kMostTop = 256;                          // alternatives of a call at most (the bound needs as many threads)
+constexpr int kKeys = 4096;                            // entries of the list
+constexpr int kMostSplit = 256;
+constexpr int kIdBits = 24;                            // V <= 2^24
+constexpr uint64_t kIdMask = ((uint64_t)1 << kIdBits) - 1;
+constexpr float kNone = -1e30f;                        // the running maximum of no logits: finite, and so is its product with s2
+constexpr float kLeastU = -200.f;                      // 2^u is 0 there; u itself must not be infinite in the product 2^u u
+constexpr double LN2 = 0.6931471805599453;
+
+struct Part { float m2, S, E; };
+struct TopArgs {
+  const void* z; int64_t ld; const int32_t* targets; const uint8_t* mask;
+  int64_t N; int V, k, split, slice;
+  float s2; double inv_T;
+  int32_t* ids; float* top; float* logp; float* lse; float* entropy;
+  Part* parts; uint64_t* keys;                         // [N][split], [N][split][k]
+};
+
+// Order of the logits as whole numbers: NaN above everything, zeros of either sign alike, no number is 0.
+__device__ inline uint32_t ordered(float z) {
+  const uint32_t b = __float_as_uint(z + 0.f);
+  return z != z ? ~0u : b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ inline float from_ordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ inline uint64_t key_of(float z, int id) { return (uint64_t)ordered(z) << kIdBits | (kIdMask - (uint64_t)id); }
+__device__ inline int id_of(uint64_t key) { return (int)(kIdMask - (key & kIdMask)); }
+__device__ inline float logit_of(uint64_t key) { return from_ordered((uint32_t)(key >> kIdBits)); }
+
+template <bool kBf16> __device__ inline float logit_at(const void* row, int v) {
+  return kBf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(row)[v] << 16) : static_cast<const float*>(row)[v];
+}
+
+// What a thread looks at of a tile: vectors of 16 bytes, kThreads apart.  Behind `end` it finds -infinity.
+template <bool kBf16> struct Tile {
+  static constexpr int kVec = kBf16 ? 8 : 4, kLoads = kPer / kVec;
+  u32x4 w[kLoads];
+  __device__ static int id(int at, int i) { return at + (i / kVec * kThreads + (int)threadIdx.x) * kVec + i % kVec; }
+  __device__ void load(const void* row, int at, int end) {
+    constexpr int kSize = kBf16 ? 2 : 4;
+    if (at + kTileLogits <= end) {
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) w[j] = load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)id(at, j * kVec) * kSize);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const int v = id(at, j * kVec);
+      if (v + kVec <= end) {
+        w[j] = load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)v * kSize);
+      } else {
+        const uint32_t none = kBf16 ? 0xff80ff80u : 0xff800000u;
+        w[j] = u32x4{none, none, none, none};
+#pragma unroll
+        for (int e = 0; e < kVec - 1; ++e)
+          if (v + e < end) {
+            if (kBf16) {
+              const uint32_t b = static_cast<const uint16_t*>(row)[v + e];
+              w[j][e >> 1] = e & 1 ? (w[j][e >> 1] & 0xffffu) | b << 16 : (w[j][e >> 1] & 0xffff0000u) | b;
+            } else {
+              w[j][e] = static_cast<const uint32_t*>(row)[v + e];
+            }
+          }
+      }
+    }
+  }
+  __device__ float operator[](int i) const {
+    if (kBf16) return i & 1 ? bf16_high(w[i / 8][i % 8 / 2]) : bf16_low(w[i / 8][i % 8 / 2]);
+    return __uint_as_float(w[i / 4][i % 4]);
+  }
+};
+
+struct Shared {
+  uint64_t keys[kKeys];
+  uint64_t best[kMostTop];
+  uint32_t maxima[kThreads];
+  float wave[kWaves][4];
+  uint32_t scan[kWaves];
+  uint32_t count, bound, digit, above, inside;
+};
+
+// A lower bound of the k-th largest of the threads' numbers sh.maxima, exact in its upper kBoundBits bits, by bisection in the first wave.  0: fewer than k
+// are above 0.  Ends with a barrier.
+constexpr int kBoundBits = 20;
+__device__ inline void find_bound(Shared& sh, int k) {
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    uint32_t m[kWaves], t = 0;
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) m[j] = sh.maxima[j * 64 + threadIdx.x];
+    for (int bit = 31; bit > 31 - kBoundBits; --bit) {
+      const uint32_t c = t | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < kWaves; ++j) n += __popcll(__ballot(m[j] >= c));
+      if (n >= k) t = c;
+    }
+    if (threadIdx.x == 0) sh.bound = t;
+  }
+  __syncthreads();
+}
+
+// The k largest of the sh.count keys of the list, largest first, to sh.best (zeros where there are fewer).
+__device__ inline void sort_best(Shared& sh, int k) {
+  __syncthreads();
+  int n = (int)sh.count;
+  if (n > kThreads) {
+    // fewer of them: those that reach the k-th largest of the threads' maxima
+    uint64_t own[kKeys / kThreads];
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < kKeys / kThreads; ++j) {
+      const int i = j * kThreads + threadIdx.x;
+      own[j] = i < n ? sh.keys[i] : 0;
+      most = larger(most, (uint32_t)(own[j] >> kIdBits));
+    }
+    sh.maxima[threadIdx.x] = most;
+    find_bound(sh, k);                                 // (its first barrier: all keys have been read)
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    const uint32_t bound = sh.bound;
+#pragma unroll
+    for (int j = 0; j < kKeys / kThreads; ++j)
+      if (own[j] != 0 && (uint32_t)(own[j] >> kIdBits) >= bound) sh.keys[atomicAdd(&sh.count, 1u)] = own[j];
+    __syncthreads();
+    n = (int)sh.count;
+  }
+  for (int i = threadIdx.x; i < kMostTop; i += kThreads) sh.best[i] = 0;
+  __syncthreads();
+  // a key's place is the number of larger ones: no two are alike
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t key = sh.keys[i];
+    int place = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) place += sh.keys[j] > key;
+    if (place < k) sh.best[place] = key;
+  }
+  __syncthreads();
+}
+
+// The list by digits of the whole key, whatever the logits are: at most kKeys entries, the k largest of logits begin .. end - 1 among them.
+template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const void* row, int begin, int end, int k) {
+  constexpr int kDigits = 5;
+  constexpr int kShift[kDigits] = {44, 32, 24, 12, 0}, kBits[kDigits] = {12, 12, 8, 12, 12};
+  uint32_t* const hist = reinterpret_cast<uint32_t*>(sh.keys);
+  uint64_t prefix = 0;
+  uint32_t above = 0;                                  // keys above the prefix: fewer than k
+  int level = 0;
+  for (;; ++level) {
+    const int shift = kShift[level], bits = kBits[level];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4096; i += kThreads) hist[i] = 0;
+    __syncthreads();
+    for (int v = begin + threadIdx.x; v < end; v += kThreads) {
+      const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
+      if (key >> (shift + bits) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
+    }
+    __syncthreads();
+    // from the highest digit down, eight to a thread: the one that holds the (k - above)-th key
+    const int first = 4096 - 8 * (int)(threadIdx.x + 1);
+    uint32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += hist[first + i];
+    uint32_t incl = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const uint32_t up = __shfl_up(incl, off);
+      if ((int)(threadIdx.x & 63) >= off) incl += up;
+    }
+    if ((threadIdx.x & 63) == 63) sh.scan[threadIdx.x >> 6] = incl;
+    __syncthreads();
+    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) incl += sh.scan[w];
+    const uint32_t need = (uint32_t)k - above;
+    if (incl - sum < need && need <= incl) {
+      uint32_t run = incl - sum;
+      int i = 7;
+      while (run + hist[first + i] < need) { run += hist[first + i]; --i; }
+      sh.digit = first + i; sh.above = run; sh.inside = hist[first + i];
+    }
+    __syncthreads();
+    prefix = prefix << bits | sh.digit;
+    above += sh.above;
+    if (above + sh.inside <= (uint32_t)kKeys) break;   // (behind the last digit a single key is inside)
+  }
+  const uint64_t least = prefix << kShift[level];
+  __syncthreads();
+  if (threadIdx.x == 0) sh.count = 0;
+  __syncthreads();
+  for (int v = begin + threadIdx.x; v < end; v += kThreads) {
+    const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
+    if (key >= least) sh.keys[atomicAdd(&sh.count, 1u)] = key;
+  }
+  __syncthreads();
+}
+
+// Two partial sums as one.  (A part without logits has S = 0 and the least m2.)
+__device__ inline Part join(const Part& a, const Part& b) {
+  const float m2 = fmaxf(a.m2, b.m2), da = a.m2 - m2, db = b.m2 - m2;
+  const float ca = __builtin_amdgcn_exp2f(da), cb = __builtin_amdgcn_exp2f(db);
+  return {m2, ca * a.S + cb * b.S, ca * fmaf(a.S, da, a.E) + cb * fmaf(b.S, db, b.E)};
+}
+// All threads' as one, in a fixed order; known to all.
+__device__ inline Part join_all(Shared& sh, Part p) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const Part o = {__shfl_xor(p.m2, off), __shfl_xor(p.S, off), __shfl_xor(p.E, off)};
+    p = threadIdx.x & off ? join(o, p) : join(p, o);
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) { float* w = sh.wave[threadIdx.x >> 6]; w[0] = p.m2; w[1] = p.S; w[2] = p.E; }
+  __syncthreads();
+  p = {sh.wave[0][0], sh.wave[0][1], sh.wave[0][2]};
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) p = join(p, {sh.wave[w][0], sh.wave[w][1], sh.wave[w][2]});
+  return p;
+}
+
+// Sums of a row that the pass has none for: its largest logit is NaN, infinite, or so low that m s2 is not finite.  Two passes, the differences to the
+// largest logit first.  S is NaN where there is no distribution.
+template <bool kBf16> __device__ inline void careful_sums(Shared& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
+  uint32_t most = 0;
+  for (int v = threadIdx.x; v < a.V; v += kThreads) most = larger(most, ordered(logit_at<kBf16>(row, v)));
+  most = lanes_max<64>(most);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.scan[threadIdx.x >> 6] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) most = larger(most, sh.scan[w]);
+  const float m = from_ordered(most);
+  offset = 0; S = __builtin_nanf(""); E = 0.f;
+  if (!(fabsf(m) < INFINITY)) return;
+  Part p = {0.f, 0.f, 0.f};
+  for (int v = threadIdx.x; v < a.V; v += kThreads) {
+    const float u = (logit_at<kBf16>(row, v) - m) * a.s2, e = __builtin_amdgcn_exp2f(u);
+    p.S += e;
+    p.E = fmaf(e, fmaxf(u, kLeastU), p.E);
+  }
+  p = join_all(sh, p);
+  offset = (double)m * (double)a.s2; S = p.S; E = p.E;
+}
+
+// A row's outputs: sums in p, the alternatives in sh.best.
+template <bool kBf16> __device__ inline void put_row(Shared& sh, const TopArgs& a, int64_t n, const Part& p) {
+  const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
+  double offset = p.m2;
+  float S = p.S, E = p.E;
+  if (!(S > 0.f && S < INFINITY)) careful_sums<kBf16>(sh, a, row, offset, S, E);
+  const double log2_S = log2((double)S), lse = (offset + log2_S) * LN2;
+  for (int i = threadIdx.x; i < a.k; i += kThreads) {
+    const uint64_t key = sh.best[i];
+    if (a.ids != nullptr) a.ids[n * a.k + i] = id_of(key);
+    if (a.top != nullptr) a.top[n * a.k + i] = (float)((double)logit_of(key) * a.inv_T - lse);
+  }
+  if (threadIdx.x == 0) {
+    if (a.lse != nullptr) a.lse[n] = (float)lse;
+    if (a.entropy != nullptr) a.entropy[n] = (float)((log2_S - (double)E / (double)S) * LN2);
+    if (a.logp != nullptr) {
+      const int y = a.targets[n];
+      a.logp[n] = y >= 0 && y < a.V ? (float)((double)logit_at<kBf16>(row, y) * a.inv_T - lse) : 0.f;
+    }
+  }
+}
+
+__device__ inline void put_masked_row(const TopArgs& a, int64_t n) {
+  for (int i = threadIdx.x; i < a.k; i += kThreads) {
+    if (a.ids != nullptr) a.ids[n * a.k + i] = -1;
+    if (a.top != nullptr) a.top[n * a.k + i] = 0.f;
+  }
+  if (threadIdx.x == 0) {
+    if (a.lse != nullptr) a.lse[n] = 0.f;
+    if (a.entropy != nullptr) a.entropy[n] = 0.f;
+    if (a.logp != nullptr) a.logp[n] = 0.f;
+  }
+}
+
+template <bool kBf16> __global__ __launch_bounds__(kThreads) void k_top(TopArgs a) {
+  __shared__ Shared sh;
+  const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, n = item / a.split;
+  if (n >= a.N) return;
+  if (a.mask != nullptr && a.mask[n] == 0) {
+    if (a.split == 1) put_masked_row(a, n);
+    return;
+  }
+  const int part = (int)(item - n * a.split), begin = part * a.slice, end = a.V - begin < a.slice ? a.V : begin + a.slice;
+  const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
+  const int k = a.k < end - begin ? a.k : end - begin;
+  if (threadIdx.x == 0) sh.count = 0;                  // (the first bound's barriers lie before its first use)
+  float m = kNone, m2 = kNone * a.s2, S = 0.f, E = 0.f, bound = 0.f;
+  Tile<kBf16> next;
+  next.load(row, begin, end);
+  int tile = 0;
+  for (int at = begin; at < end; at += kTileLogits, ++tile) {
+    const Tile<kBf16> z = next;
+    if (at + kTileLogits < end) next.load(row, at + kTileLogits, end);
+    float most = z[0];
+#pragma unroll
+    for (int i = 1; i < kPer; ++i) most = fmaxf(most, z[i]);
+    if (most > m) {
+      const float to = most * a.s2, d = m2 - to, c = __builtin_amdgcn_exp2f(d);
+      E = c * fmaf(S, d, E);
+      S = c * S;
+      m = most; m2 = to;
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const float u = fmaf(z[i], a.s2, -m2), e = __builtin_amdgcn_exp2f(u);
+      S += e;
+      E = fmaf(e, fmaxf(u, kLeastU), E);
+    }
+    if (k == 0) continue;
+    if ((tile & (tile + 1)) == 0) {                    // behind tiles 0, 1, 3, 7 ...: a higher bound
+      sh.maxima[threadIdx.x] = m > kNone ? ordered(m) : 0;
+      find_bound(sh, k);
+      bound = sh.bound == 0 ? -INFINITY : from_ordered(sh.bound);
+    }
+    if (!(most < bound)) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int v = Tile<kBf16>::id(at, i);
+        if (!(z[i] < bound) && v < end) {
+          const uint32_t place = atomicAdd(&sh.count, 1u);
+          if (place < (uint32_t)kKeys) sh.keys[place] = key_of(z[i], v);
+        }
+      }
+    }
+  }
+  const Part p = join_all(sh, {m2, S, E});
+  if (k > 0) {
+    // (a NaN is the only thing that makes S one, but for an infinite logit: the comparisons above went past it)
+    if (sh.count > (uint32_t)kKeys || p.S != p.S) collect_by_digits<kBf16>(sh, row, begin, end, k);
+    sort_best(sh, k);
+  }
+  if (a.split == 1) {
+    put_row<kBf16>(sh, a, n, p);
+    return;
+  }
+  if (threadIdx.x == 0) a.parts[item] = p;
+  for (int i = threadIdx.x; i < a.k; i += kThreads) a.keys[item * a.k + i] = sh.best[i];
+}
+
+template <bool kBf16> __global__ __launch_bounds__(kThreads) void k_top_join(TopArgs a) {
+  __shared__ Shared sh;
+  const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (n >= a.N) return;
+  if (a.mask != nullptr && a.mask[n] == 0) { put_masked_row(a, n); return; }
+  const int count = a.split * a.k;                     // (at most kKeys)
+  for (int i = threadIdx.x; i < count; i += kThreads) sh.keys[i] = a.keys[n * count + i];
+  if (threadIdx.x == 0) sh.count = (uint32_t)count;
+  const Part p = join_all(sh, (int)threadIdx.x < a.split ? a.parts[n * a.split + threadIdx.x] : Part{kNone * a.s2, 0.f, 0.f});
+  if (a.k > 0) sort_best(sh, a.k);
+  put_row<kBf16>(sh, a, n, p);
+}
+
+// Workgroups of a row: one where there are rows enough for the chip (four workgroups to a compute unit), else as many as it has room for, each with a
+// quarter of a tile or more and no more alternatives in all than the list of the join holds.
+struct Split { int split, slice; };
+Split split_of(int64_t N, int V, int k) {
+  int64_t s = N > 0 ? 1024 / N : 1;
+  if (s > kMostSplit) s = kMostSplit;
+  if (k > 0 && s > kKeys / k) s = kKeys / k;
+  const int64_t by_length = (V + kTileLogits / 4 - 1) / (kTileLogits / 4);
+  if (s > by_length) s = by_length;
+  if (s <= 1) return {1, V};
+  const int slice = (int)round_up((V + s - 1) / s, 64);
+  return {(V + slice - 1) / slice, slice};
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 30, kMostWide = 1 << 21;
+dim3 grid_of(int64_t groups) {
+  const int64_t wide = groups < kMostWide ? groups : kMostWide;
+  return dim3((unsigned)wide, (unsigned)((groups + wide - 1) / wide));
+}
+bool top_shape(int64_t N, int32_t V, int32_t k) { return N >= 0 && N <= kMostRows && V > 0 && V <= 1 << kIdBits && k >= 0 && k <= kMostTop && k <= V; }
+bool is_float_type(int32_t t) { return t == MRL_F32 || t == MRL_BF16; }
+size_t parts_bytes(int64_t N, int split) { return (size_t)round_up(N * split * (int64_t)sizeof(Part), 256); }
+
+}  // namespace
+}  // namespace mrl
+
+using namespace mrl;
+
+extern "C" size_t mrl_top_logprobs_workspace(int64_t N, int32_t V, int32_t k) {
+  if (!top_shape(N, V, k)) return 0;
+  const Split s = split_of(N, V, k);
+  return s.split == 1 ? 256 : parts_bytes(N, s.split) + (size_t)round_up(N * s.split * k * 8, 256);
+}
+
+extern "C" int mrl_top_logprobs(const void* logits, int64_t row_stride, const int32_t* target_ids, const uint8_t* token_mask, int64_t N, int32_t V,
+                                int32_t k, int32_t dtype, float temperature, int32_t* out_ids, float* out_top_logp, float* out_logp, float* out_lse,
+                                float* out_entropy, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!is_float_type(dtype)) return MRL_ERR_DTYPE;
+  if (!top_shape(N, V, k) || row_stride < V || row_stride > ((int64_t)1 << 40)) return MRL_ERR_SHAPE;
+  if (!(temperature >= 1e-4f && temperature <= 1e4f)) return MRL_ERR_CONFIG;
+  if (N == 0) return MRL_OK;
+  if (!logits || (k > 0 && !out_ids && !out_top_logp) || (out_logp && !target_ids) || (k == 0 && !out_logp && !out_lse && !out_entropy)) return MRL_ERR_NULL;
+  const Split s = split_of(N, V, k);
+  if (s.split > 1 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < mrl_top_logprobs_workspace(N, V, k)))
+    return MRL_ERR_WORKSPACE;
+  const int rc = require_gfx950();
+  if (rc != MRL_OK) return rc;
+  TopArgs a = {logits, row_stride, target_ids, token_mask, N, V, k, s.split, s.slice, (float)(1.4426950408889634 / (double)temperature), 1.0 / (double)temperature,
+               out_ids, out_top_logp, out_logp, out_lse, out_entropy, nullptr, nullptr};
+  if (s.split > 1) {
+    a.parts = static_cast<Part*>(workspace);
+    a.keys = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(workspace) + parts_bytes(N, s.split));
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto go = [&](auto kernel, int64_t groups) { hipLaunchKernelGGL(kernel, grid_of(groups), dim3(kThreads), 0, st, a); };
+  if (dtype == MRL_BF16) go(k_top<true>, N * s.split); else go(k_top<false>, N * s.split);
+  if (s.split > 1) { if (dtype == MRL_BF16) go(k_top_join<true>, N); else go(k_top_join<false>, N); }
+  return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
+}
