@@ -473,6 +473,54 @@ int mrl_top_logprobs(const void* logits /*[N, row_stride] dev*/, int64_t row_str
                      void* stream);
 
 /* ------------------------------------------------------------------------
+ * (10) Distillation from a teacher's top log-probs through the head, forward and backward: what call (3) is for rewards, with the
+ *     same products.  Row n has k alternatives with ids teacher_ids[n, j] and log-probs teacher_logp[n, j], those of call (9) as a rule.
+ *
+ *   q_j = exp teacher_logp[n, j], divided by their sum with renormalize = 1 (any logits do then);   m = sum_j q_j
+ *   z = hidden[n, :] lm_head_w^T,   p = softmax(z / T)
+ *   out_kl[n] = sum_j q_j (log q_j - log p[teacher_ids[n, j]])
+ *   loss_total = T^2 sum_n w_n out_kl[n],  w_n = row_weight[n], or 1 / (rows that count) where row_weight is NULL
+ *   dz[n, v] = w_n T (m p_v - sum of the q_j whose id is v),   out_dH = dz W,  out_dW (+)= dz^T H
+ *
+ * The N x V logits are never written to memory on the bf16 path, but for a pass of their exponentials in 16 bits as in call (3).
+ * The temperature T (0.01 to 100) divides the student's logits; the teacher's log-probs are given at it.
+ * An id outside [0, V) is no alternative (-1 for lists of different lengths; those at or above V are counted).  An id may be listed several times: the gradient
+ * has the sum of its probabilities, the divergence a term for each.  A log-prob of -infinity is a probability of 0.
+ * A row counts where its mask is not 0 (token_mask NULL: every row) and its alternatives' mass is above 0 (renormalize = 0: at least 1e-30); the others have
+ * out_kl and out_dH of zero and add nothing; those with mask 0 are not read.  NaN in a row that counts makes its outputs NaN, and out_dW.
+ * Numerical range (bf16 path): a row whose most likely alternative has a log-prob below about -97 with the student reports a divergence that may be too small, is left
+ * out of the loss and the gradients and counted in n_saturated_rows.
+ * dtype, d and V as in call (3).  dh_dtype, dw_dtype: types of the gradients; MRL_BF16 with bf16 inputs only, dw_dtype MRL_BF16 only
+ * without accumulate_dw (passes are added in fp32 and rounded once).  Either gradient may be NULL; without both the call scores only.
+ * k from 1 to 256; N from 1.  Bit-reproducible from run to run; no host synchronisation.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  float temperature;
+  int32_t renormalize;    /* 0 or 1 */
+  int32_t accumulate_dw;  /* 0 = overwrite out_dW, 1 = add into it */
+  int32_t dh_dtype;       /* mrl_dtype of out_dH */
+  int32_t dw_dtype;       /* mrl_dtype of out_dW */
+  int32_t chunk_rows;     /* 0 = automatic; else rows per pass (multiple of 256) */
+} mrl_distill_config;
+
+typedef struct {
+  double loss_total;
+  int64_t n_scored_rows;     /* rows that count                                                    */
+  int64_t n_empty_rows;      /* rows whose mask is not 0 but that have no alternative with any mass */
+  int64_t n_saturated_rows;  /* see "Numerical range" above                                        */
+  int64_t n_bad_ids;         /* alternatives of rows that count whose id is V or more              */
+} mrl_distill_stats;
+
+/* (A smaller workspace than the query's may do as well, as in call (3).) */
+size_t mrl_distill_loss_workspace(int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype, const mrl_distill_config* cfg);
+int mrl_distill_loss_fwd_bwd(const void* hidden /*[N,d] dev*/, const void* lm_head_w /*[V,d] dev*/, const int32_t* teacher_ids /*[N,k] dev*/,
+                             const float* teacher_logp /*[N,k] dev*/, const uint8_t* token_mask /*[N] dev | NULL*/,
+                             const float* row_weight /*[N] dev | NULL*/, int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype,
+                             const mrl_distill_config* cfg /*host*/, float* out_kl /*[N] dev*/, void* out_dH /*[N,d] dev | NULL*/,
+                             void* out_dW /*[V,d] dev | NULL*/, mrl_distill_stats* out_stats /*dev*/, void* workspace /*dev*/,
+                             size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * (11), (12) Embedding lookup with a scale, and its gradient: the input end of a model whose head shares the table (accumulate = 1 adds
  *     into the out_dW of call (3) or (10)) or has its own.
  *

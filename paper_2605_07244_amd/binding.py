@@ -44,6 +44,11 @@ class _LossConfig(ctypes.Structure):
                 ("ratio_level", c_int32), ("debug_sync", c_int32)]
 
 
+class _DistillConfig(ctypes.Structure):
+    _fields_ = [("temperature", c_float), ("renormalize", c_int32), ("accumulate_dw", c_int32), ("dh_dtype", c_int32), ("dw_dtype", c_int32),
+                ("chunk_rows", c_int32)]
+
+
 class _ParamTensor(ctypes.Structure):
     _fields_ = [("param", c_void_p), ("copy", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p),
                 ("v_scale", c_void_p), ("n", c_int64), ("weight_decay", c_float), ("grad_dtype", c_int32)]
@@ -74,6 +79,21 @@ class LossConfig:
                            self.scored_rows_hint, self.ratio_level, self.debug_sync)
 
 
+@dataclass
+class DistillConfig:
+    temperature: float = 1.0
+    renormalize: int = 1
+    accumulate_dw: int = 0
+    dh_dtype: int = BF16
+    dw_dtype: int = F32
+    chunk_rows: int = 0
+
+    def to_c(self) -> _DistillConfig:
+        return _DistillConfig(self.temperature, int(self.renormalize), int(self.accumulate_dw), self.dh_dtype, self.dw_dtype, self.chunk_rows)
+
+
+DISTILL_STATS_FIELDS = ("loss_total", "n_scored_rows", "n_empty_rows", "n_saturated_rows", "n_bad_ids")
+DISTILL_STATS_BYTES = 8 + 4 * 8
 STATS_FIELDS = ("loss_total", "loss_pg", "loss_kl", "loss_sgt", "mean_ratio", "max_ratio", "mean_k3",
                 "n_scored_tokens", "n_clipped_tokens", "n_zero_grad_tokens", "n_bad_targets",
                 "n_unprocessed_rows", "n_saturated_rows")
@@ -148,6 +168,10 @@ def lib() -> ctypes.CDLL:
     L.mrl_embedding_backward_workspace.argtypes = [c_int64, c_int32, c_int32]
     L.mrl_embedding_backward.restype = c_int
     L.mrl_embedding_backward.argtypes = [c_void_p] * 3 + [c_int64, c_int32, c_int32, c_float] + [c_int32] * 3 + [c_void_p] * 2 + [c_size_t, c_void_p]
+    L.mrl_distill_loss_workspace.restype = c_size_t
+    L.mrl_distill_loss_workspace.argtypes = [c_int64] + [c_int32] * 4 + [POINTER(_DistillConfig)]
+    L.mrl_distill_loss_fwd_bwd.restype = c_int
+    L.mrl_distill_loss_fwd_bwd.argtypes = [c_void_p] * 6 + [c_int64] + [c_int32] * 4 + [POINTER(_DistillConfig)] + [c_void_p] * 5 + [c_size_t, c_void_p]
     L.mrl_diag_dw_tail_plan.restype = c_int
     L.mrl_diag_dw_tail_plan.argtypes = [c_int32, c_int32, POINTER(c_int32)]
     L.mrl_diag_gemm_cut.restype = c_int
@@ -378,6 +402,63 @@ def read_stats(stats: torch.Tensor) -> dict:
     import struct
     vals = struct.unpack("<7d6q", raw)
     return dict(zip(STATS_FIELDS, vals))
+
+
+def distill_loss_workspace(N: int, d: int, V: int, k: int, dtype: int, cfg: DistillConfig) -> int:
+    c = cfg.to_c()
+    return int(lib().mrl_distill_loss_workspace(N, d, V, k, dtype, ctypes.byref(c)))
+
+
+def distill_loss_fwd_bwd(hidden, lm_head_w, teacher_ids, teacher_logp, cfg: DistillConfig, token_mask=None, row_weight=None, out_dH=None, out_dW=None,
+                         want_dH=True, want_dW=True, workspace=None, out_kl=None, out_stats=None):
+    """mrl_distill_loss_fwd_bwd: dict(kl [N], dH, dW, stats) of hidden [N, d] and a teacher's alternatives, ids [N, k] int32 and log-probs [N, k] float32 (those of
+    top_logprobs, at cfg.temperature); `read_distill_stats` turns the device stats block into a Python dict (synchronises)."""
+    if hidden.dim() != 2 or lm_head_w.dim() != 2 or teacher_ids.dim() != 2:
+        raise ValueError("hidden must be [N, d], lm_head_w [V, d] and teacher_ids [N, k]")
+    N, d = hidden.shape
+    V, k = lm_head_w.shape[0], teacher_ids.shape[1]
+    dt = _dtype_code(hidden)
+    if lm_head_w.dtype != hidden.dtype or lm_head_w.shape[1] != d:
+        raise ValueError("lm_head_w must be [V, d] with the dtype of hidden")
+    _shaped(teacher_ids, (N, k), "teacher_ids")
+    _shaped(teacher_logp, (N, k), "teacher_logp")
+    for t, name in ((token_mask, "token_mask"), (row_weight, "row_weight"), (out_kl, "out_kl")):
+        if t is not None and t.numel() != N:
+            raise ValueError(f"{name} must have N entries")
+    types = {F32: torch.float32, BF16: torch.bfloat16}
+    if cfg.dh_dtype not in types or cfg.dw_dtype not in types:
+        raise TypeError("dh_dtype and dw_dtype must be F32 or BF16")
+    _shaped(out_dH, (N, d), "out_dH")
+    _shaped(out_dW, (V, d), "out_dW")
+    if cfg.accumulate_dw and want_dW and out_dW is None:
+        raise ValueError("accumulate_dw needs out_dW")
+    args = [_ptr(hidden, name="hidden"), _ptr(lm_head_w, name="lm_head_w"), _ptr(teacher_ids, torch.int32, "teacher_ids"),
+            _ptr(teacher_logp, torch.float32, "teacher_logp"), _ptr(token_mask, torch.uint8, "token_mask"), _ptr(row_weight, torch.float32, "row_weight")]
+    _here(hidden, lm_head_w, teacher_ids, teacher_logp, token_mask, row_weight, out_dH, out_dW, workspace, out_kl, out_stats)
+    dev = hidden.device
+    if out_kl is None:
+        out_kl = torch.empty(N, dtype=torch.float32, device=dev)
+    if out_dH is None and want_dH:
+        out_dH = torch.empty((N, d), dtype=types[cfg.dh_dtype], device=dev)
+    if out_dW is None and want_dW:
+        out_dW = torch.empty((V, d), dtype=types[cfg.dw_dtype], device=dev)
+    if out_stats is None:
+        out_stats = torch.empty(DISTILL_STATS_BYTES, dtype=torch.uint8, device=dev)
+    elif out_stats.numel() < DISTILL_STATS_BYTES:
+        raise ValueError(f"out_stats must have {DISTILL_STATS_BYTES} bytes")
+    if workspace is None:
+        workspace = _workspace(distill_loss_workspace(N, d, V, k, dt, cfg), dev)
+    c = cfg.to_c()
+    _check(lib().mrl_distill_loss_fwd_bwd(*args, N, d, V, k, dt, ctypes.byref(c), _ptr(out_kl, torch.float32, "out_kl"), _ptr(out_dH, types[cfg.dh_dtype], "out_dH"),
+                                          _ptr(out_dW, types[cfg.dw_dtype], "out_dW"), _ptr(out_stats, torch.uint8, "out_stats"),
+                                          _ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "mrl_distill_loss_fwd_bwd")
+    return dict(kl=out_kl, dH=out_dH, dW=out_dW, stats=out_stats)
+
+
+def read_distill_stats(stats: torch.Tensor) -> dict:
+    """Copies the device stats block to the host (synchronises) and decodes it."""
+    import struct
+    return dict(zip(DISTILL_STATS_FIELDS, struct.unpack("<d4q", stats.cpu().numpy().tobytes()[:DISTILL_STATS_BYTES])))
 
 
 def profile_enable(on: bool = True):

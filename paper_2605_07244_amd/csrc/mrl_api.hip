@@ -112,6 +112,7 @@ struct Layout {
   size_t tail = 0;             // bf16: partial tiles of the dH and dW launches' K-split tails
   int tail_items = 0;          // ... how many
   size_t head_bytes = 0;
+  size_t targets = 0, zk = 0, dw_sum = 0;   // distillation: targets, the alternatives' logits, and the float dW of a call of several passes whose dW is bf16
   size_t Hc = 0, Wp = 0;       // bf16: the pass's token rows, gathered and zero-padded to dp columns; zero-padded tail of W (only if dp != d)
   int dp = 0;                  // bf16: d rounded up to the 128-wide panel pairs of the GEMM kernels
   int64_t ldh = 0;             // row stride of Hc and Wp
@@ -126,8 +127,9 @@ size_t take(size_t& off, size_t bytes) {
   return at;
 }
 
+// k: alternatives per row of a distillation call (0: another call); dw_bf16: its dW is
 Layout make_layout(int64_t N, int64_t B, int d, int V, int dtype, int chunk_rows, bool loss,
-                   bool entropy = false) {
+                   bool entropy = false, int k = 0, bool dw_bf16 = false) {
   Layout L;
   const bool bf16 = dtype == MRL_BF16;
   const size_t es = bf16 ? 2 : 4;
@@ -164,7 +166,13 @@ Layout make_layout(int64_t N, int64_t B, int d, int V, int dtype, int chunk_rows
     L.lse_c = take(off, (size_t)(N + 1) * 4);
     L.g_c = take(off, (size_t)(N + 1) * 4);
     L.row_scale = bf16 ? take(off, (size_t)(N + 1) * 4) : 0;
-    L.loss_partials = take(off, (size_t)(L.epi_blocks_total + 1) * 10 * 8);
+    L.loss_partials = take(off, k == 0 ? (size_t)(L.epi_blocks_total + 1) * 10 * 8
+                                       : (size_t)(bf16 ? L.epi_blocks_total : distill_f32_blocks(N) + L.n_chunks) * kDistillSums * 8);
+    if (k > 0) {
+      L.targets = take(off, (size_t)N * 4);
+      if (bf16) L.zk = take(off, (size_t)chunk_rows * k * 4);
+      if (dw_bf16) L.dw_sum = take(off, (size_t)V * d * 4);
+    }
     L.Z = take(off, (size_t)chunk_rows * L.ldz * es);
     if (bf16) L.Ht = take(off, (size_t)dk * L.ldr * es);
     if (bf16) {
@@ -222,13 +230,13 @@ bool fits(Layout& L, size_t workspace_bytes) {
 // with rows; halving it until it fits took 2560 of 4096 slots, V = 151936, d = 4096, in the 32 MiB of the call without a workspace as 2048
 // and 512 rows: 2312 us a call, now 2219.)
 int pick_chunk(int64_t N, int64_t B, int d, int V, int dtype, int cfg_chunk, bool loss,
-               size_t workspace_bytes, Layout& L, bool entropy = false) {
+               size_t workspace_bytes, Layout& L, bool entropy = false, int k = 0, bool dw_bf16 = false) {
   if (cfg_chunk > 0) {
-    L = make_layout(N, B, d, V, dtype, cfg_chunk, loss, entropy);
+    L = make_layout(N, B, d, V, dtype, cfg_chunk, loss, entropy, k, dw_bf16);
     return fits(L, workspace_bytes) ? MRL_OK : MRL_ERR_WORKSPACE;
   }
   for (int r = default_chunk(N, dtype); r >= kTile; r -= kTile) {
-    L = make_layout(N, B, d, V, dtype, r, loss, entropy);
+    L = make_layout(N, B, d, V, dtype, r, loss, entropy, k, dw_bf16);
     if (fits(L, workspace_bytes)) return MRL_OK;
   }
   return MRL_ERR_WORKSPACE;
@@ -286,7 +294,7 @@ void prepare_call(const uint8_t* mask, const int32_t* targets, const void* W, in
 // forward of one chunk: logits tile GEMM with fused (or, in fp32, separate) log-sum-exp
 // (lse: fp32, the latter wanted)
 void forward_chunk(const void* H, const void* W, int d, int V, bool bf16, const Layout& L, void* ws,
-                   int64_t c0, bool stash, hipStream_t s, bool entropy = false, bool lse = true) {
+                   int64_t c0, bool stash, hipStream_t s, bool entropy = false, bool lse = true, float log2_scale = kLog2e) {
   const int32_t* row_index = at<int32_t>(ws, L.row_index);
   const int64_t* n_scored = at<int64_t>(ws, L.counters);
   if (bf16) {
@@ -304,7 +312,7 @@ void forward_chunk(const void* H, const void* W, int d, int V, bool bf16, const 
                            n_scored, c0 + sub, rows, V, d,
                            at<float>(ws, L.part_sum) + sub, entropy ? at<float>(ws, L.part_ez) + sub : nullptr,
                            L.chunk_rows,
-                           stash ? at<uint16_t>(ws, L.Z) + (size_t)sub * L.ldz : nullptr, L.ldz, blocks, s);
+                           stash ? at<uint16_t>(ws, L.Z) + (size_t)sub * L.ldz : nullptr, L.ldz, blocks, log2_scale, s);
     }
   } else {
     Scope sc(MRL_PROF_GEMM_FWD, s);
@@ -320,6 +328,27 @@ void forward_chunk(const void* H, const void* W, int d, int V, bool bf16, const 
       launch_row_lse_f32(at<float>(ws, L.Z), L.ldz, n_scored, c0, L.chunk_rows, V, at<float>(ws, L.part_max),
                          at<float>(ws, L.part_sum), entropy ? at<float>(ws, L.part_ez) : nullptr, s);
   }
+}
+
+// fp32 path: dH = dz W and dW (+)= dz^T H of a pass
+struct Products { GemmF32Args h, w; };
+Products f32_products(const void* H, const void* W, const int32_t* row_index, const int64_t* n_scored, void* dH, float* dW, int d, int V, const Layout& L,
+                      void* ws, int64_t c0, int overwrite) {
+  GemmF32Args h = {};
+  h.A = at<float>(ws, L.Z); h.lda = L.ldz;
+  h.B = static_cast<const float*>(W); h.ldb = d; h.b_kmajor = 1;
+  h.C = static_cast<float*>(dH); h.ldc = d; h.c_rows = row_index + c0;
+  h.M = L.chunk_rows; h.N = d; h.K = V;
+  h.n_scored = n_scored; h.chunk_start = c0; h.chunk_rows = L.chunk_rows;
+  h.m_dynamic = 1;
+  GemmF32Args w = {};
+  w.A = at<float>(ws, L.Z); w.lda = L.ldz; w.a_kmajor = 1;
+  w.B = static_cast<const float*>(H); w.ldb = d; w.b_rows = row_index + c0; w.b_kmajor = 1;
+  w.C = dW; w.ldc = d;
+  w.M = V; w.N = d; w.K = L.chunk_rows;
+  w.n_scored = n_scored; w.chunk_start = c0; w.chunk_rows = L.chunk_rows;
+  w.k_dynamic = 1; w.accumulate = !overwrite;
+  return {h, w};
 }
 
 }  // namespace
@@ -635,20 +664,7 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
                          n_scored, c0, L.chunk_rows, V, s);
     }
     if (!bf16) {
-      GemmF32Args h = {};
-      h.A = at<float>(ws, L.Z); h.lda = L.ldz;
-      h.B = static_cast<const float*>(lm_head_w); h.ldb = d; h.b_kmajor = 1;
-      h.C = static_cast<float*>(out_dH); h.ldc = d; h.c_rows = row_index + c0;
-      h.M = L.chunk_rows; h.N = d; h.K = V;
-      h.n_scored = n_scored; h.chunk_start = c0; h.chunk_rows = L.chunk_rows;
-      h.m_dynamic = 1;
-      GemmF32Args w = {};
-      w.A = at<float>(ws, L.Z); w.lda = L.ldz; w.a_kmajor = 1;
-      w.B = static_cast<const float*>(hidden); w.ldb = d; w.b_rows = row_index + c0; w.b_kmajor = 1;
-      w.C = out_dW; w.ldc = d;
-      w.M = V; w.N = d; w.K = L.chunk_rows;
-      w.n_scored = n_scored; w.chunk_start = c0; w.chunk_rows = L.chunk_rows;
-      w.k_dynamic = 1; w.accumulate = !overwrite;
+      const auto [h, w] = f32_products(hidden, lm_head_w, row_index, n_scored, out_dH, out_dW, d, V, L, ws, c0, overwrite);
       if (out_dH && out_dW && gemm_f32_pairs(h, w)) {
         Scope sc(MRL_PROF_GEMM_DH, s);                  // (one launch for both, and the end of the call, counts as dH's)
         finalized = c == n_passes - 1;
@@ -676,6 +692,117 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     Scope sc(MRL_PROF_FINAL, s);
     launch_finalize(finalize(n_partials), s);
   }
+  return last_error();
+}
+
+// --------------------------------------------------------------------------- (10)
+static int check_distill(int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype, const mrl_distill_config* c) {
+  const int rc = check_common(N, d, V, dtype);
+  if (rc != MRL_OK) return rc;
+  if (N == 0 || k <= 0 || k > kMostAlternatives) return MRL_ERR_SHAPE;
+  if (!(c->temperature >= 1e-2f && c->temperature <= 1e2f)) return MRL_ERR_CONFIG;
+  if ((c->renormalize != 0 && c->renormalize != 1) || (c->accumulate_dw != 0 && c->accumulate_dw != 1)) return MRL_ERR_CONFIG;
+  if ((c->dh_dtype != MRL_F32 && c->dh_dtype != MRL_BF16) || (c->dw_dtype != MRL_F32 && c->dw_dtype != MRL_BF16)) return MRL_ERR_CONFIG;
+  if (c->dw_dtype == MRL_BF16 && (c->accumulate_dw || dtype == MRL_F32)) return MRL_ERR_CONFIG;
+  if (c->chunk_rows < 0 || c->chunk_rows % kTile != 0 || c->chunk_rows > (1 << 20)) return MRL_ERR_CONFIG;
+  return MRL_OK;
+}
+
+size_t mrl_distill_loss_workspace(int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype, const mrl_distill_config* cfg) {
+  if (cfg == nullptr || check_distill(N, d, V, k, dtype, cfg) != MRL_OK) return 0;
+  return make_layout(N, 0, d, V, dtype, cfg->chunk_rows > 0 ? cfg->chunk_rows : default_chunk(N, dtype), true, false, k, cfg->dw_dtype == MRL_BF16).total;
+}
+
+int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32_t* teacher_ids, const float* teacher_logp,
+                             const uint8_t* token_mask, const float* row_weight, int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype,
+                             const mrl_distill_config* cfg, float* out_kl, void* out_dH, void* out_dW, mrl_distill_stats* out_stats,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  if (!hidden || !lm_head_w || !teacher_ids || !teacher_logp || !cfg || !out_kl || !out_stats) return MRL_ERR_NULL;
+  int rc = check_distill(N, d, V, k, dtype, cfg);
+  if (rc != MRL_OK) return rc;
+  if (dtype == MRL_F32 && out_dH && cfg->dh_dtype != MRL_F32) return MRL_ERR_CONFIG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MRL_ERR_WORKSPACE;
+  const bool dw_bf16 = cfg->dw_dtype == MRL_BF16;
+  Layout L;
+  rc = pick_chunk(N, 0, d, V, dtype, cfg->chunk_rows, true, workspace_bytes, L, false, k, dw_bf16);
+  if (rc != MRL_OK) return rc;
+  rc = check_device();
+  if (rc != MRL_OK) return rc;
+
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool bf16 = dtype == MRL_BF16, bwd = out_dH != nullptr || out_dW != nullptr;
+  void* ws = workspace;
+  int32_t *const row_index = at<int32_t>(ws, L.row_index), *const targets = at<int32_t>(ws, L.targets);
+  int64_t* const n_scored = at<int64_t>(ws, L.counters);
+  DistillArgs a = {};
+  a.ids = teacher_ids; a.logp = teacher_logp; a.k = k; a.mask = token_mask; a.weight = row_weight;
+  a.N = N; a.d = d; a.V = V; a.renormalize = cfg->renormalize;
+  a.H = hidden; a.W = lm_head_w;
+  a.scale2 = (float)(1.4426950408889634 / (double)cfg->temperature); a.temperature = cfg->temperature;
+  a.targets = targets; a.row_index = row_index; a.n_scored = n_scored; a.chunk_rows = L.chunk_rows;
+  a.zt = at<float>(ws, L.zt); a.zk = at<float>(ws, L.zk);
+  a.part_sum = at<float>(ws, L.part_sum); a.n_partials = L.n_partials;
+  if (bf16 && bwd) { a.estash = at<uint16_t>(ws, L.Z); a.lde = L.ldz; a.row_scale = at<float>(ws, L.row_scale); }
+  if (!bf16) { a.Z = at<float>(ws, L.Z); a.ldz = L.ldz; a.write_dz = bwd; }
+  a.out_kl = out_kl; a.loss_partials = at<double>(ws, L.loss_partials);
+
+  // the slots that count: those with an alternative, which stands in the target's place
+  {
+    Scope sc(MRL_PROF_PREP, s);
+    launch_distill_targets(a, s);
+  }
+  const PrepOut po = {row_index, n_scored, n_scored + 1, at<int32_t>(ws, L.block_counts), {out_kl, nullptr, nullptr}, 0, 0, nullptr};
+  prepare_call(token_mask, targets, lm_head_w, N, d, V, po, L, ws, s);
+  RowPrepArgs once = {};
+  once.prep = prep_inline(N) ? &po : nullptr;
+  once.mask = token_mask; once.N = N; once.V = V;
+  once.dH = out_dH; once.dh_row_bytes = (int64_t)d * (cfg->dh_dtype == MRL_BF16 ? 2 : 4);
+  float* const dW = dw_bf16 && out_dW ? at<float>(ws, L.dw_sum) : static_cast<float*>(out_dW);
+  for (int64_t c = 0; c < L.n_chunks; ++c) {
+    const int64_t c0 = c * L.chunk_rows;
+    const int rows = (int)(N - c0 < L.chunk_rows ? N - c0 : L.chunk_rows);      // at most
+    prepare_chunk(hidden, lm_head_w, targets, d, bf16, L, ws, c, L.n_chunks, c == 0, c == 0 ? once : RowPrepArgs{}, s);
+    a.chunk_start = c0;
+    if (bf16) {
+      Scope sc(MRL_PROF_CONVERT, s);
+      launch_distill_logits(a, s);
+    }
+    forward_chunk(hidden, lm_head_w, d, V, bf16, L, ws, c0, bwd, s, false, false, a.scale2);
+    {
+      Scope sc(MRL_PROF_ROW_EPI, s);
+      if (bf16) launch_distill_rows(a, s); else launch_distill_f32(a, rows, s);
+      a.partial_block_offset += bf16 ? row_epilogue_blocks(L.chunk_rows) : distill_f32_blocks(rows);
+    }
+    if (!bwd) continue;
+    const int overwrite = c == 0 && !cfg->accumulate_dw;
+    if (!bf16) {
+      const Products p = f32_products(hidden, lm_head_w, row_index, n_scored, out_dH, dW, d, V, L, ws, c0, overwrite);
+      if (out_dH && dW && gemm_f32_pairs(p.h, p.w)) { Scope sc(MRL_PROF_GEMM_DH, s); launch_gemm_f32_pair(p.h, p.w, nullptr, s); continue; }
+      if (out_dH) { Scope sc(MRL_PROF_GEMM_DH, s); launch_gemm_f32(p.h, s); }
+      if (dW) { Scope sc(MRL_PROF_GEMM_DW, s); launch_gemm_f32(p.w, s); }
+      continue;
+    }
+    const bool dw_blocks = dw_rows_in_blocks(rows);
+    if (dW) {
+      Scope sc(MRL_PROF_CONVERT, s);
+      launch_backward_rows_b16(at<void>(ws, L.Hc), L.ldh, a.row_scale + c0, at<void>(ws, L.Ht), L.ldr, n_scored, c0, L.chunk_rows, L.dp,
+                               at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, s);
+    }
+    if (out_dH) {
+      Scope sc(MRL_PROF_GEMM_DH, s);
+      launch_gemm_dh_bf16(at<void>(ws, L.Z), L.ldz, lm_head_w, d, V, row_index, a.row_scale, n_scored, c0, L.chunk_rows, d, out_dH,
+                          cfg->dh_dtype == MRL_F32, at<float>(ws, L.tail), L.tail_items, s);
+    }
+    if (dW) {
+      Scope sc(MRL_PROF_GEMM_DW, s);
+      launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW, overwrite,
+                          at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
+    }
+  }
+  Scope sc(MRL_PROF_FINAL, s);
+  if (dw_bf16 && out_dW) launch_to_bf16(dW, out_dW, (int64_t)V * d, s);
+  launch_distill_final(a.loss_partials, a.partial_block_offset, n_scored, n_scored + 1, (double)cfg->temperature * (double)cfg->temperature,
+                       &out_stats->loss_total, &out_stats->n_scored_rows, s);
   return last_error();
 }
 

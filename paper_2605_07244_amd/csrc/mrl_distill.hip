@@ -1,0 +1,360 @@
+// Distillation from a teacher's top log-probs: what surrounds the products of the loss.  Row n has alternatives j = 1 .. k with ids v_j and log-probs t_j,
+// q_j = exp t_j (renormalised: over their sum), m = sum q_j, p = softmax(z / T):
+//   kl = sum_j q_j (log q_j - log p[v_j])          L = T^2 sum_n w_n kl_n          dz = w T (m p - q)
+// With the forward launch's stash e = 2^(z log2(e) / T - c) and its sum S, p = e / S and
+//   dz = (w T m / S) (e - (S / m) q):  the stored row, changed at k places, times a scalar per row.
+// The offset c comes from the largest of the row's k logits, which are products of the row with k rows of the head, taken
+// before the forward launch in fp32: the divergence needs them to more bits than the stash has.
+#include "mrl_internal.h"
+#include "mrl_partials.h"
+#include "mrl_vec.h"
+
+namespace mrl {
+namespace {
+
+constexpr int kEach = kMostAlternatives / 64;          // alternatives of a lane: j = 64 i + lane
+constexpr double LN2 = 0.6931471805599453;
+constexpr double kLeastMass = 1e-30;                   // of a row that counts: S / m stays a number
+
+__device__ inline double wave_sum(double x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+  return x;
+}
+__device__ inline float wave_max(float x) {            // NaN is passed over
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+  return x;
+}
+
+// A slot's alternatives, by one wave.
+struct Alternatives {
+  int id[kEach];                                       // -1: none
+  float t[kEach];
+  double q[kEach], log_q[kEach], m;
+  bool any;                                            // the slot counts
+  __device__ void load(const DistillArgs& a, int64_t slot) {
+    const int lane = threadIdx.x & 63;
+    const int32_t* ids = a.ids + slot * a.k;
+    const float* logp = a.logp + slot * a.k;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int j = 64 * i + lane;
+      id[i] = -1;
+      t[i] = -INFINITY;
+      if (j < a.k) {
+        const int v = ids[j];
+        if (v >= 0 && v < a.V) { id[i] = v; t[i] = logp[j]; }
+      }
+    }
+  }
+  // (best: the largest t; with nothing above -infinity and no NaN, nothing counts)
+  __device__ void weigh(const DistillArgs& a, float best) {
+    const double shift = a.renormalize ? (double)best : 0.0;
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      log_q[i] = (double)t[i] - shift;
+      q[i] = id[i] >= 0 ? t[i] == -INFINITY ? 0.0 : exp(log_q[i]) : 0.0;
+      sum += q[i];
+    }
+    m = wave_sum(sum);
+    any = m != m || m >= kLeastMass;
+    if (!a.renormalize) return;
+    const double log_m = log(m), inv = 1.0 / m;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) { q[i] *= inv; log_q[i] -= log_m; }
+    m = m != m ? m : 1.0;
+  }
+  __device__ float best_t() const {
+    float b = t[0];
+#pragma unroll
+    for (int i = 1; i < kEach; ++i) b = fmaxf(b, t[i]);
+    return wave_max(b);
+  }
+  // Per alternative the probability of its id, however often that is listed, and whether this is the id's first place.
+  __device__ void by_id(int k, float (&total)[kEach], bool (&first)[kEach]) const {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) { total[i] = 0.f; first[i] = id[i] >= 0; }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int n = k - 64 * e < 64 ? k - 64 * e : 64;
+      const float mine = (float)q[e];
+      for (int l = 0; l < n; ++l) {
+        const int other = __builtin_amdgcn_readlane(id[e], l);
+        const float p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), l));
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+          if (id[i] == other && 64 * i < k) {
+            total[i] += p;
+            if (64 * e + l < 64 * i + lane) first[i] = false;
+          }
+      }
+    }
+  }
+};
+
+__device__ inline float weight_of(const DistillArgs& a, int64_t slot) {
+  return a.weight != nullptr ? a.weight[slot] : (float)(1.0 / (double)*a.n_scored);
+}
+// Ids that name no token though they are not negative.
+__device__ inline double too_large(const DistillArgs& a, int64_t slot) {
+  int n = 0;
+  for (int j = threadIdx.x & 63; j < a.k; j += 64) n += a.ids[slot * a.k + j] >= a.V;
+  return wave_sum((double)n);
+}
+
+// A wave per slot: the id of its best alternative, or -1.
+__global__ __launch_bounds__(256) void k_distill_targets(DistillArgs a) {
+  const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (n >= a.N) return;
+  int target = -1;
+  if (a.mask == nullptr || a.mask[n] != 0) {
+    Alternatives alt;
+    alt.load(a, n);
+    const float best = alt.best_t();
+    alt.weigh(a, best);
+    // the lowest lane that has it (of NaN alone: any alternative)
+#pragma unroll
+    for (int i = kEach - 1; i >= 0; --i) {
+      const unsigned long long has = __ballot(alt.id[i] >= 0 && (alt.t[i] == best || best == -INFINITY));
+      if (has != 0) target = __builtin_amdgcn_readlane(alt.id[i], __builtin_ctzll(has));
+    }
+    if (!alt.any) target = -1;
+  }
+  if ((threadIdx.x & 63) == 0) a.targets[n] = target;
+}
+
+// ----------------------------------------------------------------------------
+// bf16: the alternatives' logits.  A workgroup per row, its waves taking eight alternatives at a time, a lane eight columns.
+// ----------------------------------------------------------------------------
+constexpr int kTogether = 8;
+__global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
+  __shared__ float most[4];
+  const int64_t r = blockIdx.x;
+  if (r >= valid_rows(a.n_scored, a.chunk_start, a.chunk_rows)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t slot = a.row_index[a.chunk_start + r];
+  const u32x4* const h = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.H) + slot * a.d);
+  const int32_t* const ids = a.ids + slot * a.k;
+  const float* const logp = a.logp + slot * a.k;
+  const int vectors = a.d / 8;
+  float largest = -INFINITY;
+  for (int j0 = wave * kTogether; j0 < a.k; j0 += 4 * kTogether) {
+    const u32x4* w[kTogether];
+    bool there[kTogether];
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      const int id = j0 + i < a.k ? ids[j0 + i] : -1;
+      there[i] = id >= 0 && id < a.V;
+      w[i] = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.W) + (int64_t)(there[i] ? id : 0) * a.d);
+    }
+    float acc[kTogether] = {};
+    for (int c = lane; c < vectors; c += 64) {
+      const u32x4 u = h[c];
+      u32x4 b[kTogether];
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i) b[i] = w[i][c];
+#pragma unroll
+      for (int i = 0; i < kTogether; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[i] = fmaf(bf16_low(u[e]), bf16_low(b[i][e]), acc[i]);
+          acc[i] = fmaf(bf16_high(u[e]), bf16_high(b[i][e]), acc[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kTogether; ++i) {
+      const float z = lanes_sum<64>(acc[i]);
+      if (j0 + i >= a.k) continue;
+      if (lane == 0) a.zk[r * a.k + j0 + i] = z;
+      if (there[i] && logp[j0 + i] != -INFINITY) largest = fmaxf(largest, z);
+    }
+  }
+  if (lane == 0) most[wave] = largest;
+  __syncthreads();
+  if (threadIdx.x == 0) a.zt[a.chunk_start + r] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+}
+
+// Behind the forward launch: a block takes EPI_ROWS rows, first their sums, then a wave each row.
+__global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
+  __shared__ float4 sh[EPI_LANES][EPI_ROWS / 4];
+  __shared__ float sums[EPI_ROWS];
+  __shared__ double parts[EPI_THREADS / 64][kDistillSums];
+  const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows), r0 = blockIdx.x * EPI_ROWS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  double q[kDistillSums] = {};
+  if (r0 < nvalid) {
+    const float s = merge_partials(a.part_sum + r0, a.chunk_rows, a.n_partials, sh);
+    if (threadIdx.x < EPI_ROWS) sums[threadIdx.x] = s;
+    __syncthreads();
+    for (int i = wave; i < EPI_ROWS && r0 + i < nvalid; i += EPI_THREADS / 64) {
+      const int64_t r = r0 + i, ci = a.chunk_start + r, slot = a.row_index[ci];
+      const float S = sums[i], c2 = fmaf(a.zt[ci], a.scale2, kStashMargin2), w = weight_of(a, slot);
+      Alternatives alt;
+      alt.load(a, slot);
+      alt.weigh(a, alt.best_t());
+      const double log2_sum = (double)c2 + log2((double)S);        // of exponentials in the log2 domain, with the very c2 that the launch took
+      double kl = 0.0;
+      float z[kEach];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int j = 64 * e + lane;
+        z[e] = j < a.k ? a.zk[r * a.k + j] : 0.f;
+        if (alt.q[e] != 0.0) kl += alt.q[e] * (alt.log_q[e] - ((double)z[e] * (double)a.scale2 - log2_sum) * LN2);
+      }
+      kl = wave_sum(kl);
+      // the alternative that the student thinks most of is beyond the operands' range: not in the loss, as an empty row
+      // (NaN is not: the launches' clamps go past it, so it enters the gradients with the row's scale)
+      const bool number = fabs(kl) < (double)INFINITY;
+      const bool saturated = number && ((double)a.zt[ci] * (double)a.scale2 - log2_sum) * LN2 < (double)kSaturatedLogp;
+      if (lane == 0) a.out_kl[slot] = (float)kl;
+      if (saturated) q[1] += 1.0; else q[0] += (double)w * kl;
+      q[2] += too_large(a, slot);
+      if (a.row_scale == nullptr) continue;
+      if (lane == 0) a.row_scale[ci] = saturated ? 0.f : !number ? __builtin_nanf("") : (float)((double)w * (double)a.temperature * alt.m / (double)S);
+      if (saturated) continue;
+      float total[kEach];
+      bool first[kEach];
+      alt.by_id(a.k, total, first);
+      const float per = (float)((double)S / alt.m);
+      uint16_t* const row = a.estash + r * a.lde;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (first[e]) {
+          const float x = __builtin_amdgcn_exp2f(fminf(fmaf(z[e], a.scale2, -c2), kStashClamp2)) - per * total[e];
+          row[alt.id[e]] = (uint16_t)pack_bf16(x, 0.f);
+        }
+    }
+  }
+  if (lane == 0) {
+#pragma unroll
+    for (int k = 0; k < kDistillSums; ++k) parts[wave][k] = q[k];
+  }
+  __syncthreads();
+  if (threadIdx.x < kDistillSums) {
+    double t = 0.0;
+    for (int w = 0; w < EPI_THREADS / 64; ++w) t += parts[w][threadIdx.x];
+    a.loss_partials[(a.partial_block_offset + blockIdx.x) * kDistillSums + threadIdx.x] = t;
+  }
+}
+
+// ----------------------------------------------------------------------------
+// fp32: a wave per row of the materialised logits, which become dz.
+// ----------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
+  __shared__ double parts[4][kDistillSums];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x * 4 + wave;
+  double q[kDistillSums] = {};
+  if (r < valid_rows(a.n_scored, a.chunk_start, a.chunk_rows)) {
+    const int64_t slot = a.row_index[a.chunk_start + r];
+    float* const row = a.Z + (int64_t)r * a.ldz;
+    const float w = weight_of(a, slot), inv_T = 1.f / a.temperature;
+    float mx = -INFINITY;
+    for (int v = lane; v < a.V; v += 64) mx = fmaxf(mx, row[v]);
+    mx = wave_max(mx);
+    float s = 0.f;
+    for (int v = lane; v < a.V; v += 64) s += expf((row[v] - mx) * inv_T);
+    const float S = lanes_sum<64>(s);
+    const double log_S = log((double)S);
+    Alternatives alt;
+    alt.load(a, slot);
+    alt.weigh(a, alt.best_t());
+    double kl = 0.0;
+    float z[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      z[e] = alt.id[e] >= 0 ? row[alt.id[e]] : 0.f;
+      if (alt.q[e] != 0.0) kl += alt.q[e] * (alt.log_q[e] - (((double)z[e] - (double)mx) / (double)a.temperature - log_S));
+    }
+    kl = wave_sum(kl);
+    if (lane == 0) a.out_kl[slot] = (float)kl;
+    q[0] = (double)w * kl;
+    q[2] = too_large(a, slot);
+    if (a.write_dz) {
+      const float g = (float)((double)w * (double)a.temperature), scale = (float)((double)w * (double)a.temperature * alt.m / (double)S);
+      float total[kEach];
+      bool first[kEach];
+      alt.by_id(a.k, total, first);
+      for (int v = lane; v < a.V; v += 64) row[v] = scale * expf((row[v] - mx) * inv_T);
+      __threadfence_block();                           // (the places below are other lanes' above)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (first[e]) row[alt.id[e]] = scale * expf((z[e] - mx) * inv_T) - g * total[e];
+    }
+  }
+  if (lane == 0) {
+#pragma unroll
+    for (int k = 0; k < kDistillSums; ++k) parts[wave][k] = q[k];
+  }
+  __syncthreads();
+  if (threadIdx.x < kDistillSums)
+    a.loss_partials[(a.partial_block_offset + blockIdx.x) * kDistillSums + threadIdx.x] =
+        (parts[0][threadIdx.x] + parts[1][threadIdx.x]) + (parts[2][threadIdx.x] + parts[3][threadIdx.x]);
+}
+
+constexpr int FINAL_THREADS = 256;
+__global__ __launch_bounds__(FINAL_THREADS) void k_distill_final(const double* parts, int64_t blocks, const int64_t* n_scored, const int64_t* n_empty,
+                                                                 double scale, double* out_d, int64_t* out_i) {
+  __shared__ double sh[FINAL_THREADS / 64][kDistillSums];
+  double q[kDistillSums] = {};
+  for (int64_t b = threadIdx.x; b < blocks; b += FINAL_THREADS)
+#pragma unroll
+    for (int k = 0; k < kDistillSums; ++k) q[k] += parts[b * kDistillSums + k];
+#pragma unroll
+  for (int k = 0; k < kDistillSums; ++k) {
+    q[k] = wave_sum(q[k]);
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6][k] = q[k];
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+#pragma unroll
+  for (int k = 0; k < kDistillSums; ++k) q[k] = (sh[0][k] + sh[1][k]) + (sh[2][k] + sh[3][k]);
+  *out_d = scale * q[0];
+  out_i[0] = *n_scored;
+  out_i[1] = *n_empty;
+  out_i[2] = (int64_t)(q[1] + 0.5);
+  out_i[3] = (int64_t)(q[2] + 0.5);
+}
+
+__global__ __launch_bounds__(256) void k_to_bf16(const float* in, uint16_t* out, int64_t n) {
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; i < n; i += (int64_t)gridDim.x * 256 * 8) {
+    const u32x4 lo = load_any<4, u32x4>(in + i), hi = load_any<4, u32x4>(in + i + 4);
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      w[e] = pack_bf16(__uint_as_float(lo[2 * e]), __uint_as_float(lo[2 * e + 1]));
+      w[2 + e] = pack_bf16(__uint_as_float(hi[2 * e]), __uint_as_float(hi[2 * e + 1]));
+    }
+    store_any<2>(out + i, w);
+  }
+}
+
+}  // namespace
+
+void launch_distill_targets(const DistillArgs& a, hipStream_t stream) {
+  const int64_t blocks = (a.N + 3) / 4, wide = blocks < (1 << 21) ? blocks : 1 << 21;
+  hipLaunchKernelGGL(k_distill_targets, dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide)), dim3(256), 0, stream, a);
+}
+void launch_distill_logits(const DistillArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_distill_logits, dim3(a.chunk_rows), dim3(256), 0, stream, a);
+}
+void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_distill_rows, dim3((a.chunk_rows + EPI_ROWS - 1) / EPI_ROWS), dim3(EPI_THREADS), 0, stream, a);
+}
+int distill_f32_blocks(int64_t rows) { return (int)((rows + 3) / 4); }
+void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream) {
+  hipLaunchKernelGGL(k_distill_f32, dim3(distill_f32_blocks(rows)), dim3(256), 0, stream, a);
+}
+void launch_distill_final(const double* parts, int64_t blocks, const int64_t* n_scored, const int64_t* n_empty, double scale, double* out_d, int64_t* out_i,
+                          hipStream_t stream) {
+  hipLaunchKernelGGL(k_distill_final, dim3(1), dim3(FINAL_THREADS), 0, stream, parts, blocks, n_scored, n_empty, scale, out_d, out_i);
+}
+void launch_to_bf16(const float* in, void* out, int64_t n, hipStream_t stream) {
+  const int64_t blocks = (n / 8 + 255) / 256;
+  hipLaunchKernelGGL(k_to_bf16, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, stream, in, static_cast<uint16_t*>(out), n);
+}
+
+}  // namespace mrl

@@ -70,7 +70,7 @@ struct Params {
   // FWD; a_tail_panel: the 64-wide panel from which A comes from its zero-padded tail copy, a_tail_delta
   // bytes behind where it would be
   int a_tail_panel; int64_t a_tail_delta;
-  const float* zt; float* part_sum; float* part_ez; int64_t part_stride; uint16_t* estash; int64_t lde; int V;
+  float log2_scale; const float* zt; float* part_sum; float* part_ez; int64_t part_stride; uint16_t* estash; int64_t lde; int V;
   uint64_t cuts[4];           // FWD, DH: how the token rows are cut into tiles, two bits per 128 of them (see Cut)
   // DH
   const float* row_scale; void* dH; int dh_f32; int d; int max_items;   // max_items: partial tiles tail_part holds
@@ -278,7 +278,7 @@ __device__ __forceinline__ void forward_epilogue(const Params& p, Acc read_acc, 
       // vocabulary tiles of a row: e = 2^(z log2(e) - c2), clamped so that neither e nor any sum of
       // it can overflow.  The sums over the wave's 128 vocabulary ids are this tile's partials; e
       // itself, as bf16, is the backward pass's operand (dz = (-g / S)(e - S onehot)).
-      constexpr float LOG2E = 1.4426950408889634f;
+      const float LOG2E = p.log2_scale;               // (log2(e) over the temperature)
       const bool full = (v0 + 128 <= p.V);
           // vocabulary id of accumulator (i, e) of this lane
       auto vrow = [&](int i, int e) {
@@ -1824,8 +1824,9 @@ DwPlan plan_dw(int chunk_rows, int expected_rows, int V, int d, int max_items) {
 void launch_gemm_fwd_bf16(const void* W, int64_t ldw, const void* W_tail, const void* Hc, int64_t ldh, int k_len, const float* zt,
                           const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                           int V, int d, float* part_sum, float* part_ez,
-                          int64_t part_stride, void* estash, int64_t lde, bool in_blocks, hipStream_t stream) {
+                          int64_t part_stride, void* estash, int64_t lde, bool in_blocks, float log2_scale, hipStream_t stream) {
   Params p = {};
+  p.log2_scale = log2_scale;
   p.A = static_cast<const uint16_t*>(W); p.lda = ldw; p.M = V;
   p.B = static_cast<const uint16_t*>(Hc); p.ldb = ldh; p.N = chunk_rows;
   p.K = k_len;

@@ -52,12 +52,13 @@ inline int fwd_partials_bf16(int V) { return 2 * (int)((V + kTile - 1) / kTile);
 constexpr float kStashMargin2 = 60.f;
 constexpr float kStashClamp2 = 100.f;
 constexpr float kSaturatedLogp = -97.f;
+constexpr float kLog2e = 1.4426950408889634f;      // (the forward kernel takes it divided by the temperature, and c2 with it)
 
 // ---- bf16 MFMA GEMM family: C[m][n] = sum_k A[m][k] * B[n][k] ---------------
 // n_scored: device pointer to the number of compacted rows; chunk_start/chunk_rows
 // select the rows this launch covers (valid rows = clamp(n_scored - chunk_start, 0, chunk_rows)).
 
-// Forward: A = W [V, k_len] (row stride ldw), B = Hc [chunk_rows, k_len] (row stride ldh, or, in_blocks, in
+// Forward (log2_scale: log2(e) over the temperature, in the place of log2(e) above): A = W [V, k_len] (row stride ldw), B = Hc [chunk_rows, k_len] (row stride ldh, or, in_blocks, in
 // blocks of kRowBlock columns of ldh rows each): the launch's token rows, gathered; k_len = d rounded up to 128, the columns beyond d
 // zero in both operands; zt[chunk_start + n] is the row's target logit.  Writes per-row partials part_sum[(2*tile_m + wave_m) * part_stride + n]
 // = sum of e[n, v] over the partial's 128 vocabulary rows (e as defined above), when part_ez != nullptr
@@ -68,7 +69,7 @@ constexpr float kSaturatedLogp = -97.f;
 void launch_gemm_fwd_bf16(const void* W, int64_t ldw, const void* W_tail, const void* Hc, int64_t ldh, int k_len, const float* zt,
                           const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                           int V, int d, float* part_sum, float* part_ez,
-                          int64_t part_stride, void* estash, int64_t lde, bool in_blocks, hipStream_t stream);
+                          int64_t part_stride, void* estash, int64_t lde, bool in_blocks, float log2_scale, hipStream_t stream);
 
 // dH: A = E [chunk_rows, Vp] (the patched bf16 stash), B = W^T read in place from W [V, d] (row
 // stride ldw); row m, multiplied by row_scale[chunk_start + m], goes to
@@ -232,6 +233,40 @@ struct FinalizeArgs {
   int64_t rows_enqueued; const int32_t* row_index; float* out_logp; double* out_d; int64_t* out_i;
 };
 void launch_finalize(const FinalizeArgs& a, hipStream_t stream);
+
+// ---- distillation --------------------------------------------------------------
+// Entries per row at most.
+constexpr int kMostAlternatives = 256;
+struct DistillArgs {
+  const int32_t* ids; const float* logp; int k;      // [N, k] per slot
+  const uint8_t* mask; const float* weight;          // [N] per slot, or nullptr
+  int64_t N; int d, V; int renormalize;
+  const void* H; const void* W;
+  float scale2, temperature;                         // log2(e) / temperature
+  int32_t* targets;                                  // [N]: the best alternative's id, or -1 for a slot that does not count
+  const int32_t* row_index; const int64_t* n_scored; int64_t chunk_start; int chunk_rows;
+  float* zt; float* zk;                              // [N] compacted: the largest of the row's logits zk [chunk_rows, k]
+  const float* part_sum; int n_partials;             // bf16 path
+  uint16_t* estash; int64_t lde; float* row_scale;   // (nullptr: no backward pass)
+  float* Z; int64_t ldz; int write_dz;               // fp32 path
+  float* out_kl;                                     // [N] per slot
+  double* loss_partials; int64_t partial_block_offset;   // [blocks][kDistillSums]
+};
+constexpr int kDistillSums = 3;                      // weighted loss, saturated rows, ids at or above V
+// Which slots count: targets.
+void launch_distill_targets(const DistillArgs& a, hipStream_t stream);
+// bf16 path, before a pass's forward launch: the alternatives' logits zk, and zt.
+void launch_distill_logits(const DistillArgs& a, hipStream_t stream);
+// bf16 path, behind it: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S q / m.
+void launch_distill_rows(const DistillArgs& a, hipStream_t stream);
+// fp32 path: divergence, and dz in the place of the pass's logits.
+void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream);
+int distill_f32_blocks(int64_t rows);
+// The double (times scale) and the counts of mrl_distill_stats.
+void launch_distill_final(const double* parts, int64_t blocks, const int64_t* n_scored, const int64_t* n_empty, double scale, double* out_d,
+                          int64_t* out_i, hipStream_t stream);
+// out = bf16(in), n a multiple of 8
+void launch_to_bf16(const float* in, void* out, int64_t n, hipStream_t stream);
 
 // MRL_OK when the current device is a gfx950, else MRL_ERR_UNSUPPORTED_ARCH / MRL_ERR_DEVICE.
 int require_gfx950();
