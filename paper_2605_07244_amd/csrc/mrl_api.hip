@@ -171,7 +171,7 @@ Layout make_layout(int64_t N, int64_t B, int d, int V, int dtype, int chunk_rows
     if (k > 0) {
       L.targets = take(off, (size_t)N * 4);
       if (bf16) L.zk = take(off, (size_t)chunk_rows * k * 4);
-      if (dw_bf16) L.dw_sum = take(off, (size_t)V * d * 4);
+      if (dw_bf16 && L.n_chunks > 1) L.dw_sum = take(off, (size_t)V * d * 4);
     }
     L.Z = take(off, (size_t)chunk_rows * L.ldz * es);
     if (bf16) L.Ht = take(off, (size_t)dk * L.ldr * es);
@@ -685,7 +685,7 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     if (out_dW) {
       Scope sc(MRL_PROF_GEMM_DW, s);
       launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0,
-                          L.chunk_rows, V, d, out_dW, overwrite, at<float>(ws, L.tail), L.tail_items, expected, dw_blocks, s);
+                          L.chunk_rows, V, d, out_dW, 0, overwrite, at<float>(ws, L.tail), L.tail_items, expected, dw_blocks, s);
     }
   }
   if (!finalized) {
@@ -757,7 +757,9 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
   once.prep = prep_inline(N) ? &po : nullptr;
   once.mask = token_mask; once.N = N; once.V = V;
   once.dH = out_dH; once.dh_row_bytes = (int64_t)d * (cfg->dh_dtype == MRL_BF16 ? 2 : 4);
-  float* const dW = dw_bf16 && out_dW ? at<float>(ws, L.dw_sum) : static_cast<float*>(out_dW);
+  // (in 16 bits the sum of several passes is kept in 32 until the last)
+  const bool sum_apart = dw_bf16 && out_dW && L.n_chunks > 1;
+  float* const dW = sum_apart ? at<float>(ws, L.dw_sum) : static_cast<float*>(out_dW);
   for (int64_t c = 0; c < L.n_chunks; ++c) {
     const int64_t c0 = c * L.chunk_rows;
     const int rows = (int)(N - c0 < L.chunk_rows ? N - c0 : L.chunk_rows);      // at most
@@ -795,12 +797,12 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
     }
     if (dW) {
       Scope sc(MRL_PROF_GEMM_DW, s);
-      launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW, overwrite,
-                          at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
+      launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW,
+                          dw_bf16 && !sum_apart, overwrite, at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
     }
   }
   Scope sc(MRL_PROF_FINAL, s);
-  if (dw_bf16 && out_dW) launch_to_bf16(dW, out_dW, (int64_t)V * d, s);
+  if (sum_apart) launch_to_bf16(dW, out_dW, (int64_t)V * d, s);
   launch_distill_final(a.loss_partials, a.partial_block_offset, n_scored, n_scored + 1, (double)cfg->temperature * (double)cfg->temperature,
                        &out_stats->loss_total, &out_stats->n_scored_rows, s);
   return last_error();

@@ -46,6 +46,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // 16-byte access, 4-byte alignment
 
 constexpr int BK = 64;
@@ -56,7 +57,8 @@ constexpr int kDwTailMaxItems = 256;                // K slices of dW tail tiles
 // outstanding, no wait on the export / LDS counters.
 constexpr int waitcnt_vm(int n) { return (n & 0xF) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 
-enum { MODE_FWD = 0, MODE_DH = 1, MODE_DW = 2 };
+enum { MODE_FWD = 0, MODE_DH = 1, MODE_DW = 2, MODE_DW16 = 3 };   // DW16: dW with a bf16 output, the same but for its epilogue
+__host__ __device__ constexpr int product_of(int kind) { return kind == MODE_DW16 ? MODE_DW : kind; }
 constexpr int NXCD = 8;
 template <bool B> struct Flag { static constexpr bool value = B; };
 
@@ -440,6 +442,12 @@ __device__ __forceinline__ void dh_epilogue(const Params& p, unsigned char* smem
   }
 }
 
+__device__ __forceinline__ u32x2_any four_bf16(const f32x4& x) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  const bf16x4 h = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  return __builtin_bit_cast(u32x2_any, h);
+}
+
 // dW epilogue: vocabulary rows from m0 up to v_end on the ring side, hidden columns from n0; fp32 accumulate into dW.  With the MFMA's operands
 // swapped a lane holds four consecutive columns of a row, so that dW is read and written 16 bytes at a time (d is a multiple
 // of 8; with 4-byte accesses the launch took 1128 instead of 1023 us for 512 rows, V = 151936, d = 4096, and 127 instead
@@ -480,6 +488,33 @@ __device__ __forceinline__ void dw_epilogue(const Params& p, f32x4 (&acc)[NJ][8]
   }
 }
 
+// The same with a bf16 dW, which is overwritten: each sum rounded once.  A kernel of its own, since reads of the accumulators behind one more condition
+// ran the other's epilogue out of registers.
+template <int NJ, class Acc>
+__device__ __forceinline__ void dw16_epilogue(const Params& p, Acc read_acc, int wr, int m0, int n0, int res0, int v_last, float* tail_out) {
+  const int lane = lane_now(), frow = lane & 15, fq = lane >> 4;
+  if (tail_out != nullptr) {
+#pragma unroll
+    for (int i = 0; i < NJ; ++i) {
+      float* const row = tail_out + (ring_kmajor_row(i, wr) + frow) * RES + n0 - res0 + 4 * fq;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4_any*>(row + j * 16) = f32x4{read_acc(i, j, 0), read_acc(i, j, 1), read_acc(i, j, 2), read_acc(i, j, 3)};
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < NJ; ++i) {
+    const int v = m0 + ring_kmajor_row(i, wr) + frow;
+    uint16_t* const row = reinterpret_cast<uint16_t*>(p.dW) + (int64_t)(v < v_last ? v : v_last - 1) * p.d;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int n = n0 + 4 * fq + j * 16;
+      const u32x2_any x = four_bf16(f32x4{read_acc(i, j, 0), read_acc(i, j, 1), read_acc(i, j, 2), read_acc(i, j, 3)});
+      if (v < v_last && n < p.d) *reinterpret_cast<u32x2_any*>(row + n) = x;
+    }
+  }
+}
+
 // one direct load of 1 KB to LDS address slot + lds, from byte voff + soff behind the descriptor's base
 __device__ __forceinline__ void load_lds16(uint32_t voff, uint32_t soff, const u32x4& desc, uint32_t slot, uint32_t lds) {
   uint32_t off;
@@ -503,9 +538,10 @@ __device__ __forceinline__ void load_lds16(uint32_t voff, uint32_t soff, const u
 //   other duos: the next duo's ring blocks; then, in four pieces, the loads' advance by a panel
 // Loads go through buffer descriptors that end with the operand's last row and are emptied behind the last panel: edges need
 // no clamped addresses, and nothing is fetched twice at a tile's end.
-template <int MODE, int NJ>
+template <int KIND, int NJ>
 __device__ __forceinline__ void tile_product(const Params& args, unsigned char* smem, int ring_tile, int res_tile, int ring0, int ring_end,
                                              int k_first, int nk, float* tail_out) {
+  constexpr int MODE = product_of(KIND);
   constexpr bool RES_KMAJOR = MODE == MODE_DH, RING_KMAJOR = MODE == MODE_DW;
   constexpr int ND = NJ / 2, kLoads = 8 + NJ, kSlots = tile_slots<NJ>(), kWave = wave_bytes<NJ>(), kSlot = 4 * kWave;
   // Places in a panel's sequence of 16 NJ products: the barrier behind which the next panel may be read and this one's slot
@@ -736,7 +772,8 @@ __device__ __forceinline__ void tile_product(const Params& args, unsigned char* 
     forward_epilogue<NJ>(q, [&](int i, int j, int e) { return read_acc(j, i, e); }, [&](int j) { return zt[j]; }, res0 + ws * 128, n0, res_tile * 2 + ws, ring_end);
   }
   if (MODE == MODE_DH) dh_epilogue<NJ>(p, smem, read_acc, wave, ring0 + wr * (NJ * 16), wr * (NJ * 16), res0 + ws * 128, ws * 128, ring_end, tail_out);
-  if (MODE == MODE_DW) dw_epilogue<NJ>(p, acc, wr, ring0, res0 + ws * 128, res0, ring_end, tail_out);
+  if (KIND == MODE_DW) dw_epilogue<NJ>(p, acc, wr, ring0, res0 + ws * 128, res0, ring_end, tail_out);
+  if (KIND == MODE_DW16) dw16_epilogue<NJ>(p, read_acc, wr, ring0, res0 + ws * 128, res0, ring_end, tail_out);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -768,9 +805,10 @@ static_assert(kLoadsCarriedOver + kLoadsInGroup[5] + kLoadsInGroup[6] + kLoadsIn
 
 // A rows m0 .. M - 1 (at most 256), B rows n0 .. N - 1.  Workgroups that share a panel walk its row blocks in a different cyclic order
 // (rot_a, rot_b), so that they do not all ask the L2 for the same lines at the same moment.
-template <int MODE>
+template <int KIND>
 __device__ __forceinline__ void square_tile(const Params& p, unsigned char* smem, int m0, int M, int n0, int N, int rot_a, int rot_b, int part,
                                             int k_first, int nk, float* tail_out) {
+  constexpr int MODE = product_of(KIND);
   constexpr bool A_KMAJOR = MODE == MODE_DW, B_KMAJOR = MODE == MODE_DH;
   // (wave-uniform all of them; some come out of integer divisions, which run on the vector unit)
   m0 = __builtin_amdgcn_readfirstlane(m0); n0 = __builtin_amdgcn_readfirstlane(n0);
@@ -958,7 +996,8 @@ __device__ __forceinline__ void square_tile(const Params& p, unsigned char* smem
     forward_epilogue<8>(p, read_acc, [&](int j) { return *reinterpret_cast<const float*>(zt_lds + j * 64); }, m0 + wm * 128, n0 + wn * 128, part * 2 + wm, N);
   }
   if (MODE == MODE_DH) dh_epilogue<8>(p, smem, read_acc, wave, m0 + wm * 128, wm * 128, n0 + wn * 128, wn * 128, M, tail_out);
-  if (MODE == MODE_DW) dw_epilogue<8>(p, acc, wm, m0, n0 + wn * 128, n0, M, tail_out);
+  if (KIND == MODE_DW) dw_epilogue<8>(p, acc, wm, m0, n0 + wn * 128, n0, M, tail_out);
+  if (KIND == MODE_DW16) dw16_epilogue<8>(p, read_acc, wm, m0, n0 + wn * 128, n0, M, tail_out);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1081,7 +1120,7 @@ __device__ __forceinline__ void half_column_tile(unsigned char* smem, int tm, in
                       [&](int j) { return *reinterpret_cast<const float*>(zt_lds + j * 64); }, m0 + wm * 128, n0 + wn * 64, tm * 2 + wm, N);
 }
 
-// No panels at all: a slice of the contraction that the plan did not need, or dW without a scored row.
+// No panels at all: a slice of the contraction that the plan did not need, or dW without a scored row.  (Of bf16 two elements count as one: widths are even.)
 __device__ inline void zero_rows(float* at, int64_t ld, int rows, int cols) {
   for (int r = threadIdx.x >> 6; r < rows; r += NTHREADS / 64)
     for (int c = (threadIdx.x & 63) * 4; c < cols; c += 256) *reinterpret_cast<f32x4_any*>(at + (int64_t)r * ld + c) = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1128,8 +1167,8 @@ template <int MODE> __device__ __forceinline__ Cut cut_of(const Params& p, int n
 
 __device__ __forceinline__ int dh_band(const Cut& cut) { return cut.wide > 0 ? 4 : 8; }
 
-template <int MODE>
-__global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) {
+template <int KIND> __device__ __forceinline__ void gemm_tiles(const Params& p) {
+  constexpr int MODE = product_of(KIND);
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   // valid rows of this chunk (device-side, no host sync)
   const int64_t nv64 = *p.n_scored - p.chunk_start;
@@ -1151,8 +1190,8 @@ __global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) {
     // (the arguments as they are in the short one's: read again they are two scalar latencies a tile, 1 % at 8 panels)
     if (blocks == 4) half_column_tile(smem, tm, n0, nvalid);
     else if (__builtin_expect(blocks == 8, 1))
-      square_tile<MODE>(p, smem, tm * RES, p.M, n0, nvalid < n0 + 256 ? nvalid : n0 + 256, 2 * tn & 7, tm & 7, tm, 0, p.K / BK, nullptr);
-    else tile_product<MODE, kWide>(p, smem, tn, tm, n0, nvalid, 0, p.K / BK, nullptr);
+      square_tile<KIND>(p, smem, tm * RES, p.M, n0, nvalid < n0 + 256 ? nvalid : n0 + 256, 2 * tn & 7, tm & 7, tm, 0, p.K / BK, nullptr);
+    else tile_product<KIND, kWide>(p, smem, tn, tm, n0, nvalid, 0, p.K / BK, nullptr);
   } else if constexpr (MODE == MODE_DH) {
     const int Nt = tiles_of(p.N, RES);
     const Cut cut = cut_of<MODE>(p, nvalid);
@@ -1166,17 +1205,18 @@ __global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) {
       if (nk <= 0) { zero_rows(tail_out, RES, RING, RES); return; }
     }
     const int m0 = cut.start(tm), blocks = cut.blocks(tm);
-    if (blocks == 4) tile_product<MODE, 4>(p, smem, tm, tn, m0, nvalid < m0 + 128 ? nvalid : m0 + 128, k_first, nk, tail_out);
-    else if (blocks == 8) square_tile<MODE>(p, smem, m0, nvalid < m0 + 256 ? nvalid : m0 + 256, tn * RES, p.N, 2 * tn & 7, tm & 7, 0, k_first, nk, tail_out);
-    else tile_product<MODE, kWide>(p, smem, tm, tn, m0, nvalid, k_first, nk, tail_out);
+    if (blocks == 4) tile_product<KIND, 4>(p, smem, tm, tn, m0, nvalid < m0 + 128 ? nvalid : m0 + 128, k_first, nk, tail_out);
+    else if (blocks == 8) square_tile<KIND>(p, smem, m0, nvalid < m0 + 256 ? nvalid : m0 + 256, tn * RES, p.N, 2 * tn & 7, tm & 7, 0, k_first, nk, tail_out);
+    else tile_product<KIND, kWide>(p, smem, tm, tn, m0, nvalid, k_first, nk, tail_out);
   } else if (p.wide) {
     const int panels = dw_panels(nvalid, p.K), Mt = tiles_of(p.V, RING), Nt = tiles_of(p.d, RES);
     int k_first = 0, nk = panels;
     const int item = split_tile(4, blockIdx.x, Mt, Nt, panels, p.max_items, DwSplit{}, tm, tn, k_first, nk);
     if (item < -1 || (item >= 0 && nk <= 0)) return;  // (an empty slice: nothing to store, and nobody reads it)
     const int rows = p.V - tm * RING < RING ? p.V - tm * RING : RING, cols = p.d - tn * RES < RES ? p.d - tn * RES : RES;
-    if (panels == 0) zero_rows(p.dW + (int64_t)tm * RING * p.d + tn * RES, p.d, rows, cols);
-    else tile_product<MODE, kWide>(p, smem, tm, tn, tm * RING, p.V, k_first, nk, item >= 0 ? p.tail_part + (int64_t)item * (RING * RES) : nullptr);
+    constexpr int per = KIND == MODE_DW16 ? 2 : 1;
+    if (panels == 0) zero_rows(p.dW + ((int64_t)tm * RING * p.d + tn * RES) / per, p.d / per, rows, cols / per);
+    else tile_product<KIND, kWide>(p, smem, tm, tn, tm * RING, p.V, k_first, nk, item >= 0 ? p.tail_part + (int64_t)item * (RING * RES) : nullptr);
   } else {
     // 256 x 256 tiles: the rows of tiles up to the tail's first one, and the tail's slices (see dw_tail_plan)
     const int panels = dw_panels(nvalid, p.K), Nt = tiles_of(p.d, RES);
@@ -1186,7 +1226,9 @@ __global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) {
     if (p.tail_split == 0 || (int)blockIdx.x < p.main_blocks) {
       if (!tile_coords(blockIdx.x, Mt, Nt, p.sup_m, p.sup_n, tm, tn)) return;
       if (panels == 0) {
-        zero_rows(p.dW + (int64_t)tm * RES * p.d + tn * RES, p.d, p.V - tm * RES < RES ? p.V - tm * RES : RES, p.d - tn * RES < RES ? p.d - tn * RES : RES);
+        constexpr int per = KIND == MODE_DW16 ? 2 : 1;
+        zero_rows(p.dW + ((int64_t)tm * RES * p.d + tn * RES) / per, p.d / per, p.V - tm * RES < RES ? p.V - tm * RES : RES,
+                  (p.d - tn * RES < RES ? p.d - tn * RES : RES) / per);
         return;
       }
     } else {
@@ -1204,9 +1246,12 @@ __global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) {
       tail_out = p.tail_part + (int64_t)item * (RES * RES);
       if (nk <= 0) { zero_rows(tail_out, RES, RES, RES); return; }
     }
-    square_tile<MODE>(p, smem, tm * RES, p.V, tn * RES, p.N, tn * 8 / p.sup_n & 7, tm * 8 / p.sup_m & 7, 0, k_first, nk, tail_out);
+    square_tile<KIND>(p, smem, tm * RES, p.V, tn * RES, p.N, tn * 8 / p.sup_n & 7, tm * 8 / p.sup_m & 7, 0, k_first, nk, tail_out);
   }
 }
+
+template <int MODE> __global__ __launch_bounds__(NTHREADS) void gemm_nt_bf16(Params p) { gemm_tiles<MODE>(p); }
+__global__ __launch_bounds__(NTHREADS) void gemm_dw16(Params p) { gemm_tiles<MODE_DW16>(p); }
 
 // ---------------------------------------------------------------------------------------------
 // Forward of at most 256 rows: 128 x 256 tiles (vocabulary x tokens), two workgroups per compute unit.
@@ -1393,7 +1438,7 @@ constexpr int D_LOADS = 6;                                          // direct lo
 // tiles leave little to gain, 327 rows 483 and 484, 1000 rows 825 and 846 a call.
 constexpr int kFewDwRows = 1024;
 
-__global__ __launch_bounds__(NTHREADS, 2) void dw_few_bf16(Params p) {
+template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_bf16(Params p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int frow = lane & 15, fq = lane >> 4, wm = wave >> 1, wn = wave & 1;
@@ -1496,6 +1541,12 @@ __global__ __launch_bounds__(NTHREADS, 2) void dw_few_bf16(Params p) {
                                               : __builtin_amdgcn_update_dpp(ib, ia, 0x128, 0xf, 0x3, false));
       }
     }
+    if (BF16_OUT) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (ok[j]) *reinterpret_cast<u32x2_any*>(reinterpret_cast<uint16_t*>(p.dW) + (at[j] - p.dW)) = four_bf16(x[j]);
+      continue;
+    }
     if (!p.overwrite) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) if (ok[j]) old[j] = *reinterpret_cast<const f32x4_any*>(at[j]);
@@ -1586,7 +1637,7 @@ DwTailPlan dw_tail_plan(int Mt, int Nt, int sup_m, int sup_n) {
 
 __global__ __launch_bounds__(256) void dw_tail_reduce(const float* __restrict__ part, int tiles, int split, int Nt,
                                                       int tail_m0, int V, int d, float* __restrict__ dW,
-                                                      int overwrite, const int64_t* __restrict__ n_scored,
+                                                      int overwrite, int dw_bf16, const int64_t* __restrict__ n_scored,
                                                       int64_t chunk_start, int chunk_rows) {
   int64_t nv64 = *n_scored - chunk_start;
   const int nvalid = nv64 < 0 ? 0 : (nv64 > chunk_rows ? chunk_rows : (int)nv64);
@@ -1599,6 +1650,10 @@ __global__ __launch_bounds__(256) void dw_tail_reduce(const float* __restrict__ 
   float s = 0.f;
   const int slices = slices_in_use(dw_panels(nvalid, chunk_rows), split);
   for (int k = 0; k < slices; ++k) s += part[((int64_t)k * tiles + t) * (RES * RES) + within];
+  if (dw_bf16) {
+    reinterpret_cast<__bf16*>(dW)[(int64_t)v * d + n] = (__bf16)s;
+    return;
+  }
   float* out = dW + (int64_t)v * d + n;
   *out = overwrite ? s : *out + s;
 }
@@ -1648,7 +1703,7 @@ __global__ __launch_bounds__(256) void dh_tail_reduce(Params p) {
   }
 }
 // The same for the dW launch on 384 x 256 tiles.
-__global__ __launch_bounds__(256) void dw_wide_reduce(Params p) {
+template <bool BF16_OUT> __global__ __launch_bounds__(256) void dw_wide_reduce(Params p) {
   int64_t nv64 = *p.n_scored - p.chunk_start;
   const int nvalid = nv64 < 0 ? 0 : (nv64 > p.chunk_rows ? p.chunk_rows : (int)nv64);
   const int panels = dw_panels(nvalid, p.K);
@@ -1663,6 +1718,12 @@ __global__ __launch_bounds__(256) void dw_wide_reduce(Params p) {
   if (v >= p.V || n >= p.d) return;
   f32x4 lo, hi;
   add_slices(p.tail_part, slices_in_use(panels, split), rest, t, within, lo, hi);
+  if (BF16_OUT) {
+    u32x2_any* const out = reinterpret_cast<u32x2_any*>(reinterpret_cast<uint16_t*>(p.dW) + (int64_t)v * p.d + n);
+    out[0] = four_bf16(lo);
+    out[1] = four_bf16(hi);
+    return;
+  }
   f32x4_any* const out = reinterpret_cast<f32x4_any*>(p.dW + (int64_t)v * p.d + n);
   if (!p.overwrite) { lo = out[0] + lo; hi = out[1] + hi; }
   out[0] = lo;
@@ -1886,30 +1947,31 @@ bool dw_rows_in_blocks(int rows) { return rows <= kFewDwRows; }
 
 void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
-                         int V, int d, float* dW, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
+                         int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
                          hipStream_t stream) {
   Params p = {};
   p.A = static_cast<const uint16_t*>(E); p.lda = lde;
   p.B = static_cast<const uint16_t*>(Ht); p.ldb = ldht; p.N = d;
   p.K = chunk_rows;
   p.n_scored = n_scored; p.chunk_start = chunk_start; p.chunk_rows = chunk_rows;
-  p.dW = dW; p.overwrite = overwrite; p.V = V; p.d = d;
+  p.dW = static_cast<float*>(dW); p.overwrite = overwrite; p.V = V; p.d = d;
   p.tail_part = tail_part;
   if (in_blocks) {
     p.N = (int)ldht;                                  // (rows of a block: d rounded up to 128)
     p.streaming = d % 32 == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
-    static LdsLimit lds_limit;
-    lds_limit.ensure(reinterpret_cast<const void*>(&dw_few_bf16), D_LDS);
+    static LdsLimit lds_limit[2];
+    const auto kernel = dw_bf16 ? &dw_few_bf16<true> : &dw_few_bf16<false>;
+    lds_limit[dw_bf16].ensure(reinterpret_cast<const void*>(kernel), D_LDS);
     const int64_t tiles = (int64_t)((V + DM - 1) / DM) * ((d + DN - 1) / DN);
-    hipLaunchKernelGGL(dw_few_bf16, dim3((unsigned)round_up(tiles, NXCD)), dim3(NTHREADS), D_LDS, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)round_up(tiles, NXCD)), dim3(NTHREADS), D_LDS, stream, p);
     return;
   }
   p.max_items = tail_items;
   const DwPlan plan = plan_dw(chunk_rows, rows, V, d, tail_items);
   p.wide = plan.wide;
   if (p.wide) {
-    launch<gemm_nt_bf16<MODE_DW>>(p, plan.blocks, stream);
-    if (plan.most_split > 1) hipLaunchKernelGGL(dw_wide_reduce, dim3(plan.rest * kReduceBlocks), dim3(256), 0, stream, p);
+    if (dw_bf16) launch<gemm_dw16>(p, plan.blocks, stream); else launch<gemm_nt_bf16<MODE_DW>>(p, plan.blocks, stream);
+    if (plan.most_split > 1) hipLaunchKernelGGL(dw_bf16 ? dw_wide_reduce<true> : dw_wide_reduce<false>, dim3(plan.rest * kReduceBlocks), dim3(256), 0, stream, p);
     return;
   }
   const DwTailPlan& tail = plan.tail;
@@ -1927,11 +1989,11 @@ void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldh
     p.tail_first[NXCD] = tail.first[NXCD];
     blocks += most * NXCD;
   }
-  launch<gemm_nt_bf16<MODE_DW>>(p, blocks, stream);
+  if (dw_bf16) launch<gemm_dw16>(p, blocks, stream); else launch<gemm_nt_bf16<MODE_DW>>(p, blocks, stream);
   if (tail.split > 0) {
     const int n = tail.rows * Nt;
-    hipLaunchKernelGGL(dw_tail_reduce, dim3(n * (RES * RES / 256)), dim3(256), 0, stream, tail_part, n, tail.split, Nt, tail.m0, V, d, dW,
-                       overwrite, n_scored, chunk_start, chunk_rows);
+    hipLaunchKernelGGL(dw_tail_reduce, dim3(n * (RES * RES / 256)), dim3(256), 0, stream, tail_part, n, tail.split, Nt, tail.m0, V, d,
+                       p.dW, overwrite, dw_bf16, n_scored, chunk_start, chunk_rows);
   }
 }
 

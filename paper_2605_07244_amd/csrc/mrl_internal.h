@@ -84,7 +84,7 @@ void launch_gemm_dh_bf16(const void* E, int64_t lde, const void* W, int64_t ldw,
 // dW: A = E^T read in place from E [chunk_rows, Vp] (rows >= valid rows rounded up to 128 and
 // columns >= V must be zero), B = Ht [d, chunk_rows] (the pass's hidden rows, each already
 // multiplied by its row scale); dW[v, :] = (or +=) sum over the chunk's valid rows.
-// overwrite = 1 stores, 0 adds into the existing values.
+// overwrite = 1 stores, 0 adds into the existing values.  dw_bf16 = 1: dW is bf16, each sum rounded once, and overwrite = 1.
 // tail_part: scratch of tail_items * gemm_tail_tile_bytes() bytes (gemm_tail_bytes_least() or more) for the K slices of the last
 // tiles; rows: the scored rows expected (which tiles the launch takes; right for any number).
 // in_blocks: the launch for few rows, with Ht in blocks of kRowBlock token rows, [chunk_rows / 32][ldht][32], ldht = d
@@ -95,7 +95,7 @@ size_t gemm_tail_bytes_least(size_t head_bytes);      // ... in one that has no 
 bool dw_rows_in_blocks(int rows);
 void launch_gemm_dw_bf16(const void* P, int64_t ldp, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
-                         int V, int d, float* dW, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
+                         int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
                          hipStream_t stream);
 
 // ---- fp32 GEMM (small-shape path): C[m][n] = sum_k A[m][k] * B[n][k] --------
