@@ -167,7 +167,7 @@ Layout make_layout(int64_t N, int64_t B, int d, int V, int dtype, int chunk_rows
     L.g_c = take(off, (size_t)(N + 1) * 4);
     L.row_scale = bf16 ? take(off, (size_t)(N + 1) * 4) : 0;
     L.loss_partials = take(off, k == 0 ? (size_t)(L.epi_blocks_total + 1) * 10 * 8
-                                       : (size_t)(bf16 ? L.epi_blocks_total : distill_f32_blocks(N) + L.n_chunks) * kDistillSums * 8);
+                                       : (size_t)(bf16 ? L.n_chunks * distill_row_blocks(chunk_rows) : distill_f32_blocks(N) + L.n_chunks) * kDistillSums * 8);
     if (k > 0) {
       L.targets = take(off, (size_t)N * 4);
       if (bf16) L.zk = take(off, (size_t)chunk_rows * k * 4);
@@ -773,7 +773,7 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
     {
       Scope sc(MRL_PROF_ROW_EPI, s);
       if (bf16) launch_distill_rows(a, s); else launch_distill_f32(a, rows, s);
-      a.partial_block_offset += bf16 ? row_epilogue_blocks(L.chunk_rows) : distill_f32_blocks(rows);
+      a.partial_block_offset += bf16 ? distill_row_blocks(L.chunk_rows) : distill_f32_blocks(rows);
     }
     if (!bwd) continue;
     const int overwrite = c == 0 && !cfg->accumulate_dw;

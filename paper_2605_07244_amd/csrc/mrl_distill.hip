@@ -12,7 +12,6 @@
 namespace mrl {
 namespace {
 
-constexpr int kEach = kMostAlternatives / 64;          // alternatives of a lane: j = 64 i + lane
 constexpr double LN2 = 0.6931471805599453;
 constexpr double kLeastMass = 1e-30;                   // of a row that counts: S / m stays a number
 
@@ -27,8 +26,8 @@ __device__ inline float wave_max(float x) {            // NaN is passed over
   return x;
 }
 
-// A slot's alternatives, by one wave.
-struct Alternatives {
+// A slot's alternatives, by one wave, kEach to a lane: j = 64 i + lane.
+template <int kEach> struct Alternatives {
   int id[kEach];                                       // -1: none
   float t[kEach];
   double q[kEach], log_q[kEach], m;
@@ -106,12 +105,12 @@ __device__ inline double too_large(const DistillArgs& a, int64_t slot) {
 }
 
 // A wave per slot: the id of its best alternative, or -1.
-__global__ __launch_bounds__(256) void k_distill_targets(DistillArgs a) {
+template <int kEach> __global__ __launch_bounds__(256) void k_distill_targets(DistillArgs a) {
   const int64_t n = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (n >= a.N) return;
   int target = -1;
   if (a.mask == nullptr || a.mask[n] != 0) {
-    Alternatives alt;
+    Alternatives<kEach> alt;
     alt.load(a, n);
     const float best = alt.best_t();
     alt.weigh(a, best);
@@ -177,22 +176,36 @@ __global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
   if (threadIdx.x == 0) a.zt[a.chunk_start + r] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
 }
 
-// Behind the forward launch: a block takes EPI_ROWS rows, first their sums, then a wave each row.
-__global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
-  __shared__ float4 sh[EPI_LANES][EPI_ROWS / 4];
-  __shared__ float sums[EPI_ROWS];
+// Behind the forward launch: a workgroup adds the partial sums of 16 rows, then a wave takes each.  (Blocks of 64 rows, four to a wave, left most of the chip idle:
+// 200 rows, k = 32 50 us, now ROWS_SHORT; 8192 rows, k = 64 77, now ROWS_LONG.)
+constexpr int kRows = 16, kLanes = EPI_THREADS / (kRows / 4);
+template <int kEach> __global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
+  __shared__ float sh[kLanes * (kRows + 1)];
   __shared__ double parts[EPI_THREADS / 64][kDistillSums];
-  const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows), r0 = blockIdx.x * EPI_ROWS;
+  const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows), r0 = blockIdx.x * kRows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double q[kDistillSums] = {};
   if (r0 < nvalid) {
-    const float s = merge_partials(a.part_sum + r0, a.chunk_rows, a.n_partials, sh);
-    if (threadIdx.x < EPI_ROWS) sums[threadIdx.x] = s;
+    // a thread adds every kLanes-th partial of four rows; the rows behind the valid ones hold whatever the buffer held
+    const int quad = threadIdx.x & 3, part = threadIdx.x >> 2;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int i = part; i < a.n_partials; i += kLanes) {
+      const float4 x = *reinterpret_cast<const float4*>(a.part_sum + (int64_t)i * a.chunk_rows + r0 + quad * 4);
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    float* const cell = sh + part * (kRows + 1) + quad * 4;
+    cell[0] = s.x; cell[1] = s.y; cell[2] = s.z; cell[3] = s.w;
     __syncthreads();
-    for (int i = wave; i < EPI_ROWS && r0 + i < nvalid; i += EPI_THREADS / 64) {
-      const int64_t r = r0 + i, ci = a.chunk_start + r, slot = a.row_index[ci];
-      const float S = sums[i], c2 = fmaf(a.zt[ci], a.scale2, kStashMargin2), w = weight_of(a, slot);
-      Alternatives alt;
+    const int64_t r = r0 + wave;
+    if (r < nvalid) {
+      float S = 0.f;
+#pragma unroll
+      for (int i = 0; i < kLanes / 64; ++i) S += sh[(64 * i + lane) * (kRows + 1) + wave];
+      S = lanes_sum<64>(S);
+      const int64_t ci = a.chunk_start + r, slot = a.row_index[ci];
+      const float c2 = fmaf(a.zt[ci], a.scale2, kStashMargin2), w = weight_of(a, slot);
+      Alternatives<kEach> alt;
       alt.load(a, slot);
       alt.weigh(a, alt.best_t());
       const double log2_sum = (double)c2 + log2((double)S);        // of exponentials in the log2 domain, with the very c2 that the launch took
@@ -212,20 +225,20 @@ __global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
       if (lane == 0) a.out_kl[slot] = (float)kl;
       if (saturated) q[1] += 1.0; else q[0] += (double)w * kl;
       q[2] += too_large(a, slot);
-      if (a.row_scale == nullptr) continue;
-      if (lane == 0) a.row_scale[ci] = saturated ? 0.f : !number ? __builtin_nanf("") : (float)((double)w * (double)a.temperature * alt.m / (double)S);
-      if (saturated) continue;
-      float total[kEach];
-      bool first[kEach];
-      alt.by_id(a.k, total, first);
-      const float per = (float)((double)S / alt.m);
-      uint16_t* const row = a.estash + r * a.lde;
+      if (a.row_scale != nullptr && lane == 0) a.row_scale[ci] = saturated ? 0.f : !number ? __builtin_nanf("") : (float)((double)w * (double)a.temperature * alt.m / (double)S);
+      if (a.row_scale != nullptr && !saturated) {
+        float total[kEach];
+        bool first[kEach];
+        alt.by_id(a.k, total, first);
+        const float per = (float)((double)S / alt.m);
+        uint16_t* const row = a.estash + r * a.lde;
 #pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (first[e]) {
-          const float x = __builtin_amdgcn_exp2f(fminf(fmaf(z[e], a.scale2, -c2), kStashClamp2)) - per * total[e];
-          row[alt.id[e]] = (uint16_t)pack_bf16(x, 0.f);
-        }
+        for (int e = 0; e < kEach; ++e)
+          if (first[e]) {
+            const float x = __builtin_amdgcn_exp2f(fminf(fmaf(z[e], a.scale2, -c2), kStashClamp2)) - per * total[e];
+            row[alt.id[e]] = (uint16_t)pack_bf16(x, 0.f);
+          }
+      }
     }
   }
   if (lane == 0) {
@@ -243,7 +256,7 @@ __global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
 // ----------------------------------------------------------------------------
 // fp32: a wave per row of the materialised logits, which become dz.
 // ----------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
+template <int kEach> __global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
   __shared__ double parts[4][kDistillSums];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x * 4 + wave;
@@ -259,7 +272,7 @@ __global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
     for (int v = lane; v < a.V; v += 64) s += expf((row[v] - mx) * inv_T);
     const float S = lanes_sum<64>(s);
     const double log_S = log((double)S);
-    Alternatives alt;
+    Alternatives<kEach> alt;
     alt.load(a, slot);
     alt.weigh(a, alt.best_t());
     double kl = 0.0;
@@ -334,19 +347,25 @@ __global__ __launch_bounds__(256) void k_to_bf16(const float* in, uint16_t* out,
 
 }  // namespace
 
+// Alternatives of a lane: as few as do (a double exponential each).
+template <class F> static F by_count(int k, F one, F two, F four) { return k <= 64 ? one : k <= 128 ? two : four; }
+static_assert(kMostAlternatives <= 256, "four to a lane");
+
 void launch_distill_targets(const DistillArgs& a, hipStream_t stream) {
   const int64_t blocks = (a.N + 3) / 4, wide = blocks < (1 << 21) ? blocks : 1 << 21;
-  hipLaunchKernelGGL(k_distill_targets, dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(by_count(a.k, k_distill_targets<1>, k_distill_targets<2>, k_distill_targets<4>), dim3((unsigned)wide, (unsigned)((blocks + wide - 1) / wide)),
+                     dim3(256), 0, stream, a);
 }
 void launch_distill_logits(const DistillArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(k_distill_logits, dim3(a.chunk_rows), dim3(256), 0, stream, a);
 }
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(k_distill_rows, dim3((a.chunk_rows + EPI_ROWS - 1) / EPI_ROWS), dim3(EPI_THREADS), 0, stream, a);
+  hipLaunchKernelGGL(by_count(a.k, k_distill_rows<1>, k_distill_rows<2>, k_distill_rows<4>), dim3(a.chunk_rows / kRows), dim3(EPI_THREADS), 0, stream, a);
 }
+int distill_row_blocks(int chunk_rows) { return chunk_rows / kRows; }
 int distill_f32_blocks(int64_t rows) { return (int)((rows + 3) / 4); }
 void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream) {
-  hipLaunchKernelGGL(k_distill_f32, dim3(distill_f32_blocks(rows)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(by_count(a.k, k_distill_f32<1>, k_distill_f32<2>, k_distill_f32<4>), dim3(distill_f32_blocks(rows)), dim3(256), 0, stream, a);
 }
 void launch_distill_final(const double* parts, int64_t blocks, const int64_t* n_scored, const int64_t* n_empty, double scale, double* out_d, int64_t* out_i,
                           hipStream_t stream) {

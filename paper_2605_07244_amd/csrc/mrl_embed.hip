@@ -60,12 +60,17 @@ template <bool kBf16> __global__ __launch_bounds__(kLookThreads) void k_embeddin
 struct SortArgs {
   const int32_t* ids; const uint8_t* mask; int64_t N; int V, blocks, passes;
   int32_t *key_a, *at_a, *key_b, *at_b;                   // [N] each
-  uint32_t* counts;                                       // [passes][blocks][kDigits]
+  uint32_t* counts;                                       // [blocks][kDigits], of the pass under way
   uint8_t* used;                                          // [V]: 1 where a token occurs (nullptr: not wanted)
 };
 __device__ inline int key_of(const SortArgs& a, int64_t n) {
   const int id = a.ids[n];
   return id >= 0 && id < a.V && (a.mask == nullptr || a.mask[n] != 0) ? id : a.V;
+}
+
+// (the marks are padded to whole vectors)
+__device__ inline void clear_marks(const SortArgs& a, int64_t first, int64_t step) {
+  for (int64_t v = first; v * 16 < a.V; v += step) reinterpret_cast<u32x4*>(a.used)[v] = u32x4{0, 0, 0, 0};
 }
 
 struct SortShared {
@@ -123,27 +128,24 @@ __device__ inline uint32_t before_digit(SortShared& sh, uint32_t x) {
   return incl - x;
 }
 
-// Counts of the first pass's digits, a workgroup per kItems tokens; the other passes' counts and the marks are cleared.
-__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a) {
+// Counts of a pass's digits, a workgroup per kItems items; with the first the marks are cleared.  (Counts of the second pass made by the first one's stores, with
+// atomics in memory, took 25 us of 65536 tokens, for the most common token's 3800 that meet in one; a launch more takes 5.)
+__global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a, int pass) {
   __shared__ uint32_t count[kDigits];
   if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
   __syncthreads();
+  const int32_t* const from = pass & 1 ? a.key_a : a.key_b;
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     const int64_t n = (int64_t)blockIdx.x * kItems + r * kSortThreads + threadIdx.x;
-    if (n < a.N) atomicAdd(&count[key_of(a, n) & (kDigits - 1)], 1u);
+    if (n < a.N) atomicAdd(&count[((pass == 0 ? key_of(a, n) : from[n]) >> (pass * kDigitBits)) & (kDigits - 1)], 1u);
   }
   __syncthreads();
-  if (threadIdx.x < kDigits) {
-    for (int p = 0; p < a.passes; ++p)
-      a.counts[((int64_t)p * a.blocks + blockIdx.x) * kDigits + threadIdx.x] = p == 0 ? count[threadIdx.x] : 0;
-  }
-  if (a.used != nullptr)
-    for (int64_t v = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; v < a.V; v += (int64_t)gridDim.x * kSortThreads) a.used[v] = 0;
+  if (threadIdx.x < kDigits) a.counts[(int64_t)blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
+  if (pass == 0 && a.used != nullptr) clear_marks(a, (int64_t)blockIdx.x * kSortThreads + threadIdx.x, (int64_t)gridDim.x * kSortThreads);
 }
 
-// A pass: every item to its place by the pass's digit, equal ones in their order.  pass 0 reads the tokens and marks them; the next pass's counts are
-// made here, for the blocks that the items go to.
+// A pass: every item to its place by the pass's digit, equal ones in their order.  The first reads the tokens and marks them.
 __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass) {
   __shared__ SortShared sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, shift = pass * kDigitBits;
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass
   // items of smaller digits, and of this one in earlier blocks
   uint32_t all = 0, earlier = 0;
   if (threadIdx.x < kDigits) {
-    const uint32_t* c = a.counts + (int64_t)pass * a.blocks * kDigits + threadIdx.x;
+    const uint32_t* c = a.counts + threadIdx.x;
 #pragma unroll 8
     for (int b = 0; b < a.blocks; ++b) {
       const uint32_t x = c[(int64_t)b * kDigits];
@@ -182,8 +184,6 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass
     const uint32_t to = sh.start[digit[r]] + sh.table[wave][digit[r]] + (uint32_t)place[r];
     to_key[to] = key[r];
     to_at[to] = at[r];
-    if (pass + 1 < a.passes)
-      atomicAdd(a.counts + ((int64_t)(pass + 1) * a.blocks + to / kItems) * kDigits + ((key[r] >> (shift + kDigitBits)) & (kDigits - 1)), 1u);
   }
 }
 
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs a) {
   __shared__ int32_t keys[kItems], ats[kItems];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (a.used != nullptr) {
-    for (int v = threadIdx.x; v < a.V; v += kSortThreads) a.used[v] = 0;
+    clear_marks(a, threadIdx.x, kSortThreads);
     __threadfence();
     __syncthreads();                                      // (the marks come behind the zeros)
   }
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void k_embedding_join(SumArgs a) {
     const int64_t j = j0 + lane;
     const unsigned long long same = __ballot(j < a.chunks && a.key[(j < a.chunks ? j : c) * a.chunk] == id);
     const int m = same == ~0ull ? 64 : __builtin_ctzll(~same);
-#pragma unroll 4
+#pragma unroll 16
     for (int i = 0; i < m; ++i) {
       const float* q = a.parts + (j0 + i) * 2 * ld + col;
       const float4 lo = *reinterpret_cast<const float4*>(q), hi = *reinterpret_cast<const float4*>(q + 4);
@@ -384,7 +384,7 @@ BackLayout layout_of(int64_t N, int d, int V) {
   size_t off = 0;
   L.key_a = take(off, (size_t)N * 4); L.at_a = take(off, (size_t)N * 4);
   L.key_b = take(off, (size_t)N * 4); L.at_b = take(off, (size_t)N * 4);
-  L.counts = take(off, (size_t)L.passes * L.blocks * kDigits * 4);
+  L.counts = take(off, (size_t)L.blocks * kDigits * 4);
   L.used = take(off, (size_t)V);
   L.parts = take(off, (size_t)L.chunks * 2 * L.tiles * kTileColumns * 4);
   L.total = off;
@@ -441,8 +441,10 @@ extern "C" int mrl_embedding_backward(const void* dy, const int32_t* ids, const 
   if (N <= kItems) {
     hipLaunchKernelGGL(k_sort_few, dim3(1), dim3(kSortThreads), 0, s, sort);
   } else {
-    hipLaunchKernelGGL(k_sort_count, dim3(L.blocks), dim3(kSortThreads), 0, s, sort);
-    for (int p = 0; p < L.passes; ++p) hipLaunchKernelGGL(k_sort_pass, dim3(L.blocks), dim3(kSortThreads), 0, s, sort, p);
+    for (int p = 0; p < L.passes; ++p) {
+      hipLaunchKernelGGL(k_sort_count, dim3(L.blocks), dim3(kSortThreads), 0, s, sort, p);
+      hipLaunchKernelGGL(k_sort_pass, dim3(L.blocks), dim3(kSortThreads), 0, s, sort, p);
+    }
     in_a = L.passes % 2 == 1;
   }
   const int64_t sum_blocks = N > 0 ? (L.chunks * L.tiles + 3) / 4 : 0, zero_blocks = accumulate ? 0 : ((int64_t)V + kZeroRows - 1) / kZeroRows;

@@ -46,7 +46,8 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // 16-byte access, 4-byte alignment
 
 constexpr int BK = 64;
@@ -448,6 +449,14 @@ __device__ __forceinline__ u32x2_any four_bf16(const f32x4& x) {
   return __builtin_bit_cast(u32x2_any, h);
 }
 
+// Of column blocks a and b of 16, four columns of a row per lane each, eight neighbouring ones of one of them: lanes of the first and third 16 trade
+// their b for their neighbours' a.  Lane fq then has columns 8 (fq / 2) .. + 7 of block a (fq even) or b (odd).
+__device__ __forceinline__ u32x4_any eight_bf16(const f32x4& a, const f32x4& b) {
+  const u32x2_any x = four_bf16(a), y = four_bf16(b);
+  const auto lo = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false), hi = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+  return u32x4_any{lo[0], hi[0], lo[1], hi[1]};
+}
+
 // dW epilogue: vocabulary rows from m0 up to v_end on the ring side, hidden columns from n0; fp32 accumulate into dW.  With the MFMA's operands
 // swapped a lane holds four consecutive columns of a row, so that dW is read and written 16 bytes at a time (d is a multiple
 // of 8; with 4-byte accesses the launch took 1128 instead of 1023 us for 512 rows, V = 151936, d = 4096, and 127 instead
@@ -507,10 +516,12 @@ __device__ __forceinline__ void dw16_epilogue(const Params& p, Acc read_acc, int
     const int v = m0 + ring_kmajor_row(i, wr) + frow;
     uint16_t* const row = reinterpret_cast<uint16_t*>(p.dW) + (int64_t)(v < v_last ? v : v_last - 1) * p.d;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int n = n0 + 4 * fq + j * 16;
-      const u32x2_any x = four_bf16(f32x4{read_acc(i, j, 0), read_acc(i, j, 1), read_acc(i, j, 2), read_acc(i, j, 3)});
-      if (v < v_last && n < p.d) *reinterpret_cast<u32x2_any*>(row + n) = x;
+    for (int j = 0; j < 8; j += 2) {
+      const f32x4 a = {read_acc(i, j, 0), read_acc(i, j, 1), read_acc(i, j, 2), read_acc(i, j, 3)};
+      const f32x4 b = {read_acc(i, j + 1, 0), read_acc(i, j + 1, 1), read_acc(i, j + 1, 2), read_acc(i, j + 1, 3)};
+      const u32x4_any x = eight_bf16(a, b);
+      const int n = n0 + (j + (fq & 1)) * 16 + 8 * (fq >> 1);
+      if (v < v_last && n < p.d) *reinterpret_cast<u32x4_any*>(row + n) = x;
     }
   }
 }
@@ -1523,6 +1534,30 @@ template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_b
   // and j + 1, lanes frow < 8 and frow >= 8 exchange halves: the first of a pair of stores takes rows 0 - 7 and 32
   // columns, the second rows 8 - 15.
   const int v0 = m0 + wm * 64 + (frow & 7), nb = n0 + wn * 128 + 16 * (frow >> 3) + 4 * fq;
+  if (BF16_OUT) {
+    // 16 bytes per lane; of a pair of them, lanes frow < 8 and frow >= 8 exchange one, and a store covers 8 rows x 128 bytes
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const u32x4_any a = eight_bf16(acc[i][4 * q], acc[i][4 * q + 1]), b = eight_bf16(acc[i][4 * q + 2], acc[i][4 * q + 3]);
+        const int n = n0 + wn * 128 + (4 * q + 2 * (frow >> 3) + (fq & 1)) * 16 + 8 * (fq >> 1);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          u32x4_any x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = half == 0 ? (uint32_t)__builtin_amdgcn_update_dpp((int)a[e], (int)b[e], 0x128, 0xf, 0xc, false)
+                             : (uint32_t)__builtin_amdgcn_update_dpp((int)b[e], (int)a[e], 0x128, 0xf, 0x3, false);
+          const int v = v0 + i * 16 + 8 * half;
+          uint16_t* const at = reinterpret_cast<uint16_t*>(p.dW) + (int64_t)v * p.d + n;
+          if (v < p.V && n < p.d) {
+            if (p.streaming) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_any*>(at)); else *reinterpret_cast<u32x4_any*>(at) = x;
+          }
+        }
+      }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f32x4 x[8], old[8];
@@ -1540,12 +1575,6 @@ template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_b
         x[j][e] = __int_as_float((j & 1) == 0 ? __builtin_amdgcn_update_dpp(ia, ib, 0x128, 0xf, 0xc, false)
                                               : __builtin_amdgcn_update_dpp(ib, ia, 0x128, 0xf, 0x3, false));
       }
-    }
-    if (BF16_OUT) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (ok[j]) *reinterpret_cast<u32x2_any*>(reinterpret_cast<uint16_t*>(p.dW) + (at[j] - p.dW)) = four_bf16(x[j]);
-      continue;
     }
     if (!p.overwrite) {
 #pragma unroll
@@ -1958,7 +1987,7 @@ void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldh
   p.tail_part = tail_part;
   if (in_blocks) {
     p.N = (int)ldht;                                  // (rows of a block: d rounded up to 128)
-    p.streaming = d % 32 == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
+    p.streaming = d % (dw_bf16 ? 64 : 32) == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
     static LdsLimit lds_limit[2];
     const auto kernel = dw_bf16 ? &dw_few_bf16<true> : &dw_few_bf16<false>;
     lds_limit[dw_bf16].ensure(reinterpret_cast<const void*>(kernel), D_LDS);

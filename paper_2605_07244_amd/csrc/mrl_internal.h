@@ -259,6 +259,7 @@ void launch_distill_targets(const DistillArgs& a, hipStream_t stream);
 void launch_distill_logits(const DistillArgs& a, hipStream_t stream);
 // bf16 path, behind it: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S q / m.
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream);
+int distill_row_blocks(int chunk_rows);
 // fp32 path: divergence, and dz in the place of the pass's logits.
 void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream);
 int distill_f32_blocks(int64_t rows);

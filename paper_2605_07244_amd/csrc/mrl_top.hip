@@ -16,6 +16,7 @@ namespace mrl {
 namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kWavesAtOnce = 8;                        // per SIMD: four workgroups to a compute unit
 constexpr int kPer = 16;                               // logits of a thread in a tile
 constexpr int kTileLogits = kThreads * kPer;
 constexpr int kMostTop = 256;                          // alternatives of a call at most (the bound needs as many threads)
@@ -100,7 +101,7 @@ struct Shared {
 
 // A lower bound of the k-th largest of the threads' numbers sh.maxima, exact in its upper kBoundBits bits, by bisection in the first wave.  0: fewer than k
 // are above 0.  Ends with a barrier.
-constexpr int kBoundBits = 20;
+constexpr int kBoundBits = 16;
 __device__ inline void find_bound(Shared& sh, int k) {
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -123,7 +124,7 @@ __device__ inline void find_bound(Shared& sh, int k) {
 __device__ inline void sort_best(Shared& sh, int k) {
   __syncthreads();
   int n = (int)sh.count;
-  if (n > kThreads) {
+  if (n > 2 * k && n > 64) {
     // fewer of them: those that reach the k-th largest of the threads' maxima
     uint64_t own[kKeys / kThreads];
     uint32_t most = 0;
@@ -165,11 +166,13 @@ template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const
   uint64_t prefix = 0;
   uint32_t above = 0;                                  // keys above the prefix: fewer than k
   int level = 0;
+#pragma unroll 1                                       // (rare: registers count for more than its loops' speed)
   for (;; ++level) {
     const int shift = kShift[level], bits = kBits[level];
     __syncthreads();
     for (int i = threadIdx.x; i < 4096; i += kThreads) hist[i] = 0;
     __syncthreads();
+#pragma unroll 1
     for (int v = begin + threadIdx.x; v < end; v += kThreads) {
       const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
       if (key >> (shift + bits) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
@@ -205,6 +208,7 @@ template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const
   __syncthreads();
   if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
+#pragma unroll 1
   for (int v = begin + threadIdx.x; v < end; v += kThreads) {
     const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
     if (key >= least) sh.keys[atomicAdd(&sh.count, 1u)] = key;
@@ -219,25 +223,28 @@ __device__ inline Part join(const Part& a, const Part& b) {
   return {m2, ca * a.S + cb * b.S, ca * fmaf(a.S, da, a.E) + cb * fmaf(b.S, db, b.E)};
 }
 // All threads' as one, in a fixed order; known to all.
-__device__ inline Part join_all(Shared& sh, Part p) {
+template <int kLanes> __device__ inline Part join_lanes(Part p) {
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
+  for (int off = 1; off < kLanes; off <<= 1) {
     const Part o = {__shfl_xor(p.m2, off), __shfl_xor(p.S, off), __shfl_xor(p.E, off)};
     p = threadIdx.x & off ? join(o, p) : join(p, o);
   }
+  return p;
+}
+__device__ inline Part join_all(Shared& sh, Part p) {
+  p = join_lanes<64>(p);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) { float* w = sh.wave[threadIdx.x >> 6]; w[0] = p.m2; w[1] = p.S; w[2] = p.E; }
   __syncthreads();
-  p = {sh.wave[0][0], sh.wave[0][1], sh.wave[0][2]};
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) p = join(p, {sh.wave[w][0], sh.wave[w][1], sh.wave[w][2]});
-  return p;
+  const float* w = sh.wave[threadIdx.x & (kWaves - 1)];
+  return join_lanes<kWaves>({w[0], w[1], w[2]});
 }
 
 // Sums of a row that the pass has none for: its largest logit is NaN, infinite, or so low that m s2 is not finite.  Two passes, the differences to the
 // largest logit first.  S is NaN where there is no distribution.
 template <bool kBf16> __device__ inline void careful_sums(Shared& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
   uint32_t most = 0;
+#pragma unroll 1
   for (int v = threadIdx.x; v < a.V; v += kThreads) most = larger(most, ordered(logit_at<kBf16>(row, v)));
   most = lanes_max<64>(most);
   __syncthreads();
@@ -249,6 +256,7 @@ template <bool kBf16> __device__ inline void careful_sums(Shared& sh, const TopA
   offset = 0; S = __builtin_nanf(""); E = 0.f;
   if (!(fabsf(m) < INFINITY)) return;
   Part p = {0.f, 0.f, 0.f};
+#pragma unroll 1
   for (int v = threadIdx.x; v < a.V; v += kThreads) {
     const float u = (logit_at<kBf16>(row, v) - m) * a.s2, e = __builtin_amdgcn_exp2f(u);
     p.S += e;
@@ -292,7 +300,7 @@ __device__ inline void put_masked_row(const TopArgs& a, int64_t n) {
   }
 }
 
-template <bool kBf16> __global__ __launch_bounds__(kThreads) void k_top(TopArgs a) {
+template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void k_top(TopArgs a) {
   __shared__ Shared sh;
   const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, n = item / a.split;
   if (n >= a.N) return;
