@@ -189,7 +189,7 @@ _HOST = None
 
 class _NoHost:
     """Takes nothing as it is: every call goes through ctypes."""
-    advantages = align = rms_norm = rms_norm_backward = grad_norm = adamw = staticmethod(lambda *args: None)
+    advantages = align = rms_norm = rms_norm_backward = grad_norm = adamw = top_logprobs = embedding = embedding_backward = distill = staticmethod(lambda *args: None)
 
 
 def _load_host():
@@ -205,7 +205,7 @@ def _load_host():
         why = f"was built against torch {module.torch_version}, this is {torch.__version__}"
     except (ImportError, OSError) as e:        # (a file that is not there is an ImportError or FileNotFoundError)
         why = str(e)
-    warnings.warn(f"{path}: {why}; advantages, alignment, norms and updates go through ctypes, which takes 2 - 6 us more a call "
+    warnings.warn(f"{path}: {why}; all but the scoring and GRPO calls go through ctypes, which takes 2 - 6 us more a call "
                   "(`python -m paper_2605_07244_amd.build` builds it)", RuntimeWarning, stacklevel=4)
     return None
 
@@ -413,6 +413,14 @@ def distill_loss_fwd_bwd(hidden, lm_head_w, teacher_ids, teacher_logp, cfg: Dist
                          want_dH=True, want_dW=True, workspace=None, out_kl=None, out_stats=None):
     """mrl_distill_loss_fwd_bwd: dict(kl [N], dH, dW, stats) of hidden [N, d] and a teacher's alternatives, ids [N, k] int32 and log-probs [N, k] float32 (those of
     top_logprobs, at cfg.temperature); `read_distill_stats` turns the device stats block into a Python dict (synchronises)."""
+    if (_native and out_dH is None and out_dW is None and workspace is None and out_kl is None and out_stats is None and not cfg.accumulate_dw
+            and type(hidden) is torch.Tensor and hidden.is_cuda):
+        dev = _get_device()
+        r = (_HOST or _host()).distill(hidden, lm_head_w, teacher_ids, teacher_logp, token_mask, row_weight, cfg.temperature, cfg.renormalize, cfg.dh_dtype,
+                                       cfg.dw_dtype, cfg.chunk_rows, want_dH, want_dW, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_distill_loss_fwd_bwd")
+            return dict(kl=r[1], dH=r[2], dW=r[3], stats=r[4])
     if hidden.dim() != 2 or lm_head_w.dim() != 2 or teacher_ids.dim() != 2:
         raise ValueError("hidden must be [N, d], lm_head_w [V, d] and teacher_ids [N, k]")
     N, d = hidden.shape
@@ -787,6 +795,12 @@ def _rows(t, n, name):
 def top_logprobs(logits, k, target_ids=None, token_mask=None, temperature=1.0, want_lse=True, want_entropy=True, workspace=None):
     """mrl_top_logprobs of logits [N, V], float32 or bfloat16, whose rows may lie apart (a slice of wider rows): dict(ids [N, k] int32, top_logp [N, k],
     logp [N] of target_ids, lse [N], entropy [N]), with None for what is not asked for; ids and top_logp are None with k = 0."""
+    if _native and workspace is None and type(logits) is torch.Tensor and logits.is_cuda:
+        dev = _get_device()
+        r = (_HOST or _host()).top_logprobs(logits, k, target_ids, token_mask, temperature, want_lse, want_entropy, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_top_logprobs")
+            return dict(ids=r[1], top_logp=r[2], logp=r[3], lse=r[4], entropy=r[5])
     if logits.dim() != 2:
         raise ValueError("logits must be [N, V]")
     N, V = logits.shape
@@ -814,6 +828,12 @@ def top_logprobs(logits, k, target_ids=None, token_mask=None, temperature=1.0, w
 
 def embedding(table, ids, scale=1.0, token_mask=None, out_dtype=None, out=None):
     """mrl_embedding: scale * table[ids], [N, d] in out_dtype (None: the type of table), of ids [N] int32.  Ids outside the table, and tokens with mask 0, give zero rows."""
+    if _native and out is None and type(table) is torch.Tensor and table.is_cuda:
+        dev = _get_device()
+        r = (_HOST or _host()).embedding(table, ids, scale, token_mask, table.dtype if out_dtype is None else out_dtype, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_embedding")
+            return r[1]
     if table.dim() != 2 or ids.dim() != 1:
         raise ValueError("table must be [V, d] and ids [N]")
     V, d = table.shape
@@ -839,6 +859,12 @@ def embedding(table, ids, scale=1.0, token_mask=None, out_dtype=None, out=None):
 def embedding_backward(dy, ids, V, scale=1.0, token_mask=None, out_dtype=None, out=None, accumulate=False, workspace=None):
     """mrl_embedding_backward: the gradient [V, d] of the table of an embedding whose output's gradient is dy [N, d], in out_dtype (None: float32).  accumulate
     adds into out (float32), the gradient of a head that shares the table, say; without it every row of out is written."""
+    if _native and out is None and workspace is None and not accumulate and type(dy) is torch.Tensor and dy.is_cuda:
+        dev = _get_device()
+        r = (_HOST or _host()).embedding_backward(dy, ids, V, scale, token_mask, torch.float32 if out_dtype is None else out_dtype, dev, _raw_stream(dev))
+        if r is not None:
+            _check(r[0], "mrl_embedding_backward")
+            return r[1]
     if dy.dim() != 2 or ids.dim() != 1:
         raise ValueError("dy must be [N, d] and ids [N]")
     N, d = dy.shape

@@ -281,6 +281,177 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
 }
 
+// Tensors of one int32 or float for each of N rows, or None.
+bool rows_arg(PyObject* o, at::ScalarType type, int64_t device, int64_t N, bool optional, void** p) {
+  if (!tensor_arg(o, type, optional, p)) return false;
+  return o == Py_None || (THPVariable_Unpack(o).numel() == N && THPVariable_Unpack(o).get_device() == device);
+}
+bool flag_arg(PyObject* o, bool* v) {
+  *v = o == Py_True;
+  return o == Py_True || o == Py_False;
+}
+bool float_dtype(PyObject* o, at::ScalarType* type, int32_t* code) {
+  if (!THPDtype_Check(o)) return false;
+  *type = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  *code = *type == at::kBFloat16 ? MRL_BF16 : MRL_F32;
+  return *type == at::kFloat || *type == at::kBFloat16;
+}
+template <class T> T* data_or_null(const at::Tensor& t) { return t.defined() ? static_cast<T*>(t.mutable_data_ptr()) : nullptr; }
+
+// (logits, k, target_ids, token_mask, temperature, want_lse, want_entropy, device, stream) -> (status, ids, top_logp, logp, lse, entropy) or None
+PyObject* top_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    int64_t device, stream;
+    int32_t k, type;
+    float temperature;
+    bool want_lse, want_entropy;
+    if (n != 9 || !int_arg(a[7], &device) || !int_arg(a[8], &stream) || !THPVariable_CheckExact(a[0]) || !int32_arg(a[1], &k) || !float_arg(a[4], &temperature) ||
+        !flag_arg(a[5], &want_lse) || !flag_arg(a[6], &want_entropy))
+      Py_RETURN_NONE;
+    const at::Tensor& z = THPVariable_Unpack(a[0]);
+    if (!z.is_cuda() || z.get_device() != device || z.dim() != 2 || z.numel() == 0 || z.size(1) > INT32_MAX) Py_RETURN_NONE;
+    if (z.scalar_type() == at::kBFloat16) type = MRL_BF16;
+    else if (z.scalar_type() == at::kFloat) type = MRL_F32;
+    else Py_RETURN_NONE;
+    const int64_t N = z.size(0), V = z.size(1);
+    void *targets, *mask;
+    if ((V > 1 && z.stride(1) != 1) || (N > 1 && z.stride(0) < V) || k < 0 || k > V || !rows_arg(a[2], at::kInt, device, N, true, &targets) ||
+        !rows_arg(a[3], at::kByte, device, N, true, &mask))
+      Py_RETURN_NONE;
+    const size_t bytes = mrl_top_logprobs_workspace(N, (int32_t)V, k);
+    if (bytes == 0) Py_RETURN_NONE;
+    at::Tensor ids, top, logp, lse, entropy, ws;
+    if (k > 0) { ids = new_like(z, {N, k}, at::kInt); top = new_like(z, {N, k}, at::kFloat); }
+    if (targets != nullptr) logp = new_like(z, {N}, at::kFloat);
+    if (want_lse) lse = new_like(z, {N}, at::kFloat);
+    if (want_entropy) entropy = new_like(z, {N}, at::kFloat);
+    if (bytes > 256) ws = new_like(z, {(int64_t)bytes}, at::kByte);
+    const void* zp = z.const_data_ptr();
+    int32_t* const ids_ptr = data_or_null<int32_t>(ids);
+    float *const top_ptr = data_or_null<float>(top), *const logp_ptr = data_or_null<float>(logp), *const lse_ptr = data_or_null<float>(lse);
+    float* const entropy_ptr = data_or_null<float>(entropy);
+    void* const ws_ptr = data_or_null<void>(ws);
+    const int64_t stride = N > 1 ? z.stride(0) : V;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_top_logprobs(zp, stride, static_cast<int32_t*>(targets), static_cast<uint8_t*>(mask), N, (int32_t)V, k, type, temperature, ids_ptr, top_ptr, logp_ptr,
+                          lse_ptr, entropy_ptr, ws_ptr, ws_ptr != nullptr ? bytes : 0, reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iNNNNN)", rc, THPVariable_Wrap(std::move(ids)), THPVariable_Wrap(std::move(top)), THPVariable_Wrap(std::move(logp)),
+                         THPVariable_Wrap(std::move(lse)), THPVariable_Wrap(std::move(entropy)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// (table, ids, scale, token_mask, out_dtype, device, stream) -> (status, y) or None
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    const at::Tensor* table;
+    int64_t device, stream;
+    int32_t tt, yt;
+    float scale;
+    void *ids, *mask;
+    at::ScalarType out;
+    if (n != 7 || !int_arg(a[5], &device) || !int_arg(a[6], &stream) || !typed_arg(a[0], device, &table, &tt) || !float_arg(a[2], &scale) ||
+        !float_dtype(a[4], &out, &yt) || table->dim() != 2 || table->numel() == 0 || table->size(0) > INT32_MAX || table->size(1) > INT32_MAX ||
+        !THPVariable_CheckExact(a[1]))
+      Py_RETURN_NONE;
+    const at::Tensor& which = THPVariable_Unpack(a[1]);
+    const int64_t N = which.numel(), V = table->size(0), d = table->size(1);
+    if (N == 0 || which.dim() != 1 || !rows_arg(a[1], at::kInt, device, N, false, &ids) || !rows_arg(a[3], at::kByte, device, N, true, &mask)) Py_RETURN_NONE;
+    at::Tensor y = new_like(*table, {N, d}, out);
+    const void* tp = table->const_data_ptr();
+    void* const yp = y.mutable_data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_embedding(tp, static_cast<int32_t*>(ids), static_cast<uint8_t*>(mask), N, (int32_t)d, (int32_t)V, scale, tt, yt, yp, reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(std::move(y)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// (dy, ids, V, scale, token_mask, out_dtype, device, stream) -> (status, gradient) or None
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    const at::Tensor* dy;
+    int64_t device, stream;
+    int32_t yt, ot, V;
+    float scale;
+    void *ids, *mask;
+    at::ScalarType out;
+    if (n != 8 || !int_arg(a[6], &device) || !int_arg(a[7], &stream) || !typed_arg(a[0], device, &dy, &yt) || !int32_arg(a[2], &V) || !float_arg(a[3], &scale) ||
+        !float_dtype(a[5], &out, &ot) || dy->dim() != 2 || dy->numel() == 0 || dy->size(1) > INT32_MAX || V <= 0 || !THPVariable_CheckExact(a[1]))
+      Py_RETURN_NONE;
+    const int64_t N = dy->size(0), d = dy->size(1);
+    if (THPVariable_Unpack(a[1]).dim() != 1 || !rows_arg(a[1], at::kInt, device, N, false, &ids) || !rows_arg(a[4], at::kByte, device, N, true, &mask)) Py_RETURN_NONE;
+    const size_t bytes = mrl_embedding_backward_workspace(N, (int32_t)d, V);
+    if (bytes == 0) Py_RETURN_NONE;
+    at::Tensor table = new_like(*dy, {V, d}, out), ws = new_like(*dy, {(int64_t)bytes}, at::kByte);
+    const void* dyp = dy->const_data_ptr();
+    void *const tp = table.mutable_data_ptr(), *const wsp = ws.mutable_data_ptr();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_embedding_backward(dyp, static_cast<int32_t*>(ids), static_cast<uint8_t*>(mask), N, (int32_t)d, V, scale, yt, ot, 0, tp, wsp, bytes,
+                                reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iN)", rc, THPVariable_Wrap(std::move(table)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
+// (hidden, lm_head_w, teacher_ids, teacher_logp, token_mask, row_weight, temperature, renormalize, dh_dtype, dw_dtype, chunk_rows, want_dH, want_dW, device, stream)
+// -> (status, kl, dH, dW, stats) or None
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    const at::Tensor *h, *w;
+    int64_t device, stream;
+    int32_t ht, wt;
+    mrl_distill_config c = {};
+    void *mask, *weight, *ids, *logp;
+    bool want_dH, want_dW;
+    if (n != 15 || !int_arg(a[13], &device) || !int_arg(a[14], &stream) || !typed_arg(a[0], device, &h, &ht) || !typed_arg(a[1], device, &w, &wt) || ht != wt ||
+        !float_arg(a[6], &c.temperature) || !int32_arg(a[7], &c.renormalize) || !int32_arg(a[8], &c.dh_dtype) || !int32_arg(a[9], &c.dw_dtype) ||
+        !int32_arg(a[10], &c.chunk_rows) || !flag_arg(a[11], &want_dH) || !flag_arg(a[12], &want_dW) || h->dim() != 2 || w->dim() != 2 || h->numel() == 0 ||
+        w->numel() == 0 || h->size(1) != w->size(1) || h->size(1) > INT32_MAX || w->size(0) > INT32_MAX || !tensor_arg(a[2], at::kInt, false, &ids) ||
+        !tensor_arg(a[3], at::kFloat, false, &logp))
+      Py_RETURN_NONE;
+    const at::Tensor &ti = THPVariable_Unpack(a[2]), &tl = THPVariable_Unpack(a[3]);
+    const int64_t N = h->size(0), d = h->size(1), V = w->size(0);
+    if (ti.dim() != 2 || ti.size(0) != N || ti.size(1) > INT32_MAX || !same_rows(ti, tl) || ti.get_device() != device || tl.get_device() != device ||
+        !rows_arg(a[4], at::kByte, device, N, true, &mask) || !rows_arg(a[5], at::kFloat, device, N, true, &weight) ||
+        (c.dh_dtype != MRL_F32 && c.dh_dtype != MRL_BF16) || (c.dw_dtype != MRL_F32 && c.dw_dtype != MRL_BF16))
+      Py_RETURN_NONE;
+    const int32_t k = (int32_t)ti.size(1);
+    const size_t bytes = mrl_distill_loss_workspace(N, (int32_t)d, (int32_t)V, k, ht, &c);
+    if (bytes == 0) Py_RETURN_NONE;
+    at::Tensor kl = new_like(*h, {N}, at::kFloat), dH, dW, stats = new_like(*h, {(int64_t)sizeof(mrl_distill_stats)}, at::kByte);
+    if (want_dH) dH = new_like(*h, {N, d}, c.dh_dtype == MRL_BF16 ? at::kBFloat16 : at::kFloat);
+    if (want_dW) dW = new_like(*h, {V, d}, c.dw_dtype == MRL_BF16 ? at::kBFloat16 : at::kFloat);
+    at::Tensor ws = new_like(*h, {(int64_t)bytes}, at::kByte);
+    const void *hp = h->const_data_ptr(), *wp = w->const_data_ptr();
+    float* const klp = static_cast<float*>(kl.mutable_data_ptr());
+    void *const dHp = data_or_null<void>(dH), *const dWp = data_or_null<void>(dW), *const wsp = ws.mutable_data_ptr();
+    mrl_distill_stats* const sp = static_cast<mrl_distill_stats*>(stats.mutable_data_ptr());
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = mrl_distill_loss_fwd_bwd(hp, wp, static_cast<int32_t*>(ids), static_cast<float*>(logp), static_cast<uint8_t*>(mask), static_cast<float*>(weight), N,
+                                  (int32_t)d, (int32_t)V, k, ht, &c, klp, dHp, dWp, sp, wsp, bytes, reinterpret_cast<void*>(stream));
+    Py_END_ALLOW_THREADS
+    return Py_BuildValue("(iNNNN)", rc, THPVariable_Wrap(std::move(kl)), THPVariable_Wrap(std::move(dH)), THPVariable_Wrap(std::move(dW)),
+                         THPVariable_Wrap(std::move(stats)));
+  } catch (...) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+}
+
 PyMethodDef methods[] = {
     {"advantages", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(advantages)), METH_FASTCALL, nullptr},
     {"align", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(align)), METH_FASTCALL, nullptr},
@@ -288,6 +459,10 @@ PyMethodDef methods[] = {
     {"rms_norm_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rms_norm_backward)), METH_FASTCALL, nullptr},
     {"grad_norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(grad_norm)), METH_FASTCALL, nullptr},
     {"adamw", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw)), METH_FASTCALL, nullptr},
+    {"top_logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(top_logprobs)), METH_FASTCALL, nullptr},
+    {"embedding", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding)), METH_FASTCALL, nullptr},
+    {"embedding_backward", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(embedding_backward)), METH_FASTCALL, nullptr},
+    {"distill", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(distill)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "mrl_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
