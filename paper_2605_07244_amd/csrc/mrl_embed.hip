@@ -87,6 +87,7 @@ __device__ inline uint32_t rank_items(SortShared& sh, const int (&digit)[kRounds
 #pragma unroll
   for (int r = 0; r < kRounds; ++r) {
     unsigned long long same = __ballot(valid[r]);
+    if (same == 0) continue;
 #pragma unroll
     for (int b = 0; b < kDigitBits; ++b) {
       const bool bit = (digit[r] >> b) & 1;
@@ -124,7 +125,9 @@ __device__ inline uint32_t before_digit(SortShared& sh, uint32_t x) {
   __syncthreads();
   if ((threadIdx.x & 63) == 63) sh.sums[threadIdx.x >> 6] = incl;
   __syncthreads();
-  for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) incl += sh.sums[w];
+  const uint32_t wave_sum = sh.sums[threadIdx.x & (kSortWaves - 1)];
+#pragma unroll
+  for (int w = 0; w < kDigits / 64; ++w) incl += w < (int)(threadIdx.x >> 6) ? __builtin_amdgcn_readlane(wave_sum, w) : 0;
   return incl - x;
 }
 
@@ -187,16 +190,26 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass
   }
 }
 
-// All of it for at most kItems tokens; the result in key_a, at_a.
-__global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs a) {
+// 16 bytes of zeros per thread and step over `bytes` (a multiple of 2) from `out`, by workgroups `first` .. of `count`.
+__device__ inline void fill_zeros(void* out, int64_t bytes, int64_t block, int64_t blocks) {
+  char* const p = static_cast<char*>(out);
+  const int64_t step = blocks * (kSortThreads * 16);
+  for (int64_t o = (block * kSortThreads + threadIdx.x) * 16; o < bytes; o += step) {
+    if (o + 16 <= bytes) {
+      store_any<2>(p + o, u32x4{0, 0, 0, 0});
+    } else {
+      for (int64_t e = o; e < bytes; e += 2) *reinterpret_cast<uint16_t*>(p + e) = 0;
+    }
+  }
+}
+
+// All of it for at most kItems tokens, by the first workgroup; the result in key_a, at_a.  The others clear the table meanwhile, all of it: the few rows that tokens
+// occur in are written twice, which costs less than the sort does (3001 tokens, 32000 x 713 floats FEW).
+__global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs a, void* out, int64_t out_bytes) {
   __shared__ SortShared sh;
   __shared__ int32_t keys[kItems], ats[kItems];
+  if (blockIdx.x > 0) { fill_zeros(out, out_bytes, blockIdx.x - 1, gridDim.x - 1); return; }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (a.used != nullptr) {
-    clear_marks(a, threadIdx.x, kSortThreads);
-    __threadfence();
-    __syncthreads();                                      // (the marks come behind the zeros)
-  }
   int key[kRounds], at[kRounds], digit[kRounds], place[kRounds];
   bool valid[kRounds];
 #pragma unroll
@@ -205,7 +218,6 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs a) {
     valid[r] = n < a.N;
     at[r] = n;
     key[r] = valid[r] ? key_of(a, n) : a.V;               // (no tokens at all: no ids either)
-    if (a.used != nullptr && valid[r] && key[r] < a.V) a.used[key[r]] = 1;
   }
   for (int pass = 0; pass < a.passes; ++pass) {
     const int shift = pass * kDigitBits;
@@ -267,13 +279,18 @@ template <bool kBf16> __global__ __launch_bounds__(256) void k_embedding_sum(Sum
   const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (block >= a.sum_blocks) {
     // rows of tokens that do not occur
-    if (a.used == nullptr) return;
     for (int k = 0; k < kZeroRows; ++k) {
       const int64_t v = (block - a.sum_blocks) * kZeroRows + k;
       if (v >= a.V || a.used[v] != 0) continue;
-      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      char* row = static_cast<char*>(a.out) + v * a.d * (a.out_bf16 ? 2 : 4);
-      for (int c = threadIdx.x * 8; c < a.d; c += 256 * 8) store_eight(row, a.out_bf16, Columns(c, a.d), a.d, zero);
+      const int bytes = a.d * (a.out_bf16 ? 2 : 4);
+      char* row = static_cast<char*>(a.out) + v * bytes;
+      for (int o = threadIdx.x * 16; o < bytes; o += 256 * 16) {
+        if (o + 16 <= bytes) {
+          store_any<2>(row + o, u32x4{0, 0, 0, 0});
+        } else {
+          for (int e = o; e < bytes; e += 2) *reinterpret_cast<uint16_t*>(row + e) = 0;
+        }
+      }
     }
     return;
   }
@@ -323,38 +340,52 @@ template <bool kBf16> __global__ __launch_bounds__(256) void k_embedding_sum(Sum
   }
 }
 
-// Tokens that reach over several chunks: the chunk where one begins adds the partial sums behind its own.
+// Tokens that reach over several chunks: the chunk where one begins adds the partial sums behind its own, four waves a quarter of them each.
 __global__ __launch_bounds__(256) void k_embedding_join(SumArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t task = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = task / a.tiles;
+  __shared__ float4 sh[4][2][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t task = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, c = task / a.tiles;
   const int64_t last = (c + 1) * a.chunk;                 // behind the chunk
   if (c >= a.chunks || last >= a.N) return;
-  const int id = a.key[last - 1];
-  if (id >= a.V || a.key[last] != id || (c > 0 && a.key[c * a.chunk - 1] == id)) return;
+  const int id = a.key[last - 1], next = a.key[last], prev = c > 0 ? a.key[c * a.chunk - 1] : -1;
+  if (id >= a.V || next != id || prev == id) return;
   const int tile = (int)(task - c * a.tiles), col = tile * kTileColumns + lane * 8;
   const int64_t ld = (int64_t)a.tiles * kTileColumns;
-  float acc[8];
-  const float* p = a.parts + (c * 2 + 1) * ld + col;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = p[e];
   // the chunks whose first token it is, 64 of them looked up at a time
+  int64_t m = 0;
   for (int64_t j0 = c + 1; j0 < a.chunks; j0 += 64) {
     const int64_t j = j0 + lane;
     const unsigned long long same = __ballot(j < a.chunks && a.key[(j < a.chunks ? j : c) * a.chunk] == id);
-    const int m = same == ~0ull ? 64 : __builtin_ctzll(~same);
-#pragma unroll 16
-    for (int i = 0; i < m; ++i) {
-      const float* q = a.parts + (j0 + i) * 2 * ld + col;
-      const float4 lo = *reinterpret_cast<const float4*>(q), hi = *reinterpret_cast<const float4*>(q + 4);
-      acc[0] += lo.x; acc[1] += lo.y; acc[2] += lo.z; acc[3] += lo.w;
-      acc[4] += hi.x; acc[5] += hi.y; acc[6] += hi.z; acc[7] += hi.w;
-    }
-    if (m < 64) break;
+    m += same == ~0ull ? 64 : __builtin_ctzll(~same);
+    if (same != ~0ull) break;
   }
-  if (col < a.d) put(a, id, Columns(col, a.d), acc);
+  // part 0 is the chunk's own
+  const int64_t per = (m + 1 + 3) / 4, i0 = wave * per, i1 = i0 + per < m + 1 ? i0 + per : m + 1;
+  float4 lo = make_float4(0.f, 0.f, 0.f, 0.f), hi = lo;
+#pragma unroll 8
+  for (int64_t i = i0; i < i1; ++i) {
+    const float* q = a.parts + ((c + i) * 2 + (i == 0)) * ld + col;
+    const float4 x = *reinterpret_cast<const float4*>(q), y = *reinterpret_cast<const float4*>(q + 4);
+    lo.x += x.x; lo.y += x.y; lo.z += x.z; lo.w += x.w;
+    hi.x += y.x; hi.y += y.y; hi.z += y.z; hi.w += y.w;
+  }
+  sh[wave][0][lane] = lo;
+  sh[wave][1][lane] = hi;
+  __syncthreads();
+  if (wave != 0 || col >= a.d) return;
+  float acc[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float4 s = sh[0][h][lane];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) { const float4 x = sh[w][h][lane]; s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w; }
+    acc[4 * h] = s.x; acc[4 * h + 1] = s.y; acc[4 * h + 2] = s.z; acc[4 * h + 3] = s.w;
+  }
+  put(a, id, Columns(col, a.d), acc);
 }
 
 // ----------------------------------------------------------------------------
+constexpr int64_t kFillBytes = 16 * kSortThreads * 4, kMostFill = 2048;      // of a workgroup of k_sort_few, or more where that makes too many of them
 constexpr int64_t kMostRows = (int64_t)1 << 30, kMostWide = 1 << 21;
 constexpr int kMostColumns = 1 << 20, kMostIds = 1 << 24;
 dim3 grid_of(int64_t groups) {
@@ -434,12 +465,15 @@ extern "C" int mrl_embedding_backward(const void* dy, const int32_t* ids, const 
   hipStream_t s = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   auto at = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
-  uint8_t* const used = accumulate ? nullptr : ws + L.used;
+  const bool few = N <= kItems;
+  uint8_t* const used = accumulate || few ? nullptr : ws + L.used;
   const SortArgs sort = {ids, token_mask, N, V, L.blocks, L.passes, at(L.key_a), at(L.at_a), at(L.key_b), at(L.at_b),
                          reinterpret_cast<uint32_t*>(ws + L.counts), used};
   bool in_a = true;
-  if (N <= kItems) {
-    hipLaunchKernelGGL(k_sort_few, dim3(1), dim3(kSortThreads), 0, s, sort);
+  if (few) {
+    const int64_t bytes = (int64_t)V * d * (out_dtype == MRL_BF16 ? 2 : 4), fill = accumulate ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
+    hipLaunchKernelGGL(k_sort_few, dim3((unsigned)(1 + (fill < kMostFill ? fill : kMostFill))), dim3(kSortThreads), 0, s, sort, out_dtable, bytes);
+    if (N == 0) return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
   } else {
     for (int p = 0; p < L.passes; ++p) {
       hipLaunchKernelGGL(k_sort_count, dim3(L.blocks), dim3(kSortThreads), 0, s, sort, p);
@@ -447,10 +481,10 @@ extern "C" int mrl_embedding_backward(const void* dy, const int32_t* ids, const 
     }
     in_a = L.passes % 2 == 1;
   }
-  const int64_t sum_blocks = N > 0 ? (L.chunks * L.tiles + 3) / 4 : 0, zero_blocks = accumulate ? 0 : ((int64_t)V + kZeroRows - 1) / kZeroRows;
+  const int64_t sum_blocks = N > 0 ? (L.chunks * L.tiles + 3) / 4 : 0, zero_blocks = used == nullptr ? 0 : ((int64_t)V + kZeroRows - 1) / kZeroRows;
   const SumArgs a = {dy, in_a ? sort.key_a : sort.key_b, in_a ? sort.at_a : sort.at_b, used, N, L.chunks, d, V, L.chunk, L.tiles, scale, accumulate,
                      out_dtype == MRL_BF16, out_dtable, reinterpret_cast<float*>(ws + L.parts), sum_blocks};
   hipLaunchKernelGGL(dy_dtype == MRL_BF16 ? k_embedding_sum<true> : k_embedding_sum<false>, grid_of(sum_blocks + zero_blocks), dim3(256), 0, s, a);
-  if (N > L.chunk) hipLaunchKernelGGL(k_embedding_join, grid_of(sum_blocks), dim3(256), 0, s, a);
+  if (N > L.chunk) hipLaunchKernelGGL(k_embedding_join, grid_of(L.chunks * L.tiles), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
 }
