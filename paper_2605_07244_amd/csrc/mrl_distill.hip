@@ -254,9 +254,9 @@ template <int kEach> __global__ __launch_bounds__(EPI_THREADS) void k_distill_ro
 }
 
 // ----------------------------------------------------------------------------
-// fp32: a wave per row of the materialised logits, which become dz.
+// fp32: a wave per row of the materialised logits, which become dz.  Up to 64 kHeld logits stay in registers between the three looks at them.
 // ----------------------------------------------------------------------------
-template <int kEach> __global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
+template <int kEach, int kHeld> __global__ __launch_bounds__(256) void k_distill_f32(DistillArgs a) {
   __shared__ double parts[4][kDistillSums];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x * 4 + wave;
@@ -265,23 +265,33 @@ template <int kEach> __global__ __launch_bounds__(256) void k_distill_f32(Distil
     const int64_t slot = a.row_index[a.chunk_start + r];
     float* const row = a.Z + (int64_t)r * a.ldz;
     const float w = weight_of(a, slot), inv_T = 1.f / a.temperature;
-    float mx = -INFINITY;
-    for (int v = lane; v < a.V; v += 64) mx = fmaxf(mx, row[v]);
-    mx = wave_max(mx);
-    float s = 0.f;
-    for (int v = lane; v < a.V; v += 64) s += expf((row[v] - mx) * inv_T);
-    const float S = lanes_sum<64>(s);
-    const double log_S = log((double)S);
     Alternatives<kEach> alt;
     alt.load(a, slot);
+    float z[kEach], held[kHeld > 0 ? kHeld : 1];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) z[e] = alt.id[e] >= 0 ? row[alt.id[e]] : 0.f;
+    // f(place in registers, id) for the lane's logits
+    auto each = [&](auto f) {
+      if constexpr (kHeld > 0) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+          if (i * 64 < a.V && i * 64 + lane < a.V) f(held[i], i * 64 + lane);
+      } else {
+        for (int v = lane; v < a.V; v += 64) { held[0] = row[v]; f(held[0], v); }
+      }
+    };
+    float mx = -INFINITY;
+    each([&](float& x, int v) { if (kHeld > 0) x = row[v]; mx = fmaxf(mx, x); });
+    mx = wave_max(mx);
+    float s = 0.f;
+    each([&](float& x, int) { const float e = expf((x - mx) * inv_T); if (kHeld > 0) x = e; s += e; });
+    const float S = lanes_sum<64>(s);
+    const double log_S = log((double)S);
     alt.weigh(a, alt.best_t());
     double kl = 0.0;
-    float z[kEach];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      z[e] = alt.id[e] >= 0 ? row[alt.id[e]] : 0.f;
+    for (int e = 0; e < kEach; ++e)
       if (alt.q[e] != 0.0) kl += alt.q[e] * (alt.log_q[e] - (((double)z[e] - (double)mx) / (double)a.temperature - log_S));
-    }
     kl = wave_sum(kl);
     if (lane == 0) a.out_kl[slot] = (float)kl;
     q[0] = (double)w * kl;
@@ -291,7 +301,7 @@ template <int kEach> __global__ __launch_bounds__(256) void k_distill_f32(Distil
       float total[kEach];
       bool first[kEach];
       alt.by_id(a.k, total, first);
-      for (int v = lane; v < a.V; v += 64) row[v] = scale * expf((row[v] - mx) * inv_T);
+      each([&](float& x, int v) { row[v] = scale * (kHeld > 0 ? x : expf((x - mx) * inv_T)); });
       __threadfence_block();                           // (the places below are other lanes' above)
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
@@ -365,7 +375,9 @@ void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
 int distill_row_blocks(int chunk_rows) { return chunk_rows / kRows; }
 int distill_f32_blocks(int64_t rows) { return (int)((rows + 3) / 4); }
 void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream) {
-  hipLaunchKernelGGL(by_count(a.k, k_distill_f32<1>, k_distill_f32<2>, k_distill_f32<4>), dim3(distill_f32_blocks(rows)), dim3(256), 0, stream, a);
+  const auto kernel = a.V <= 8 * 64 ? by_count(a.k, k_distill_f32<1, 8>, k_distill_f32<2, 8>, k_distill_f32<4, 8>)
+                                    : by_count(a.k, k_distill_f32<1, 0>, k_distill_f32<2, 0>, k_distill_f32<4, 0>);
+  hipLaunchKernelGGL(kernel, dim3(distill_f32_blocks(rows)), dim3(256), 0, stream, a);
 }
 void launch_distill_final(const double* parts, int64_t blocks, const int64_t* n_scored, const int64_t* n_empty, double scale, double* out_d, int64_t* out_i,
                           hipStream_t stream) {

@@ -19,13 +19,14 @@ constexpr int64_t kMostTokens = 1 << 24;                  // of a backward call
 constexpr int kTileColumns = 512;
 
 // ----------------------------------------------------------------------------
-// Lookup: eight columns per thread and vector, kPerThread vectors each.
+// Lookup: eight columns per thread and vector, kPerThread vectors each.  Four of them where they leave as 16 bytes each, one where they leave as 32
+// (32768 tokens, V = 151936, us, four, two and one: 3584 columns bf16 73, 78 and 90; 4096 floats 173, 163 and 149, 713 floats 26.5, 25.4 and 25.0).
 // ----------------------------------------------------------------------------
-constexpr int kLookThreads = 256, kPerThread = 4;
+constexpr int kLookThreads = 256;
 struct LookArgs {
   const void* table; const int32_t* ids; const uint8_t* mask; int64_t N; int d, V, vectors; float scale; int y_bf16; void* y;
 };
-template <bool kBf16> __global__ __launch_bounds__(kLookThreads) void k_embedding(LookArgs a) {
+template <bool kBf16, int kPerThread> __global__ __launch_bounds__(kLookThreads) void k_embedding(LookArgs a) {
   const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (kLookThreads * kPerThread);
   const int64_t n0 = first / a.vectors;                   // (the same for all threads; from there on 32 bits do)
   const int off = (int)(first - n0 * a.vectors);
@@ -190,25 +191,24 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass
   }
 }
 
-// 16 bytes of zeros per thread and step over `bytes` (a multiple of 2) from `out`, by workgroups `first` .. of `count`.
-__device__ inline void fill_zeros(void* out, int64_t bytes, int64_t block, int64_t blocks) {
-  char* const p = static_cast<char*>(out);
-  const int64_t step = blocks * (kSortThreads * 16);
-  for (int64_t o = (block * kSortThreads + threadIdx.x) * 16; o < bytes; o += step) {
-    if (o + 16 <= bytes) {
-      store_any<2>(p + o, u32x4{0, 0, 0, 0});
-    } else {
-      for (int64_t e = o; e < bytes; e += 2) *reinterpret_cast<uint16_t*>(p + e) = 0;
-    }
+// 16 bytes of zeros, as far as they lie before `bytes` (a multiple of 2).
+__device__ inline void zero_16(char* p, int64_t o, int64_t bytes) {
+  if (o + 16 <= bytes) {
+    store_any<2>(p + o, u32x4{0, 0, 0, 0});
+  } else {
+    for (; o < bytes; o += 2) *reinterpret_cast<uint16_t*>(p + o) = 0;
   }
 }
+// Zeros go out as one store per thread and as many workgroups as that makes: 2.5 GB, us, one and four stores per thread of 256: 367 and 418, of 1024: 395 and 443.
+constexpr int64_t kFillBytes = 16 * kSortThreads;
 
 // All of it for at most kItems tokens, by the first workgroup; the result in key_a, at_a.  The others clear the table meanwhile, all of it: the few rows that tokens
-// occur in are written twice, which costs less than the sort does (3001 tokens, 32000 x 713 floats FEW).
+// occur in are written twice, which costs less than the sort does (3001 tokens, 32000 x 713 floats: 47 us with marks of the rows and their zeros behind the sort, 30).
 __global__ __launch_bounds__(kSortThreads) void k_sort_few(SortArgs a, void* out, int64_t out_bytes) {
   __shared__ SortShared sh;
   __shared__ int32_t keys[kItems], ats[kItems];
-  if (blockIdx.x > 0) { fill_zeros(out, out_bytes, blockIdx.x - 1, gridDim.x - 1); return; }
+  const int64_t group = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (group > 0) { zero_16(static_cast<char*>(out), (group - 1) * kFillBytes + threadIdx.x * 16, out_bytes); return; }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int key[kRounds], at[kRounds], digit[kRounds], place[kRounds];
   bool valid[kRounds];
@@ -257,8 +257,9 @@ struct SumArgs {
   int64_t N, chunks; int d, V, chunk /*tokens*/, tiles /*of columns*/; float scale; int accumulate, out_bf16; void* out;
   float* parts;                                           // [chunks][2][tiles * kTileColumns]: sums of the first token's rows if it comes from the chunk before,
   int64_t sum_blocks;                                     // and of the last one's if it begins here and goes on
+  int wave_rows;                                          // zeros: a wave per row
 };
-constexpr int kZeroRows = 4;                              // per workgroup
+constexpr int kWaveRow = 1024;                            // bytes of a row that a wave clears
 
 __device__ inline void put(const SumArgs& a, int id, const Columns& c, const float (&acc)[8]) {
   char* row = static_cast<char*>(a.out) + (int64_t)id * a.d * (a.out_bf16 ? 2 : 4);
@@ -278,20 +279,11 @@ template <bool kBf16> __global__ __launch_bounds__(256) void k_embedding_sum(Sum
   const int lane = threadIdx.x & 63;
   const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (block >= a.sum_blocks) {
-    // rows of tokens that do not occur
-    for (int k = 0; k < kZeroRows; ++k) {
-      const int64_t v = (block - a.sum_blocks) * kZeroRows + k;
-      if (v >= a.V || a.used[v] != 0) continue;
-      const int bytes = a.d * (a.out_bf16 ? 2 : 4);
-      char* row = static_cast<char*>(a.out) + v * bytes;
-      for (int o = threadIdx.x * 16; o < bytes; o += 256 * 16) {
-        if (o + 16 <= bytes) {
-          store_any<2>(row + o, u32x4{0, 0, 0, 0});
-        } else {
-          for (int e = o; e < bytes; e += 2) *reinterpret_cast<uint16_t*>(row + e) = 0;
-        }
-      }
-    }
+    // rows of tokens that do not occur, a workgroup each, or a short one a wave
+    const int row_bytes = a.d * (a.out_bf16 ? 2 : 4), lanes = a.wave_rows ? 64 : 256;
+    const int64_t item = block - a.sum_blocks, v = a.wave_rows ? item * 4 + (threadIdx.x >> 6) : item;
+    if (v >= a.V || a.used[v] != 0) return;
+    for (int o = (int)(threadIdx.x & (lanes - 1)) * 16; o < row_bytes; o += lanes * 16) zero_16(static_cast<char*>(a.out) + v * row_bytes, o, row_bytes);
     return;
   }
   const int64_t task = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = task / a.tiles;
@@ -385,7 +377,6 @@ __global__ __launch_bounds__(256) void k_embedding_join(SumArgs a) {
 }
 
 // ----------------------------------------------------------------------------
-constexpr int64_t kFillBytes = 16 * kSortThreads * 4, kMostFill = 2048;      // of a workgroup of k_sort_few, or more where that makes too many of them
 constexpr int64_t kMostRows = (int64_t)1 << 30, kMostWide = 1 << 21;
 constexpr int kMostColumns = 1 << 20, kMostIds = 1 << 24;
 dim3 grid_of(int64_t groups) {
@@ -439,9 +430,11 @@ extern "C" int mrl_embedding(const void* table, const int32_t* ids, const uint8_
   if (rc != MRL_OK) return rc;
   const int vectors = (d + 7) / 8;
   const LookArgs a = {table, ids, token_mask, N, d, V, vectors, scale, y_dtype == MRL_BF16, out_y};
-  const dim3 grid = grid_of((N * vectors + kLookThreads * kPerThread - 1) / (kLookThreads * kPerThread));
+  const int per_group = kLookThreads * (a.y_bf16 ? 4 : 1);
+  const dim3 grid = grid_of((N * vectors + per_group - 1) / per_group);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(table_dtype == MRL_BF16 ? k_embedding<true> : k_embedding<false>, grid, dim3(kLookThreads), 0, s, a);
+  const auto kernel = table_dtype == MRL_BF16 ? (a.y_bf16 ? k_embedding<true, 4> : k_embedding<true, 1>) : a.y_bf16 ? k_embedding<false, 4> : k_embedding<false, 1>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kLookThreads), 0, s, a);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
 }
 
@@ -472,7 +465,7 @@ extern "C" int mrl_embedding_backward(const void* dy, const int32_t* ids, const 
   bool in_a = true;
   if (few) {
     const int64_t bytes = (int64_t)V * d * (out_dtype == MRL_BF16 ? 2 : 4), fill = accumulate ? 0 : (bytes + kFillBytes - 1) / kFillBytes;
-    hipLaunchKernelGGL(k_sort_few, dim3((unsigned)(1 + (fill < kMostFill ? fill : kMostFill))), dim3(kSortThreads), 0, s, sort, out_dtable, bytes);
+    hipLaunchKernelGGL(k_sort_few, grid_of(1 + fill), dim3(kSortThreads), 0, s, sort, out_dtable, bytes);
     if (N == 0) return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
   } else {
     for (int p = 0; p < L.passes; ++p) {
@@ -481,9 +474,11 @@ extern "C" int mrl_embedding_backward(const void* dy, const int32_t* ids, const 
     }
     in_a = L.passes % 2 == 1;
   }
-  const int64_t sum_blocks = N > 0 ? (L.chunks * L.tiles + 3) / 4 : 0, zero_blocks = used == nullptr ? 0 : ((int64_t)V + kZeroRows - 1) / kZeroRows;
+  const int64_t sum_blocks = N > 0 ? (L.chunks * L.tiles + 3) / 4 : 0, row_bytes = (int64_t)d * (out_dtype == MRL_BF16 ? 2 : 4);
+  const bool wave_rows = row_bytes <= kWaveRow;
+  const int64_t zero_blocks = used == nullptr ? 0 : wave_rows ? ((int64_t)V + 3) / 4 : V;
   const SumArgs a = {dy, in_a ? sort.key_a : sort.key_b, in_a ? sort.at_a : sort.at_b, used, N, L.chunks, d, V, L.chunk, L.tiles, scale, accumulate,
-                     out_dtype == MRL_BF16, out_dtable, reinterpret_cast<float*>(ws + L.parts), sum_blocks};
+                     out_dtype == MRL_BF16, out_dtable, reinterpret_cast<float*>(ws + L.parts), sum_blocks, wave_rows};
   hipLaunchKernelGGL(dy_dtype == MRL_BF16 ? k_embedding_sum<true> : k_embedding_sum<false>, grid_of(sum_blocks + zero_blocks), dim3(256), 0, s, a);
   if (N > L.chunk) hipLaunchKernelGGL(k_embedding_join, grid_of(L.chunks * L.tiles), dim3(256), 0, s, a);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;

@@ -147,6 +147,60 @@ def test_passes(mrl, dtype, dw):
         _check(mrl, h, w, ids, logp, mrl.DistillConfig(dh_dtype=dh, accumulate_dw=1), base=base)
 
 
+@pytest.mark.parametrize("N,scored,d,V,chunk_rows,cut", [
+    (200, 200, 1536, 5000, 0, None),                    # a launch for few rows, whole lines of dW
+    (900, 577, 712, 1031, 0, None),                     # ... lines that straddle, ragged tiles
+    (300, 0, 136, 700, 0, None),                        # ... without a row
+    (1280, 1, 1024, 16405, 1280, (0, 65, 0, 4, 8)),     # tiles of 256 with a tail of slices, most of them empty
+    (1280, 327, 1024, 16405, 1280, (0, 65, 0, 4, 8)),
+    (1280, 0, 1024, 16405, 1280, (0, 65, 0, 4, 8)),
+    (1536, 1400, 1536, 11000, 0, (0, 43, 0, 18, 8)),
+    (4200, 4200, 1032, 24000, 0, (0, 94, 0, 30, 2)),
+    (2000, 2000, 136, 1000, 0, (3, 0, 0, 3, 4)),        # tiles of 384, all of them in slices
+    (2000, 0, 136, 1000, 0, (3, 0, 0, 3, 1)),
+    (2000, 2000, 3080, 9999, 0, (27, 0, 0, 95, 2)),     # a whole round and slices
+    (3500, 3400, 2056, 21000, 0, (55, 0, 0, 239, 1)),
+])
+def test_bf16_gradient_of_the_head_is_the_float_one_rounded(mrl, N, scored, d, V, chunk_rows, cut):
+    """Each of the launches of dW with a bf16 output: the bits of the float output, rounded once; scratch that holds NaN before."""
+    h, w = rand((N, d), BF16, N), rand((V, d), BF16, N + 1, 2.0 / d ** 0.5)
+    g = torch.Generator("cuda").manual_seed(N)
+    ids = torch.randint(0, V, (N, 9), device="cuda", generator=g, dtype=torch.int32)
+    logp = -3 * torch.rand(N, 9, device="cuda", generator=g)
+    mask = (torch.randperm(N, device="cuda", generator=g) < scored).to(torch.uint8)
+    chunk = chunk_rows or -(-N // 256) * 256
+    if cut is None:
+        assert N <= mrl.dw_few_rows()
+    else:
+        c = mrl.gemm_cut(mrl.GEMM_DW, max(scored, 1), V, d, chunk, min(N, chunk))
+        assert (c["wide"], c["narrow"], c["half"], c["rest"]) == cut[:4] and (scored == 0 or c["split"] == cut[4])
+    out = []
+    for dw in (mrl.F32, mrl.BF16):
+        cfg = mrl.DistillConfig(dw_dtype=dw, chunk_rows=chunk_rows)
+        ws = torch.full((mrl.distill_loss_workspace(N, d, V, 9, mrl.BF16, cfg),), 255, dtype=torch.uint8, device="cuda")
+        dW = torch.full((V + 1, d), float("nan"), device="cuda", dtype=F32 if dw == mrl.F32 else BF16)
+        out.append(mrl.distill_loss_fwd_bwd(h, w, ids, logp, cfg, token_mask=mask, out_dW=dW[:V], workspace=ws))
+        assert torch.all(torch.isnan(dW[V].float()))    # (nothing behind the last row)
+    a, b = out
+    assert torch.equal(a["dW"].bfloat16(), b["dW"]) and torch.equal(a["dH"], b["dH"]) and torch.equal(a["kl"], b["kl"])
+    if scored == 0:
+        assert torch.all(a["dW"] == 0) and torch.all(b["dW"] == 0)
+    else:
+        # column sums of dz are zero: so are those of dW's rows, to its operands' rounding
+        assert float(a["dW"].double().sum(0).abs().max()) <= 2.0 ** -7 * float(a["dW"].double().abs().sum(0).max())
+
+
+def test_bf16_gradient_at_any_address(mrl):
+    N, d, V = 1500, 136, 900
+    h, w, ids, logp = _case(N, d, V, 7, BF16, 3)
+    for n in (N, 200):
+        args = (h[:n].contiguous(), w, ids[:n].contiguous(), logp[:n].contiguous())
+        want = mrl.distill_loss_fwd_bwd(*args, mrl.DistillConfig(dw_dtype=mrl.BF16))
+        buf = torch.zeros(V * d + 3, device="cuda", dtype=BF16)
+        got = mrl.distill_loss_fwd_bwd(*args, mrl.DistillConfig(dw_dtype=mrl.BF16), out_dW=buf[1:1 + V * d].view(V, d))
+        assert torch.equal(got["dW"], want["dW"]) and buf[0] == 0 and torch.all(buf[1 + V * d:] == 0)
+
+
 def test_smaller_workspace(mrl):
     N, d, V, k = 3000, 128, 1000, 20
     h, w, ids, logp = _case(N, d, V, k, BF16, 4)
