@@ -2,12 +2,13 @@
 //   u_v = z_v s2 - m s2,  S = sum 2^u,  E = sum 2^u u     (m: the largest logit met; all in the log2 domain)
 //   lse = (m s2 + log2 S) ln 2,  entropy = (log2 S - E / S) ln 2,  log-prob = z / T - lse
 //   alternatives: the k largest by (logit, then the lower id first), exactly those
-// One pass over the logits, which are read once.  The alternatives come out of the same pass: the k-th largest of the threads'
-// running maxima is a lower bound of the k-th largest logit (each maximum is another element), so a thread looks at its tile's elements one by one
-// only where their maximum reaches that bound, and what reaches it goes to a list in LDS.  With random logits the list gets about
-// k (1 + log2(tiles)) entries; where it overflows (sorted or constant rows), and for rows with NaN, the workgroup selects by digits of the whole
-// key instead, in at most six further passes.
+// One pass over the logits, which are read once (but for what few of them the next sentences name).  A thread notes the largest of every few tiles it has seen.  The
+// k-th largest of the threads' maxima is a lower bound of the k-th largest logit (each maximum is another element); behind the pass, the notes that reach it
+// say where the logits that do can be, and those places, k and a little, are looked at again: what reaches the bound goes to a list in LDS, which is sorted.  So the pass
+// itself has no branch, barrier or atomic for the alternatives' sake.  Where the list overflows (sorted or constant rows), and for rows with NaN, the workgroup selects by digits of
+// the whole key instead, in at most six further passes.
 // Few rows are split over several workgroups each, whose lists and sums a second launch joins.
+// Memory bounds it in 32 bits, and the vector unit all but does in 16: 9.5 issue slots a logit, four of them the exponential's.
 #include "../../include/mrl.h"
 #include "mrl_internal.h"
 #include "mrl_vec.h"
@@ -20,7 +21,9 @@ constexpr int kWavesAtOnce = 8;                        // per SIMD: four workgro
 constexpr int kPer = 16;                               // logits of a thread in a tile
 constexpr int kTileLogits = kThreads * kPer;
 constexpr int kMostTop = 256;                          // alternatives of a call at most (the bound needs as many threads)
-constexpr int kKeys = 4096;                            // entries of the list
+constexpr int kHeld = 8, kKeys = kHeld * kThreads;     // entries of the list: a thread's own kOwn, and what more they have
+constexpr int kNotes = 32;                             // of a thread, each the largest of as many tiles as that makes (one up to V = 262144)
+constexpr int kPairs = 512;                            // notes that reach the bound, at most (about 350 where 256 alternatives are asked for)
 constexpr int kMostSplit = 256;
 constexpr int kIdBits = 24;                            // V <= 2^24
 constexpr uint64_t kIdMask = ((uint64_t)1 << kIdBits) - 1;
@@ -53,36 +56,34 @@ template <bool kBf16> __device__ inline float logit_at(const void* row, int v) {
 
 // What a thread looks at of a tile: vectors of 16 bytes, kThreads apart.  Behind `end` it finds -infinity.
 template <bool kBf16> struct Tile {
-  static constexpr int kVec = kBf16 ? 8 : 4, kLoads = kPer / kVec;
+  static constexpr int kVec = kBf16 ? 8 : 4, kLoads = kPer / kVec, kSize = kBf16 ? 2 : 4;
   u32x4 w[kLoads];
   __device__ static int id(int at, int i) { return at + (i / kVec * kThreads + (int)threadIdx.x) * kVec + i % kVec; }
   __device__ void load(const void* row, int at, int end) {
-    constexpr int kSize = kBf16 ? 2 : 4;
     if (at + kTileLogits <= end) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) w[j] = load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)id(at, j * kVec) * kSize);
       return;
     }
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const int v = id(at, j * kVec);
-      if (v + kVec <= end) {
-        w[j] = load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)v * kSize);
-      } else {
-        const uint32_t none = kBf16 ? 0xff80ff80u : 0xff800000u;
-        w[j] = u32x4{none, none, none, none};
+    for (int j = 0; j < kLoads; ++j) w[j] = load_to(row, id(at, j * kVec), end);
+  }
+  // The vector from logit v on, -infinity from `end` on.
+  __device__ static u32x4 load_to(const void* row, int v, int end) {
+    if (v + kVec <= end) return load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)v * kSize);
+    const uint32_t none = kBf16 ? 0xff80ff80u : 0xff800000u;
+    u32x4 w = {none, none, none, none};
 #pragma unroll
-        for (int e = 0; e < kVec - 1; ++e)
-          if (v + e < end) {
-            if (kBf16) {
-              const uint32_t b = static_cast<const uint16_t*>(row)[v + e];
-              w[j][e >> 1] = e & 1 ? (w[j][e >> 1] & 0xffffu) | b << 16 : (w[j][e >> 1] & 0xffff0000u) | b;
-            } else {
-              w[j][e] = static_cast<const uint32_t*>(row)[v + e];
-            }
-          }
+    for (int e = 0; e < kVec - 1; ++e)
+      if (v + e < end) {
+        if (kBf16) {
+          const uint32_t b = static_cast<const uint16_t*>(row)[v + e];
+          w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | b << 16 : (w[e >> 1] & 0xffff0000u) | b;
+        } else {
+          w[e] = static_cast<const uint32_t*>(row)[v + e];
+        }
       }
-    }
+    return w;
   }
   __device__ float operator[](int i) const {
     if (kBf16) return i & 1 ? bf16_high(w[i / 8][i % 8 / 2]) : bf16_low(w[i / 8][i % 8 / 2]);
@@ -90,18 +91,31 @@ template <bool kBf16> struct Tile {
   }
 };
 
+template <bool kBf16> __device__ inline void load_vector(const void* row, int v, int end, float (&z)[Tile<kBf16>::kVec]) {
+  const u32x4 w = Tile<kBf16>::load_to(row, v, end);
+#pragma unroll
+  for (int e = 0; e < Tile<kBf16>::kVec; ++e)
+    z[e] = kBf16 ? e & 1 ? bf16_high(w[e >> 1]) : bf16_low(w[e >> 1]) : __uint_as_float(w[e & 3]);
+}
+
 struct Shared {
-  uint64_t keys[kKeys];
-  uint64_t best[kMostTop];
+  union {
+    uint16_t notes[kNotes][kThreads];                  // upper half of the ordered number, as many bits as the bound has
+    uint64_t keys[kKeys];                              // the list
+  };
+  union {
+    uint64_t best[kMostTop];
+    uint32_t pairs[kPairs];
+  };
   uint32_t maxima[kThreads];
   float wave[kWaves][4];
   uint32_t scan[kWaves];
-  uint32_t count, bound, digit, above, inside;
+  uint32_t n_pairs, count /*entries of the list*/, bound, digit, above, inside;
 };
 
 // A lower bound of the k-th largest of the threads' numbers sh.maxima, exact in its upper kBoundBits bits, by bisection in the first wave.  0: fewer than k
 // are above 0.  Ends with a barrier.
-constexpr int kBoundBits = 16;
+constexpr int kBoundBits = 16;                         // (as many as a note has)
 __device__ inline void find_bound(Shared& sh, int k) {
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -120,16 +134,15 @@ __device__ inline void find_bound(Shared& sh, int k) {
   __syncthreads();
 }
 
-// The k largest of the sh.count keys of the list, largest first, to sh.best (zeros where there are fewer).
+// The k largest of the list's sh.count keys, largest first, to sh.best (zeros where there are fewer).  Begins behind a barrier.
 __device__ inline void sort_best(Shared& sh, int k) {
-  __syncthreads();
   int n = (int)sh.count;
-  if (n > 2 * k && n > 64) {
+  if (n > 2 * k + 64) {
     // fewer of them: those that reach the k-th largest of the threads' maxima
-    uint64_t own[kKeys / kThreads];
+    uint64_t own[kHeld];
     uint32_t most = 0;
 #pragma unroll
-    for (int j = 0; j < kKeys / kThreads; ++j) {
+    for (int j = 0; j < kHeld; ++j) {
       const int i = j * kThreads + threadIdx.x;
       own[j] = i < n ? sh.keys[i] : 0;
       most = larger(most, (uint32_t)(own[j] >> kIdBits));
@@ -140,14 +153,12 @@ __device__ inline void sort_best(Shared& sh, int k) {
     __syncthreads();
     const uint32_t bound = sh.bound;
 #pragma unroll
-    for (int j = 0; j < kKeys / kThreads; ++j)
+    for (int j = 0; j < kHeld; ++j)
       if (own[j] != 0 && (uint32_t)(own[j] >> kIdBits) >= bound) sh.keys[atomicAdd(&sh.count, 1u)] = own[j];
     __syncthreads();
     n = (int)sh.count;
   }
-  for (int i = threadIdx.x; i < kMostTop; i += kThreads) sh.best[i] = 0;
-  __syncthreads();
-  // a key's place is the number of larger ones: no two are alike
+  // a key's place is the number of larger ones: no two are alike (but for the zeros that stand for none)
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t key = sh.keys[i];
     int place = 0;
@@ -155,6 +166,7 @@ __device__ inline void sort_best(Shared& sh, int k) {
     for (int j = 0; j < n; ++j) place += sh.keys[j] > key;
     if (place < k) sh.best[place] = key;
   }
+  for (int i = n + threadIdx.x; i < k; i += kThreads) sh.best[i] = 0;
   __syncthreads();
 }
 
@@ -216,20 +228,10 @@ template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const
   __syncthreads();
 }
 
-// Two partial sums as one.  (A part without logits has S = 0 and the least m2.)
-__device__ inline Part join(const Part& a, const Part& b) {
-  const float m2 = fmaxf(a.m2, b.m2), da = a.m2 - m2, db = b.m2 - m2;
-  const float ca = __builtin_amdgcn_exp2f(da), cb = __builtin_amdgcn_exp2f(db);
-  return {m2, ca * a.S + cb * b.S, ca * fmaf(a.S, da, a.E) + cb * fmaf(b.S, db, b.E)};
-}
-// All threads' as one, in a fixed order; known to all.
+// All threads' sums as one, relative to the largest of their m2, in a fixed order; known to all.  (A part without logits has S = 0 and the least m2.)
 template <int kLanes> __device__ inline Part join_lanes(Part p) {
-#pragma unroll
-  for (int off = 1; off < kLanes; off <<= 1) {
-    const Part o = {__shfl_xor(p.m2, off), __shfl_xor(p.S, off), __shfl_xor(p.E, off)};
-    p = threadIdx.x & off ? join(o, p) : join(p, o);
-  }
-  return p;
+  const float m2 = over_lanes<kLanes>(p.m2, [](float a, float b) { return fmaxf(a, b); }), d = p.m2 - m2, c = __builtin_amdgcn_exp2f(d);
+  return {m2, lanes_sum<kLanes>(c * p.S), lanes_sum<kLanes>(c * fmaf(p.S, d, p.E))};
 }
 __device__ inline Part join_all(Shared& sh, Part p) {
   p = join_lanes<64>(p);
@@ -272,6 +274,7 @@ template <bool kBf16> __device__ inline void put_row(Shared& sh, const TopArgs& 
   double offset = p.m2;
   float S = p.S, E = p.E;
   if (!(S > 0.f && S < INFINITY)) careful_sums<kBf16>(sh, a, row, offset, S, E);
+  if ((int)(threadIdx.x & ~63u) >= (a.k > 1 ? a.k : 1)) return;      // (waves without outputs; no barrier from here on)
   const double log2_S = log2((double)S), lse = (offset + log2_S) * LN2;
   for (int i = threadIdx.x; i < a.k; i += kThreads) {
     const uint64_t key = sh.best[i];
@@ -311,14 +314,15 @@ template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void 
   const int part = (int)(item - n * a.split), begin = part * a.slice, end = a.V - begin < a.slice ? a.V : begin + a.slice;
   const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
   const int k = a.k < end - begin ? a.k : end - begin;
-  if (threadIdx.x == 0) sh.count = 0;                  // (the first bound's barriers lie before its first use)
-  float m = kNone, m2 = kNone * a.s2, S = 0.f, E = 0.f, bound = 0.f;
+  const int tiles = (end - begin + kTileLogits - 1) / kTileLogits, per_note = (tiles + kNotes - 1) / kNotes;
+  if (threadIdx.x == 0) sh.n_pairs = sh.count = 0;
+  float m = kNone, m2 = kNone * a.s2, S = 0.f, E = 0.f, note = -INFINITY;
   Tile<kBf16> next;
   next.load(row, begin, end);
-  int tile = 0;
-  for (int at = begin; at < end; at += kTileLogits, ++tile) {
+  int left = per_note, notes = 0;                      // tiles of the note under way, notes so far
+  for (int tile = 0; tile < tiles; ++tile) {
     const Tile<kBf16> z = next;
-    if (at + kTileLogits < end) next.load(row, at + kTileLogits, end);
+    if (tile + 1 < tiles) next.load(row, begin + (tile + 1) * kTileLogits, end);
     float most = z[0];
 #pragma unroll
     for (int i = 1; i < kPer; ++i) most = fmaxf(most, z[i]);
@@ -334,27 +338,43 @@ template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void 
       S += e;
       E = fmaf(e, fmaxf(u, kLeastU), E);
     }
-    if (k == 0) continue;
-    if ((tile & (tile + 1)) == 0) {                    // behind tiles 0, 1, 3, 7 ...: a higher bound
-      sh.maxima[threadIdx.x] = m > kNone ? ordered(m) : 0;
-      find_bound(sh, k);
-      bound = sh.bound == 0 ? -INFINITY : from_ordered(sh.bound);
-    }
-    if (!(most < bound)) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int v = Tile<kBf16>::id(at, i);
-        if (!(z[i] < bound) && v < end) {
-          const uint32_t place = atomicAdd(&sh.count, 1u);
-          if (place < (uint32_t)kKeys) sh.keys[place] = key_of(z[i], v);
-        }
-      }
-    }
+    note = fmaxf(note, most);
+    if (--left == 0 || tile + 1 == tiles) { sh.notes[notes++][threadIdx.x] = (uint16_t)(ordered(note) >> 16); note = -INFINITY; left = per_note; }
   }
+  sh.maxima[threadIdx.x] = m > kNone ? ordered(m) : 0;
   const Part p = join_all(sh, {m2, S, E});
   if (k > 0) {
+    find_bound(sh, k);
+    const float bound = sh.bound == 0 ? -INFINITY : from_ordered(sh.bound);
+    for (int i = 0; i < notes; ++i)
+      if (sh.notes[i][threadIdx.x] >= sh.bound >> 16) {
+        const uint32_t at = atomicAdd(&sh.n_pairs, 1u);
+        if (at < (uint32_t)kPairs) sh.pairs[at] = (uint32_t)i << 16 | threadIdx.x;
+      }
+    __syncthreads();
+    const uint32_t n_pairs = sh.n_pairs;
+    if (n_pairs <= (uint32_t)kPairs) {
+      // a vector of a noted tile per thread and step
+      constexpr int kVec = Tile<kBf16>::kVec, kLoads = Tile<kBf16>::kLoads;
+      const int each = per_note * kLoads;
+      for (int q = threadIdx.x; q < (int)n_pairs * each; q += kThreads) {
+        const int which = q / each, in = q - which * each, thread = (int)(sh.pairs[which] & 0xffffu);
+        const int tile = (int)(sh.pairs[which] >> 16) * per_note + in / kLoads;
+        const int v = begin + tile * kTileLogits + (in % kLoads * kThreads + thread) * kVec;
+        if (tile >= tiles || v >= end) continue;
+        float z[kVec];
+        load_vector<kBf16>(row, v, end, z);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (!(z[e] < bound) && v + e < end) {
+            const uint32_t place = atomicAdd(&sh.count, 1u);
+            if (place < (uint32_t)kKeys) sh.keys[place] = key_of(z[e], v + e);
+          }
+      }
+    }
+    __syncthreads();
     // (a NaN is the only thing that makes S one, but for an infinite logit: the comparisons above went past it)
-    if (sh.count > (uint32_t)kKeys || p.S != p.S) collect_by_digits<kBf16>(sh, row, begin, end, k);
+    if (n_pairs > (uint32_t)kPairs || sh.count > (uint32_t)kKeys || p.S != p.S) collect_by_digits<kBf16>(sh, row, begin, end, k);
     sort_best(sh, k);
   }
   if (a.split == 1) {

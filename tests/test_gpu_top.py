@@ -152,6 +152,38 @@ def test_masked_rows_are_not_read(mrl, N):
     assert torch.all(r["ids"] == -1) and torch.all(r["top_logp"] == 0) and torch.all(r["lse"] == 0) and r["logp"] is None
 
 
+@pytest.mark.parametrize("N,V,k,dtype", [(1030, 300001, 64, BF16), (1030, 300001, 256, F32), (2, 1 << 24, 100, F32), (3, 5000011, 7, BF16)])
+def test_long_rows(mrl, N, V, k, dtype):
+    """Rows of more tiles than a workgroup has notes for, whole and in slices; the reference in 64 bits on the GPU."""
+    z = rand((N, V), dtype, N, 3.0)
+    z[0, V - 1] = 40.0
+    r = mrl.top_logprobs(z, k)
+    for n in (0, 1, N - 1):
+        x = z[n].double()
+        order = torch.sort(x, descending=True, stable=True).indices[:k]
+        assert torch.equal(r["ids"][n].long(), order)
+        lse = torch.logsumexp(x, 0)
+        p = torch.exp(x - lse)
+        A = (V / 512 + 56) * U + 4 * U * float(x.abs().max())
+        assert abs(float(r["lse"][n]) - float(lse)) <= A + U * float(lse)
+        assert float((r["top_logp"][n].double() - (x[order] - lse)).abs().max()) <= A + 40 * U
+        H = float(lse - (p * x).sum())
+        assert abs(float(r["entropy"][n]) - H) <= (2 + H) * A + U * 200 ** 2 / 4
+
+
+@pytest.mark.parametrize("N", [3, 1100])
+def test_one_thread_holds_the_largest(mrl, N):
+    """All alternatives among the logits that one thread of the workgroup looks at; and more equal logits than the list holds."""
+    V = 60000
+    z = torch.zeros((N, V), device="cuda")
+    z[:, 4096 * torch.arange(14, device="cuda")] = torch.arange(14, device="cuda").float() + 1
+    z[:, 30000:] -= 1.0
+    z[:, 100:5000] = 0.25
+    _check(mrl, z[:3].contiguous(), 30)
+    r = mrl.top_logprobs(z, 30)
+    assert torch.equal(r["ids"], mrl.top_logprobs(z[:3].contiguous(), 30)["ids"][:1].expand(N, 30))
+
+
 def test_no_rows_and_outputs_left_out(mrl):
     r = mrl.top_logprobs(torch.empty(0, 100, device="cuda"), 5)
     assert r["ids"].shape == (0, 5) and r["lse"].shape == (0,)
