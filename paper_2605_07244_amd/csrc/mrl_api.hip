@@ -651,7 +651,7 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     // (rows of the pass at most, as far as the caller says)
     const int64_t hinted = cfg->scored_rows_hint > 0 ? cfg->scored_rows_hint - c0 : L.chunk_rows;
     const int expected = (int)(hinted < L.chunk_rows ? hinted : L.chunk_rows);
-    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected);
+    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected, V, d, false);
     if (bf16 && out_dW) {
       // the stash already holds the backward operand; the dW launch needs the pass's gathered rows, each
       // times its row scale, transposed, and zeros behind the last valid row
@@ -784,7 +784,7 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
       if (dW) { Scope sc(MRL_PROF_GEMM_DW, s); launch_gemm_f32(p.w, s); }
       continue;
     }
-    const bool dw_blocks = dw_rows_in_blocks(rows);
+    const bool dw_blocks = dw_rows_in_blocks(rows, V, d, dw_bf16 && !sum_apart);
     if (dW) {
       Scope sc(MRL_PROF_CONVERT, s);
       launch_backward_rows_b16(at<void>(ws, L.Hc), L.ldh, a.row_scale + c0, at<void>(ws, L.Ht), L.ldr, n_scored, c0, L.chunk_rows, L.dp,

@@ -1972,7 +1972,13 @@ int gemm_tail_items(size_t head_bytes) {
 }
 // (as many of 256 x 256: what a workspace had before the tiles grew; their last round is then cut into fewer slices)
 size_t gemm_tail_bytes_least(size_t head_bytes) { return (size_t)gemm_tail_items(head_bytes) * RES * RES * sizeof(float); }
-bool dw_rows_in_blocks(int rows) { return rows <= kFewDwRows; }
+// A bf16 dW has half the stores to hide, and with enough tiles the larger ones' smaller traffic counts for more at any number of rows.  dW's share of a call, us, this launch
+// and the large tile: V = 151936, d = 4096, 200 rows 618 and 514, 1000 rows 1304 and 1070; d = 1536 260 and 256, 539 and 470; V = 100000, d = 1536 (2346 tiles of
+// 256) 300 rows 193 and 183, 1000 rows 355 and 324; V = 32000, d = 4096 (2000) 156 and 161, 282 and 273; V = 50257, d = 2048 (1576) 400 rows 159 and 185, 700 rows 190 and 212.
+constexpr int kFewDw16Tiles = 8 * kRound;
+bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16) {
+  return rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles);
+}
 
 void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
@@ -2052,7 +2058,7 @@ extern "C" int mrl_diag_gemm_cut(int32_t launch, int32_t rows, int32_t expected,
     out9[4] = all % kRound; out9[5] = split; out9[6] = blocks;
   };
   if (launch == MRL_PROF_GEMM_DW) {
-    if (dw_rows_in_blocks(expected)) return MRL_OK;
+    if (dw_rows_in_blocks(expected, V, d, false)) return MRL_OK;
     const DwPlan plan = plan_dw(chunk_rows, expected, V, d, items);
     const int panels = dw_panels(rows, chunk_rows);
     if (plan.wide) put(tiles(V, RING), 0, 0, plan.tiles, plan.rest > 0 ? dw_split(plan.rest, panels, items) : 1, plan.blocks);

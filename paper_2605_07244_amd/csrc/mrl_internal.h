@@ -92,7 +92,7 @@ void launch_gemm_dh_bf16(const void* E, int64_t lde, const void* W, int64_t ldw,
 size_t gemm_tail_tile_bytes();
 int gemm_tail_items(size_t head_bytes);               // of a workspace, for a head of so many bytes
 size_t gemm_tail_bytes_least(size_t head_bytes);      // ... in one that has no room for them all
-bool dw_rows_in_blocks(int rows);
+bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16);
 void launch_gemm_dw_bf16(const void* P, int64_t ldp, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                          int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,

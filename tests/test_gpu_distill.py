@@ -190,6 +190,21 @@ def test_bf16_gradient_of_the_head_is_the_float_one_rounded(mrl, N, scored, d, V
         assert float(a["dW"].double().sum(0).abs().max()) <= 2.0 ** -7 * float(a["dW"].double().abs().sum(0).max())
 
 
+@pytest.mark.parametrize("N,d,V", [(100, 2048, 66001), (700, 1032, 110000)])
+def test_bf16_gradient_of_a_large_head_and_few_rows(mrl, N, d, V):
+    """Heads of 2048 tiles and more take the large tiles for few rows too, with a bf16 gradient: another order of the same products than the float one's launch."""
+    h, w = rand((N, d), BF16, N), rand((V, d), BF16, N + 1, 2.0 / d ** 0.5)
+    ids = torch.randint(0, V, (N, 5), device="cuda", generator=torch.Generator("cuda").manual_seed(N), dtype=torch.int32)
+    logp = torch.full((N, 5), -1.0, device="cuda")
+    a = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig())
+    ws = torch.full((mrl.distill_loss_workspace(N, d, V, 5, mrl.BF16, mrl.DistillConfig(dw_dtype=mrl.BF16)),), 255, dtype=torch.uint8, device="cuda")
+    b = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(dw_dtype=mrl.BF16), workspace=ws)
+    assert torch.equal(a["dH"], b["dH"]) and torch.equal(a["kl"], b["kl"])
+    # N products, each partial sum rounded, of at most the sum of their magnitudes: that of column k is below the sum of |h| times the largest scaled exponential's share
+    mag = 2.0 / N * h.float().abs().sum(0)
+    assert torch.all((a["dW"] - b["dW"].float()).abs() <= 2.0 ** -8 * a["dW"].abs() + 2 * N * U * mag)
+
+
 def test_bf16_gradient_at_any_address(mrl):
     N, d, V = 1500, 136, 900
     h, w, ids, logp = _case(N, d, V, 7, BF16, 3)
