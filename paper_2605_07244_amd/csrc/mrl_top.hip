@@ -16,12 +16,11 @@
 namespace mrl {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kMostThreads = 512;                      // of a workgroup
 constexpr int kWavesAtOnce = 8;                        // per SIMD: four workgroups to a compute unit
 constexpr int kPer = 16;                               // logits of a thread in a tile
-constexpr int kTileLogits = kThreads * kPer;
 constexpr int kMostTop = 256;                          // alternatives of a call at most (the bound needs as many threads)
-constexpr int kHeld = 8, kKeys = kHeld * kThreads;     // entries of the list: a thread's own kOwn, and what more they have
+constexpr int kHeld = 8;                               // entries of the list per thread
 constexpr int kNotes = 32;                             // of a thread, each the largest of as many tiles as that makes (one up to V = 262144)
 constexpr int kPairs = 512;                            // notes that reach the bound, at most (about 350 where 256 alternatives are asked for)
 constexpr int kMostSplit = 256;
@@ -54,13 +53,13 @@ template <bool kBf16> __device__ inline float logit_at(const void* row, int v) {
   return kBf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(row)[v] << 16) : static_cast<const float*>(row)[v];
 }
 
-// What a thread looks at of a tile: vectors of 16 bytes, kThreads apart.  Behind `end` it finds -infinity.
-template <bool kBf16> struct Tile {
-  static constexpr int kVec = kBf16 ? 8 : 4, kLoads = kPer / kVec, kSize = kBf16 ? 2 : 4;
+// What a thread of a workgroup of T looks at of a tile: vectors of 16 bytes, T apart.  Behind `end` it finds -infinity.
+template <bool kBf16, int T> struct Tile {
+  static constexpr int kVec = kBf16 ? 8 : 4, kLoads = kPer / kVec, kSize = kBf16 ? 2 : 4, kLogits = T * kPer;
   u32x4 w[kLoads];
-  __device__ static int id(int at, int i) { return at + (i / kVec * kThreads + (int)threadIdx.x) * kVec + i % kVec; }
+  __device__ static int id(int at, int i) { return at + (i / kVec * T + (int)threadIdx.x) * kVec + i % kVec; }
   __device__ void load(const void* row, int at, int end) {
-    if (at + kTileLogits <= end) {
+    if (at + kLogits <= end) {
 #pragma unroll
       for (int j = 0; j < kLoads; ++j) w[j] = load_any<kSize, u32x4>(static_cast<const char*>(row) + (int64_t)id(at, j * kVec) * kSize);
       return;
@@ -91,23 +90,24 @@ template <bool kBf16> struct Tile {
   }
 };
 
-template <bool kBf16> __device__ inline void load_vector(const void* row, int v, int end, float (&z)[Tile<kBf16>::kVec]) {
-  const u32x4 w = Tile<kBf16>::load_to(row, v, end);
+template <bool kBf16, int T> __device__ inline void load_vector(const void* row, int v, int end, float (&z)[Tile<kBf16, T>::kVec]) {
+  const u32x4 w = Tile<kBf16, T>::load_to(row, v, end);
 #pragma unroll
-  for (int e = 0; e < Tile<kBf16>::kVec; ++e)
+  for (int e = 0; e < Tile<kBf16, T>::kVec; ++e)
     z[e] = kBf16 ? e & 1 ? bf16_high(w[e >> 1]) : bf16_low(w[e >> 1]) : __uint_as_float(w[e & 3]);
 }
 
-struct Shared {
+template <int T> struct Shared {
+  static constexpr int kWaves = T / 64, kKeys = kHeld * T;
   union {
-    uint16_t notes[kNotes][kThreads];                  // upper half of the ordered number, as many bits as the bound has
+    uint16_t notes[kNotes][T];                  // upper half of the ordered number, as many bits as the bound has
     uint64_t keys[kKeys];                              // the list
   };
   union {
     uint64_t best[kMostTop];
     uint32_t pairs[kPairs];
   };
-  uint32_t maxima[kThreads];
+  uint32_t maxima[T];
   float wave[kWaves][4];
   uint32_t scan[kWaves];
   uint32_t n_pairs, count /*entries of the list*/, bound, digit, above, inside;
@@ -116,7 +116,8 @@ struct Shared {
 // A lower bound of the k-th largest of the threads' numbers sh.maxima, exact in its upper kBoundBits bits, by bisection in the first wave.  0: fewer than k
 // are above 0.  Ends with a barrier.
 constexpr int kBoundBits = 16;                         // (as many as a note has)
-__device__ inline void find_bound(Shared& sh, int k) {
+template <int T> __device__ inline void find_bound(Shared<T>& sh, int k) {
+  constexpr int kWaves = T / 64;
   __syncthreads();
   if (threadIdx.x < 64) {
     uint32_t m[kWaves], t = 0;
@@ -135,7 +136,7 @@ __device__ inline void find_bound(Shared& sh, int k) {
 }
 
 // The k largest of the list's sh.count keys, largest first, to sh.best (zeros where there are fewer).  Begins behind a barrier.
-__device__ inline void sort_best(Shared& sh, int k) {
+template <int T> __device__ inline void sort_best(Shared<T>& sh, int k) {
   int n = (int)sh.count;
   if (n > 2 * k + 64) {
     // fewer of them: those that reach the k-th largest of the threads' maxima
@@ -143,7 +144,7 @@ __device__ inline void sort_best(Shared& sh, int k) {
     uint32_t most = 0;
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
-      const int i = j * kThreads + threadIdx.x;
+      const int i = j * T + threadIdx.x;
       own[j] = i < n ? sh.keys[i] : 0;
       most = larger(most, (uint32_t)(own[j] >> kIdBits));
     }
@@ -159,39 +160,39 @@ __device__ inline void sort_best(Shared& sh, int k) {
     n = (int)sh.count;
   }
   // a key's place is the number of larger ones: no two are alike (but for the zeros that stand for none)
-  for (int i = threadIdx.x; i < n; i += kThreads) {
+  for (int i = threadIdx.x; i < n; i += T) {
     const uint64_t key = sh.keys[i];
     int place = 0;
 #pragma unroll 8
     for (int j = 0; j < n; ++j) place += sh.keys[j] > key;
     if (place < k) sh.best[place] = key;
   }
-  for (int i = n + threadIdx.x; i < k; i += kThreads) sh.best[i] = 0;
+  for (int i = n + threadIdx.x; i < k; i += T) sh.best[i] = 0;
   __syncthreads();
 }
 
 // The list by digits of the whole key, whatever the logits are: at most kKeys entries, the k largest of logits begin .. end - 1 among them.
-template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const void* row, int begin, int end, int k) {
-  constexpr int kDigits = 5;
-  constexpr int kShift[kDigits] = {44, 32, 24, 12, 0}, kBits[kDigits] = {12, 12, 8, 12, 12};
+template <bool kBf16, int T> __device__ inline void collect_by_digits(Shared<T>& sh, const void* row, int begin, int end, int k) {
+  constexpr int kBits = T == 512 ? 12 : 10, kBins = 1 << kBits;           // eight bins to a thread
+  static_assert(kBins == 8 * T && kBins * 4 <= Shared<T>::kKeys * 8, "the bins take the list's place");
   uint32_t* const hist = reinterpret_cast<uint32_t*>(sh.keys);
   uint64_t prefix = 0;
   uint32_t above = 0;                                  // keys above the prefix: fewer than k
-  int level = 0;
+  int rest = 32 + kIdBits;                             // bits below the prefix
 #pragma unroll 1                                       // (rare: registers count for more than its loops' speed)
-  for (;; ++level) {
-    const int shift = kShift[level], bits = kBits[level];
+  for (;;) {
+    const int bits = rest < kBits ? rest : kBits, shift = rest - bits;
     __syncthreads();
-    for (int i = threadIdx.x; i < 4096; i += kThreads) hist[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += T) hist[i] = 0;
     __syncthreads();
 #pragma unroll 1
-    for (int v = begin + threadIdx.x; v < end; v += kThreads) {
+    for (int v = begin + threadIdx.x; v < end; v += T) {
       const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
-      if (key >> (shift + bits) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
+      if (key >> rest == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1u);
     }
     __syncthreads();
     // from the highest digit down, eight to a thread: the one that holds the (k - above)-th key
-    const int first = 4096 - 8 * (int)(threadIdx.x + 1);
+    const int first = kBins - 8 * (int)(threadIdx.x + 1);
     uint32_t sum = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += hist[first + i];
@@ -214,14 +215,15 @@ template <bool kBf16> __device__ inline void collect_by_digits(Shared& sh, const
     __syncthreads();
     prefix = prefix << bits | sh.digit;
     above += sh.above;
-    if (above + sh.inside <= (uint32_t)kKeys) break;   // (behind the last digit a single key is inside)
+    rest = shift;
+    if (above + sh.inside <= (uint32_t)Shared<T>::kKeys) break;            // (behind the last digit a single key is inside)
   }
-  const uint64_t least = prefix << kShift[level];
+  const uint64_t least = prefix << rest;
   __syncthreads();
   if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
 #pragma unroll 1
-  for (int v = begin + threadIdx.x; v < end; v += kThreads) {
+  for (int v = begin + threadIdx.x; v < end; v += T) {
     const uint64_t key = key_of(logit_at<kBf16>(row, v), v);
     if (key >= least) sh.keys[atomicAdd(&sh.count, 1u)] = key;
   }
@@ -233,33 +235,33 @@ template <int kLanes> __device__ inline Part join_lanes(Part p) {
   const float m2 = over_lanes<kLanes>(p.m2, [](float a, float b) { return fmaxf(a, b); }), d = p.m2 - m2, c = __builtin_amdgcn_exp2f(d);
   return {m2, lanes_sum<kLanes>(c * p.S), lanes_sum<kLanes>(c * fmaf(p.S, d, p.E))};
 }
-__device__ inline Part join_all(Shared& sh, Part p) {
+template <int T> __device__ inline Part join_all(Shared<T>& sh, Part p) {
   p = join_lanes<64>(p);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) { float* w = sh.wave[threadIdx.x >> 6]; w[0] = p.m2; w[1] = p.S; w[2] = p.E; }
   __syncthreads();
-  const float* w = sh.wave[threadIdx.x & (kWaves - 1)];
-  return join_lanes<kWaves>({w[0], w[1], w[2]});
+  const int w = threadIdx.x & 7;                       // (eight lanes join them, of waves that there are not nothing)
+  return join_lanes<8>(w < T / 64 ? Part{sh.wave[w][0], sh.wave[w][1], sh.wave[w][2]} : Part{p.m2, 0.f, 0.f});
 }
 
 // Sums of a row that the pass has none for: its largest logit is NaN, infinite, or so low that m s2 is not finite.  Two passes, the differences to the
 // largest logit first.  S is NaN where there is no distribution.
-template <bool kBf16> __device__ inline void careful_sums(Shared& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
+template <bool kBf16, int T> __device__ inline void careful_sums(Shared<T>& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
   uint32_t most = 0;
 #pragma unroll 1
-  for (int v = threadIdx.x; v < a.V; v += kThreads) most = larger(most, ordered(logit_at<kBf16>(row, v)));
+  for (int v = threadIdx.x; v < a.V; v += T) most = larger(most, ordered(logit_at<kBf16>(row, v)));
   most = lanes_max<64>(most);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.scan[threadIdx.x >> 6] = most;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) most = larger(most, sh.scan[w]);
+  for (int w = 0; w < T / 64; ++w) most = larger(most, sh.scan[w]);
   const float m = from_ordered(most);
   offset = 0; S = __builtin_nanf(""); E = 0.f;
   if (!(fabsf(m) < INFINITY)) return;
   Part p = {0.f, 0.f, 0.f};
 #pragma unroll 1
-  for (int v = threadIdx.x; v < a.V; v += kThreads) {
+  for (int v = threadIdx.x; v < a.V; v += T) {
     const float u = (logit_at<kBf16>(row, v) - m) * a.s2, e = __builtin_amdgcn_exp2f(u);
     p.S += e;
     p.E = fmaf(e, fmaxf(u, kLeastU), p.E);
@@ -269,14 +271,14 @@ template <bool kBf16> __device__ inline void careful_sums(Shared& sh, const TopA
 }
 
 // A row's outputs: sums in p, the alternatives in sh.best.
-template <bool kBf16> __device__ inline void put_row(Shared& sh, const TopArgs& a, int64_t n, const Part& p) {
+template <bool kBf16, int T> __device__ inline void put_row(Shared<T>& sh, const TopArgs& a, int64_t n, const Part& p) {
   const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
   double offset = p.m2;
   float S = p.S, E = p.E;
   if (!(S > 0.f && S < INFINITY)) careful_sums<kBf16>(sh, a, row, offset, S, E);
   if ((int)(threadIdx.x & ~63u) >= (a.k > 1 ? a.k : 1)) return;      // (waves without outputs; no barrier from here on)
   const double log2_S = log2((double)S), lse = (offset + log2_S) * LN2;
-  for (int i = threadIdx.x; i < a.k; i += kThreads) {
+  for (int i = threadIdx.x; i < a.k; i += T) {
     const uint64_t key = sh.best[i];
     if (a.ids != nullptr) a.ids[n * a.k + i] = id_of(key);
     if (a.top != nullptr) a.top[n * a.k + i] = (float)((double)logit_of(key) * a.inv_T - lse);
@@ -291,8 +293,8 @@ template <bool kBf16> __device__ inline void put_row(Shared& sh, const TopArgs& 
   }
 }
 
-__device__ inline void put_masked_row(const TopArgs& a, int64_t n) {
-  for (int i = threadIdx.x; i < a.k; i += kThreads) {
+template <int T> __device__ inline void put_masked_row(const TopArgs& a, int64_t n) {
+  for (int i = threadIdx.x; i < a.k; i += T) {
     if (a.ids != nullptr) a.ids[n * a.k + i] = -1;
     if (a.top != nullptr) a.top[n * a.k + i] = 0.f;
   }
@@ -303,12 +305,14 @@ __device__ inline void put_masked_row(const TopArgs& a, int64_t n) {
   }
 }
 
-template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void k_top(TopArgs a) {
-  __shared__ Shared sh;
+template <bool kBf16, int T> __global__ __launch_bounds__(T, kWavesAtOnce) void k_top(TopArgs a) {
+  using Tile = Tile<kBf16, T>;
+  constexpr int kKeys = Shared<T>::kKeys, kTileLogits = Tile::kLogits;
+  __shared__ Shared<T> sh;
   const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, n = item / a.split;
   if (n >= a.N) return;
   if (a.mask != nullptr && a.mask[n] == 0) {
-    if (a.split == 1) put_masked_row(a, n);
+    if (a.split == 1) put_masked_row<T>(a, n);
     return;
   }
   const int part = (int)(item - n * a.split), begin = part * a.slice, end = a.V - begin < a.slice ? a.V : begin + a.slice;
@@ -317,11 +321,11 @@ template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void 
   const int tiles = (end - begin + kTileLogits - 1) / kTileLogits, per_note = (tiles + kNotes - 1) / kNotes;
   if (threadIdx.x == 0) sh.n_pairs = sh.count = 0;
   float m = kNone, m2 = kNone * a.s2, S = 0.f, E = 0.f, note = -INFINITY;
-  Tile<kBf16> next;
+  Tile next;
   next.load(row, begin, end);
   int left = per_note, notes = 0;                      // tiles of the note under way, notes so far
   for (int tile = 0; tile < tiles; ++tile) {
-    const Tile<kBf16> z = next;
+    const Tile z = next;
     if (tile + 1 < tiles) next.load(row, begin + (tile + 1) * kTileLogits, end);
     float most = z[0];
 #pragma unroll
@@ -355,15 +359,15 @@ template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void 
     const uint32_t n_pairs = sh.n_pairs;
     if (n_pairs <= (uint32_t)kPairs) {
       // a vector of a noted tile per thread and step
-      constexpr int kVec = Tile<kBf16>::kVec, kLoads = Tile<kBf16>::kLoads;
+      constexpr int kVec = Tile::kVec, kLoads = Tile::kLoads;
       const int each = per_note * kLoads;
-      for (int q = threadIdx.x; q < (int)n_pairs * each; q += kThreads) {
+      for (int q = threadIdx.x; q < (int)n_pairs * each; q += T) {
         const int which = q / each, in = q - which * each, thread = (int)(sh.pairs[which] & 0xffffu);
         const int tile = (int)(sh.pairs[which] >> 16) * per_note + in / kLoads;
-        const int v = begin + tile * kTileLogits + (in % kLoads * kThreads + thread) * kVec;
+        const int v = begin + tile * kTileLogits + (in % kLoads * T + thread) * kVec;
         if (tile >= tiles || v >= end) continue;
         float z[kVec];
-        load_vector<kBf16>(row, v, end, z);
+        load_vector<kBf16, T>(row, v, end, z);
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
           if (!(z[e] < bound) && v + e < end) {
@@ -382,16 +386,17 @@ template <bool kBf16> __global__ __launch_bounds__(kThreads, kWavesAtOnce) void 
     return;
   }
   if (threadIdx.x == 0) a.parts[item] = p;
-  for (int i = threadIdx.x; i < a.k; i += kThreads) a.keys[item * a.k + i] = sh.best[i];
+  for (int i = threadIdx.x; i < a.k; i += T) a.keys[item * a.k + i] = sh.best[i];
 }
 
-template <bool kBf16> __global__ __launch_bounds__(kThreads) void k_top_join(TopArgs a) {
-  __shared__ Shared sh;
+template <bool kBf16> __global__ __launch_bounds__(kMostThreads) void k_top_join(TopArgs a) {
+  constexpr int T = kMostThreads;
+  __shared__ Shared<T> sh;
   const int64_t n = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (n >= a.N) return;
-  if (a.mask != nullptr && a.mask[n] == 0) { put_masked_row(a, n); return; }
+  if (a.mask != nullptr && a.mask[n] == 0) { put_masked_row<T>(a, n); return; }
   const int count = a.split * a.k;                     // (at most kKeys)
-  for (int i = threadIdx.x; i < count; i += kThreads) sh.keys[i] = a.keys[n * count + i];
+  for (int i = threadIdx.x; i < count; i += T) sh.keys[i] = a.keys[n * count + i];
   if (threadIdx.x == 0) sh.count = (uint32_t)count;
   const Part p = join_all(sh, (int)threadIdx.x < a.split ? a.parts[n * a.split + threadIdx.x] : Part{kNone * a.s2, 0.f, 0.f});
   if (a.k > 0) sort_best(sh, a.k);
@@ -404,13 +409,17 @@ struct Split { int split, slice; };
 Split split_of(int64_t N, int V, int k) {
   int64_t s = N > 0 ? 1024 / N : 1;
   if (s > kMostSplit) s = kMostSplit;
-  if (k > 0 && s > kKeys / k) s = kKeys / k;
+  constexpr int kTileLogits = kMostThreads * kPer;
+  if (k > 0 && s > Shared<kMostThreads>::kKeys / k) s = Shared<kMostThreads>::kKeys / k;
   const int64_t by_length = (V + kTileLogits / 4 - 1) / (kTileLogits / 4);
   if (s > by_length) s = by_length;
   if (s <= 1) return {1, V};
   const int slice = (int)round_up((V + s - 1) / s, 64);
   return {(V + slice - 1) / slice, slice};
 }
+
+constexpr int kFewThreads = 128;
+bool short_rows(int split, int V, int k) { return split == 1 && V <= 16384 && k <= kFewThreads / 2; }
 
 constexpr int64_t kMostRows = (int64_t)1 << 30, kMostWide = 1 << 21;
 dim3 grid_of(int64_t groups) {
@@ -452,8 +461,10 @@ extern "C" int mrl_top_logprobs(const void* logits, int64_t row_stride, const in
     a.keys = reinterpret_cast<uint64_t*>(static_cast<unsigned char*>(workspace) + parts_bytes(N, s.split));
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  auto go = [&](auto kernel, int64_t groups) { hipLaunchKernelGGL(kernel, grid_of(groups), dim3(kThreads), 0, st, a); };
-  if (dtype == MRL_BF16) go(k_top<true>, N * s.split); else go(k_top<false>, N * s.split);
-  if (s.split > 1) { if (dtype == MRL_BF16) go(k_top_join<true>, N); else go(k_top_join<false>, N); }
+  auto go = [&](auto kernel, int threads, int64_t groups) { hipLaunchKernelGGL(kernel, grid_of(groups), dim3(threads), 0, st, a); };
+  const bool bf16 = dtype == MRL_BF16;
+  if (short_rows(s.split, V, k)) go(bf16 ? k_top<true, kFewThreads> : k_top<false, kFewThreads>, kFewThreads, N);
+  else go(bf16 ? k_top<true, kMostThreads> : k_top<false, kMostThreads>, kMostThreads, N * s.split);
+  if (s.split > 1) go(bf16 ? k_top_join<true> : k_top_join<false>, kMostThreads, N);
   return hipGetLastError() == hipSuccess ? MRL_OK : MRL_ERR_DEVICE;
 }
