@@ -404,13 +404,18 @@ template <bool kBf16> __global__ __launch_bounds__(kMostThreads) void k_top_join
 }
 
 // Workgroups of a row: one where there are rows enough for the chip (four workgroups to a compute unit), else as many as it has room for, each with a
-// quarter of a tile or more and no more alternatives in all than the list of the join holds.
+// quarter of a tile or more.  The join takes longer the more keys it is given, so that their lists hold 1024 together where that leaves no more than two tiles to each
+// (one row of 151936 floats, us, with 4096 and 1024: k = 64 20.2 and 16.6; 48 rows of 128256, k = 200 30.1 and 24.0), and at most what the join's list holds.
 struct Split { int split, slice; };
 Split split_of(int64_t N, int V, int k) {
+  constexpr int kTileLogits = kMostThreads * kPer, kMostKeys = Shared<kMostThreads>::kKeys;
   int64_t s = N > 0 ? 1024 / N : 1;
   if (s > kMostSplit) s = kMostSplit;
-  constexpr int kTileLogits = kMostThreads * kPer;
-  if (k > 0 && s > Shared<kMostThreads>::kKeys / k) s = Shared<kMostThreads>::kKeys / k;
+  if (k > 0) {
+    const int64_t few = 1024 / k, by_tiles = V / (2 * kTileLogits), most = few > by_tiles ? few : by_tiles;
+    if (s > most) s = most;
+    if (s > kMostKeys / k) s = kMostKeys / k;
+  }
   const int64_t by_length = (V + kTileLogits / 4 - 1) / (kTileLogits / 4);
   if (s > by_length) s = by_length;
   if (s <= 1) return {1, V};
@@ -418,8 +423,11 @@ Split split_of(int64_t N, int V, int k) {
   return {(V + slice - 1) / slice, slice};
 }
 
+// Workgroups of 128 where a row is short: what a row costs beyond its logits is the same latencies with any number of threads, and eight such rows are under way where
+// two of 512 were (16384 rows, us: of 1000 floats, k = 10 111 and 37, of 9000 in bf16 146 and 75, of 37000 262 and 243; of 151936 in bf16, k = 64 (4096 rows) 231 and 295).
+// With more alternatives the bound by the threads' maxima is too wide.
 constexpr int kFewThreads = 128;
-bool short_rows(int split, int V, int k) { return split == 1 && V <= 16384 && k <= kFewThreads / 2; }
+bool short_rows(int split, int V, int k) { return split == 1 && ((V <= 65536 && k <= kFewThreads / 4) || (V <= 32768 && k <= kFewThreads / 2)); }
 
 constexpr int64_t kMostRows = (int64_t)1 << 30, kMostWide = 1 << 21;
 dim3 grid_of(int64_t groups) {
