@@ -6,8 +6,10 @@
  * sampled tokens under the learner (LM-head projection, log-softmax over the
  * full vocabulary, gather at the target id), group-relative advantages, the
  * clipped importance-ratio surrogate with a KL term to a reference policy,
- * and the backward pass to the hidden states and the LM-head weight; and what stands
- * around that in a training step: the norm that makes the hidden states, its
+ * and the backward pass to the hidden states and the LM-head weight; the same head
+ * learning from a teacher's top alternatives in the place of rewards, and those
+ * alternatives from given logits; and what stands around that in a training step: the
+ * embedding and its gradient, the norm that makes the hidden states, its
  * backward pass, the clipping of the gradients and the AdamW update.
  *
  * Conventions for every entry point
@@ -24,13 +26,13 @@
  *     valid once the caller has synchronised that stream.  No host
  *     synchronisation happens inside a call (debug_sync of call (3) excepted).
  *   - Inputs are never modified.  Outputs are fully overwritten, except
- *     out_dW (out_dweight) when accumulate_dw = 1.  (Call (8) updates in place, and calls (5) and (6) may be given
+ *     out_dW (out_dweight, out_dtable) when accumulate_dw (accumulate) = 1.  (Call (8) updates in place, and calls (5) and (6) may be given
  *     an output that is one of their inputs.)
- *   - All tensors are dense and row-major.  lm_head_w is [V, d], one row per
+ *   - All tensors are dense and row-major (the rows of call (9)'s logits may lie apart).  lm_head_w is [V, d], one row per
  *     vocabulary id (the layout of a linear layer's weight).  Row n of hidden
  *     is the final hidden state that PREDICTS target_ids[n]; the shift
  *     between inputs and labels is the caller's business.  No bias, sampling
- *     temperature 1.
+ *     temperature 1 (calls (9) and (10) take one).
  *   - dtype MRL_BF16: hidden / lm_head_w are bfloat16, matrix products run on
  *     the bf16 MFMA units with fp32 accumulation; d must be a multiple of 8 (rows of 16-byte
  *     vectors).  Widths that are not a multiple of 128 run on zero-padded copies of the operands
@@ -487,7 +489,7 @@ int mrl_top_logprobs(const void* logits /*[N, row_stride] dev*/, int64_t row_str
  * An id outside [0, V) is no alternative (-1 for lists of different lengths; those at or above V are counted).  An id may be listed several times: the gradient
  * has the sum of its probabilities, the divergence a term for each.  A log-prob of -infinity is a probability of 0.
  * A row counts where its mask is not 0 (token_mask NULL: every row) and its alternatives' mass is above 0 (renormalize = 0: at least 1e-30); the others have
- * out_kl and out_dH of zero and add nothing; those with mask 0 are not read.  NaN in a row that counts makes its outputs NaN, and out_dW.
+ * out_kl and out_dH of zero and add nothing; those with mask 0 are not read.  NaN, or an infinite hidden state or log-prob, in a row that counts makes its outputs NaN, and out_dW.
  * Numerical range (bf16 path): a row whose most likely alternative has a log-prob below about -97 with the student reports a divergence that may be too small, is left
  * out of the loss and the gradients and counted in n_saturated_rows.
  * dtype, d and V as in call (3).  dh_dtype, dw_dtype: types of the gradients; MRL_BF16 with bf16 inputs only, dw_dtype MRL_BF16 only

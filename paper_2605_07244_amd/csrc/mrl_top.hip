@@ -2,13 +2,16 @@
 //   u_v = z_v s2 - m s2,  S = sum 2^u,  E = sum 2^u u     (m: the largest logit met; all in the log2 domain)
 //   lse = (m s2 + log2 S) ln 2,  entropy = (log2 S - E / S) ln 2,  log-prob = z / T - lse
 //   alternatives: the k largest by (logit, then the lower id first), exactly those
-// One pass over the logits, which are read once (but for what few of them the next sentences name).  A thread notes the largest of every few tiles it has seen.  The
-// k-th largest of the threads' maxima is a lower bound of the k-th largest logit (each maximum is another element); behind the pass, the notes that reach it
-// say where the logits that do can be, and those places, k and a little, are looked at again: what reaches the bound goes to a list in LDS, which is sorted.  So the pass
-// itself has no branch, barrier or atomic for the alternatives' sake.  Where the list overflows (sorted or constant rows), and for rows with NaN, the workgroup selects by digits of
-// the whole key instead, in at most six further passes.
-// Few rows are split over several workgroups each, whose lists and sums a second launch joins.
-// Memory bounds it in 32 bits, and the vector unit all but does in 16: 9.5 issue slots a logit, four of them the exponential's.
+// One pass reads the logits once.  A thread notes the largest of every few tiles it has seen.  The k-th largest of the threads' maxima is a lower bound of the
+// k-th largest logit (each maximum is another element); behind the pass, the notes that reach it say where the logits that do can be, and those places, k and a
+// little, are read again: what reaches the bound goes to a list in LDS, which is sorted.  So the pass itself has no branch, barrier or atomic for the alternatives' sake.
+// (With a list kept during the pass, under a bound renewed behind tiles 0, 1, 3, 7 ..., the entries' branches and atomics took as long as a third of the pass: 4096 rows of
+// 151936 in bf16, k = 64 264 us, now 229; 620 rows of 50257 floats 36 and 30.)  Where the list is too long (sorted or constant rows), and for rows with
+// NaN, the workgroup selects by digits of the whole key instead, in at most seven further passes.
+// Few rows are split over several workgroups each, whose lists and sums a second launch joins: a launch in which the last of them to end joins them would need
+// counters that are zero before the call.
+// Memory bounds it in 32 bits (4096 rows of 151936: k = 64 428 us, 5.8 TB/s; k = 0 408, 6.1), and the vector unit all but does in 16 (229 us, 5.4 TB/s): 9.5 issue slots a
+// logit, four of them the exponential's.
 #include "../../include/mrl.h"
 #include "mrl_internal.h"
 #include "mrl_vec.h"
@@ -20,7 +23,8 @@ constexpr int kMostThreads = 512;                      // of a workgroup
 constexpr int kWavesAtOnce = 8;                        // per SIMD: four workgroups to a compute unit
 constexpr int kPer = 16;                               // logits of a thread in a tile
 constexpr int kMostTop = 256;                          // alternatives of a call at most (the bound needs as many threads)
-constexpr int kHeld = 8;                               // entries of the list per thread
+constexpr int kHeld = 8;                               // entries that the list has room for, per thread
+constexpr int kMostList = 1024;                        // entries of a list that is sorted (k and a little as a rule): every entry is compared with every other
 constexpr int kNotes = 32;                             // of a thread, each the largest of as many tiles as that makes (one up to V = 262144)
 constexpr int kPairs = 512;                            // notes that reach the bound, at most (about 350 where 256 alternatives are asked for)
 constexpr int kMostSplit = 256;
@@ -100,7 +104,7 @@ template <bool kBf16, int T> __device__ inline void load_vector(const void* row,
 template <int T> struct Shared {
   static constexpr int kWaves = T / 64, kKeys = kHeld * T;
   union {
-    uint16_t notes[kNotes][T];                  // upper half of the ordered number, as many bits as the bound has
+    uint16_t notes[kNotes][T];                         // upper half of the ordered number, as many bits as the bound has
     uint64_t keys[kKeys];                              // the list
   };
   union {
@@ -171,7 +175,7 @@ template <int T> __device__ inline void sort_best(Shared<T>& sh, int k) {
   __syncthreads();
 }
 
-// The list by digits of the whole key, whatever the logits are: at most kKeys entries, the k largest of logits begin .. end - 1 among them.
+// The list by digits of the whole key, whatever the logits are: at most 2 k + 64 entries, the k largest of logits begin .. end - 1 among them.
 template <bool kBf16, int T> __device__ inline void collect_by_digits(Shared<T>& sh, const void* row, int begin, int end, int k) {
   constexpr int kBits = T == 512 ? 12 : 10, kBins = 1 << kBits;           // eight bins to a thread
   static_assert(kBins == 8 * T && kBins * 4 <= Shared<T>::kKeys * 8, "the bins take the list's place");
@@ -216,7 +220,7 @@ template <bool kBf16, int T> __device__ inline void collect_by_digits(Shared<T>&
     prefix = prefix << bits | sh.digit;
     above += sh.above;
     rest = shift;
-    if (above + sh.inside <= (uint32_t)Shared<T>::kKeys) break;            // (behind the last digit a single key is inside)
+    if (above + sh.inside <= 2u * k + 64) break;       // (behind the last digit a single key is inside)
   }
   const uint64_t least = prefix << rest;
   __syncthreads();
@@ -307,7 +311,8 @@ template <int T> __device__ inline void put_masked_row(const TopArgs& a, int64_t
 
 template <bool kBf16, int T> __global__ __launch_bounds__(T, kWavesAtOnce) void k_top(TopArgs a) {
   using Tile = Tile<kBf16, T>;
-  constexpr int kKeys = Shared<T>::kKeys, kTileLogits = Tile::kLogits;
+  constexpr int kTileLogits = Tile::kLogits;
+  static_assert(kMostList <= Shared<T>::kKeys && 2 * kMostTop + 64 <= kMostList, "lists have their room");
   __shared__ Shared<T> sh;
   const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, n = item / a.split;
   if (n >= a.N) return;
@@ -372,13 +377,13 @@ template <bool kBf16, int T> __global__ __launch_bounds__(T, kWavesAtOnce) void 
         for (int e = 0; e < kVec; ++e)
           if (!(z[e] < bound) && v + e < end) {
             const uint32_t place = atomicAdd(&sh.count, 1u);
-            if (place < (uint32_t)kKeys) sh.keys[place] = key_of(z[e], v + e);
+            if (place < (uint32_t)kMostList) sh.keys[place] = key_of(z[e], v + e);
           }
       }
     }
     __syncthreads();
     // (a NaN is the only thing that makes S one, but for an infinite logit: the comparisons above went past it)
-    if (n_pairs > (uint32_t)kPairs || sh.count > (uint32_t)kKeys || p.S != p.S) collect_by_digits<kBf16>(sh, row, begin, end, k);
+    if (n_pairs > (uint32_t)kPairs || sh.count > (uint32_t)kMostList || p.S != p.S) collect_by_digits<kBf16>(sh, row, begin, end, k);
     sort_best(sh, k);
   }
   if (a.split == 1) {

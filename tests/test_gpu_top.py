@@ -152,7 +152,7 @@ def test_masked_rows_are_not_read(mrl, N):
     assert torch.all(r["ids"] == -1) and torch.all(r["top_logp"] == 0) and torch.all(r["lse"] == 0) and r["logp"] is None
 
 
-@pytest.mark.parametrize("N,V,k,dtype", [(1030, 300001, 64, BF16), (1030, 300001, 256, F32), (2, 1 << 24, 100, F32), (3, 5000011, 7, BF16)])
+@pytest.mark.parametrize("N,V,k,dtype", [(1030, 300001, 64, BF16), (1030, 300001, 256, F32), (2, 1 << 24, 100, F32), (3, 5000011, 7, BF16), (1030, 65536, 32, F32), (1030, 32768, 64, BF16)])
 def test_long_rows(mrl, N, V, k, dtype):
     """Rows of more tiles than a workgroup has notes for, whole and in slices; the reference in 64 bits on the GPU."""
     z = rand((N, V), dtype, N, 3.0)
