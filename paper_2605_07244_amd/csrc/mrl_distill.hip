@@ -8,7 +8,6 @@
 // 64 bits: a few dozen operations beside 6 d V.  What is rounded to 16 bits, and how far that takes the gradients: e (or e - (S / m) q) in the stash and the row of
 // hidden states times its scale, half a step of 2^-9 each on average a third of it; dH 1.7e-3 of its norm and dW 2.4e-3, with the rounding of a bf16 output 2.4e-3 and 2.9e-3.
 #include "mrl_internal.h"
-#include "mrl_partials.h"
 #include "mrl_vec.h"
 
 namespace mrl {
@@ -182,10 +181,10 @@ __global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
 
 // Behind the forward launch: a workgroup adds the partial sums of 16 rows, then a wave takes each.  (Blocks of 64 rows, four to a wave, left most of the chip idle:
 // V = 151936, 200 rows, k = 32 50 us, now 14; 8192 rows, k = 64 77, now 34, 39 MB of partial sums and the alternatives' logits.)
-constexpr int kRows = 16, kLanes = EPI_THREADS / (kRows / 4);
-template <int kEach> __global__ __launch_bounds__(EPI_THREADS) void k_distill_rows(DistillArgs a) {
+constexpr int kRows = 16, kRowThreads = 64 * kRows, kLanes = kRowThreads / (kRows / 4);
+template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_rows(DistillArgs a) {
   __shared__ float sh[kLanes * (kRows + 1)];
-  __shared__ double parts[EPI_THREADS / 64][kDistillSums];
+  __shared__ double parts[kRowThreads / 64][kDistillSums];
   const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows), r0 = blockIdx.x * kRows;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double q[kDistillSums] = {};
@@ -252,7 +251,7 @@ template <int kEach> __global__ __launch_bounds__(EPI_THREADS) void k_distill_ro
   __syncthreads();
   if (threadIdx.x < kDistillSums) {
     double t = 0.0;
-    for (int w = 0; w < EPI_THREADS / 64; ++w) t += parts[w][threadIdx.x];
+    for (int w = 0; w < kRowThreads / 64; ++w) t += parts[w][threadIdx.x];
     a.loss_partials[(a.partial_block_offset + blockIdx.x) * kDistillSums + threadIdx.x] = t;
   }
 }
@@ -374,7 +373,7 @@ void launch_distill_logits(const DistillArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(k_distill_logits, dim3(a.chunk_rows), dim3(256), 0, stream, a);
 }
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(by_count(a.k, k_distill_rows<1>, k_distill_rows<2>, k_distill_rows<4>), dim3(a.chunk_rows / kRows), dim3(EPI_THREADS), 0, stream, a);
+  hipLaunchKernelGGL(by_count(a.k, k_distill_rows<1>, k_distill_rows<2>, k_distill_rows<4>), dim3(a.chunk_rows / kRows), dim3(kRowThreads), 0, stream, a);
 }
 int distill_row_blocks(int chunk_rows) { return chunk_rows / kRows; }
 int distill_f32_blocks(int64_t rows) { return (int)((rows + 3) / 4); }

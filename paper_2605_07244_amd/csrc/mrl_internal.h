@@ -98,6 +98,12 @@ void launch_gemm_dw_bf16(const void* P, int64_t ldp, const void* Ht, int64_t ldh
                          int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
                          hipStream_t stream);
 
+// Scored rows of the pass of chunk_rows rows from chunk_start on.
+__device__ inline int valid_rows(const int64_t* n_scored, int64_t chunk_start, int chunk_rows) {
+  const int64_t r = *n_scored - chunk_start;
+  return r < 0 ? 0 : (r > chunk_rows ? chunk_rows : (int)r);
+}
+
 // ---- fp32 GEMM (small-shape path): C[m][n] = sum_k A[m][k] * B[n][k] --------
 // An operand is k-contiguous (element (row, k) at row * ld + k) or, with its kmajor flag, stored with
 // k as the row (at k * ld + row).  a_rows / b_rows: optional maps of the operand's stored rows, c_rows

@@ -248,8 +248,8 @@ template <int T> __device__ inline Part join_all(Shared<T>& sh, Part p) {
   return join_lanes<8>(w < T / 64 ? Part{sh.wave[w][0], sh.wave[w][1], sh.wave[w][2]} : Part{p.m2, 0.f, 0.f});
 }
 
-// Sums of a row that the pass has none for: its largest logit is NaN, infinite, or so low that m s2 is not finite.  Two passes, the differences to the
-// largest logit first.  S is NaN where there is no distribution.
+// Sums of a row that the pass has none for: its largest logit is NaN, infinite, below kNone, or so large that m s2, or its distance from kNone s2, is not finite
+// (there E alone may be NaN).  Two passes, the differences to the largest logit first.  S is NaN where there is no distribution.
 template <bool kBf16, int T> __device__ inline void careful_sums(Shared<T>& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
   uint32_t most = 0;
 #pragma unroll 1
@@ -279,7 +279,7 @@ template <bool kBf16, int T> __device__ inline void put_row(Shared<T>& sh, const
   const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
   double offset = p.m2;
   float S = p.S, E = p.E;
-  if (!(S > 0.f && S < INFINITY)) careful_sums<kBf16>(sh, a, row, offset, S, E);
+  if (!(S > 0.f && S < INFINITY) || E != E) careful_sums<kBf16>(sh, a, row, offset, S, E);
   if ((int)(threadIdx.x & ~63u) >= (a.k > 1 ? a.k : 1)) return;      // (waves without outputs; no barrier from here on)
   const double log2_S = log2((double)S), lse = (offset + log2_S) * LN2;
   for (int i = threadIdx.x; i < a.k; i += T) {

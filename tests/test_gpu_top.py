@@ -2,8 +2,8 @@
 
 Bounds.  U = 2^-24 is half a step of fp32; s = z / T.  The scale log2(e) / T is rounded once, which moves every s by U |s|, and the exponents u = (z - m) scale are
 rounded to U |u|; where u = 0 is taken to, m scale, cancels.  A thread adds one 512th of the row's exponentials, in sums of 16 to a tile, the lanes, waves and
-parts another 30 at most, each exponential is good to 2 U: lse is off by A = (V / 512 + 16 + 40) U + 4 U max |s|, and log-probs by that and the rounding of the
-result.  The entropy takes a second such sum, of 2^u u, whose size is the entropy's and a little, and changes by the variance of s
+parts another 30 at most (a row of up to 65536 logits may go to 128 threads, four times as many to each: the bound below is held there without that
+factor), each exponential is good to 2 U: lse is off by A = (V / 512 + 16 + 40) U + 4 U max |s|, and log-probs by that and the rounding of the result.  The entropy takes a second such sum, of 2^u u, whose size is the entropy's and a little, and changes by the variance of s
 (at most a quarter of its squared range) times what s is off by relative to itself."""
 import numpy as np
 import pytest
@@ -128,6 +128,22 @@ def test_infinities_nan_and_lowest_values(mrl, V, dtype):
             assert torch.equal(a["ids"].view(80, 14, k), b["ids"].expand(80, 14, k))
         assert torch.equal(torch.isnan(a["lse"]).view(80, 14), torch.isnan(b["lse"]).expand(80, 14))
         assert torch.allclose(a["lse"].view(80, 14), b["lse"].expand(80, 14), rtol=1e-6, atol=1e-5, equal_nan=True)
+
+
+@pytest.mark.parametrize("V", [9, 700, 30011])
+@pytest.mark.parametrize("N", [2, 1100])
+def test_logits_that_fill_the_range(mrl, N, V):
+    # At this temperature the scale is 8192, a power of two, so that the largest float over it, scaled, is the largest float exactly: its distance from where
+    # a thread's running maximum begins is infinite, though the sum of exponentials is not.  Three such logits: entropy log 3, good to the rounding of the result.
+    T = float(np.float32(1.4426950408889634 / 8192))
+    assert np.float32(1.4426950408889634 / T) == np.float32(8192)
+    z = torch.zeros((N, V), device="cuda")
+    z[:, [1, 4, 8]] = torch.finfo(F32).max / 8192
+    r = mrl.top_logprobs(z, 3, temperature=T)
+    assert torch.equal(r["ids"], torch.tensor([1, 4, 8], dtype=torch.int32, device="cuda").expand(N, 3))
+    _near("entropy", r["entropy"], np.full(N, np.log(3.0)), 4 * U * np.log(3.0))
+    want = float(z[0, 1]) / T
+    _near("lse", r["lse"], np.full(N, want), 4 * U * want)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
