@@ -651,13 +651,13 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     // (rows of the pass at most, as far as the caller says)
     const int64_t hinted = cfg->scored_rows_hint > 0 ? cfg->scored_rows_hint - c0 : L.chunk_rows;
     const int expected = (int)(hinted < L.chunk_rows ? hinted : L.chunk_rows);
-    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected, V, d, false);
+    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected, L.chunk_rows, V, d, false);
     if (bf16 && out_dW) {
       // the stash already holds the backward operand; the dW launch needs the pass's gathered rows, each
       // times its row scale, transposed, and zeros behind the last valid row
       Scope sc(MRL_PROF_CONVERT, s);
       launch_backward_rows_b16(at<void>(ws, L.Hc), L.ldh, at<float>(ws, L.row_scale) + c0, at<void>(ws, L.Ht), L.ldr,
-                               n_scored, c0, L.chunk_rows, L.dp, at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, s);
+                               n_scored, c0, L.chunk_rows, L.dp, at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, false, s);
     } else if (!bf16 && !row_f32) {
       Scope sc(MRL_PROF_CONVERT, s);
       launch_convert_f32(at<float>(ws, L.Z), L.ldz, at<float>(ws, L.lse_c), at<float>(ws, L.g_c), target_ids, row_index,
@@ -784,22 +784,24 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
       if (dW) { Scope sc(MRL_PROF_GEMM_DW, s); launch_gemm_f32(p.w, s); }
       continue;
     }
-    const bool dw_blocks = dw_rows_in_blocks(rows, V, d, dw_bf16 && !sum_apart);
+    const bool dw16 = dw_bf16 && !sum_apart, dw_blocks = dw_rows_in_blocks(rows, L.chunk_rows, V, d, dw16), resident = dw_resident(L.chunk_rows, d, dw16);
+    auto head_gradient = [&] {
+      Scope sc(MRL_PROF_GEMM_DW, s);
+      launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW, dw16, overwrite,
+                          at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
+    };
     if (dW) {
       Scope sc(MRL_PROF_CONVERT, s);
       launch_backward_rows_b16(at<void>(ws, L.Hc), L.ldh, a.row_scale + c0, at<void>(ws, L.Ht), L.ldr, n_scored, c0, L.chunk_rows, L.dp,
-                               at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, s);
+                               at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, resident, s);
     }
+    if (dW && resident) head_gradient();                  // (before the head's rows push the stash out of the memory-side cache)
     if (out_dH) {
       Scope sc(MRL_PROF_GEMM_DH, s);
       launch_gemm_dh_bf16(at<void>(ws, L.Z), L.ldz, lm_head_w, d, V, row_index, a.row_scale, n_scored, c0, L.chunk_rows, d, out_dH,
                           cfg->dh_dtype == MRL_F32, at<float>(ws, L.tail), L.tail_items, s);
     }
-    if (dW) {
-      Scope sc(MRL_PROF_GEMM_DW, s);
-      launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW,
-                          dw_bf16 && !sum_apart, overwrite, at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
-    }
+    if (dW && !resident) head_gradient();
   }
   Scope sc(MRL_PROF_FINAL, s);
   if (sum_apart) launch_to_bf16(dW, out_dW, (int64_t)V * d, s);

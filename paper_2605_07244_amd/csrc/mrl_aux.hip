@@ -3,6 +3,7 @@
 // preparation, the fp32 path's logits -> dz conversion, final reductions.
 #include "mrl_finalize.h"
 #include "mrl_internal.h"
+#include "mrl_vec.h"
 
 namespace mrl {
 namespace {
@@ -879,6 +880,7 @@ __global__ __launch_bounds__(256) void k_convert_f32(float* ZP, int64_t ldz, con
 // rows, zeros up to the multiple of 128 the contraction runs over.  Tile 64 rows x 64 cols; n_cols a
 // multiple of 64, 16-byte aligned rows on both sides.  The blocks behind the tiles clear the stash
 // rows between the valid count and that multiple (the contraction must not meet stale bits there).
+constexpr int kFetched = 4;
 __global__ __launch_bounds__(256) void k_backward_rows_b16(const uint16_t* in, int64_t ld_in, const float* scale,
                                                            uint16_t* out, int64_t ld_out, const int64_t* n_scored,
                                                            int64_t chunk_start, int chunk_rows, int row_tiles,
@@ -886,6 +888,21 @@ __global__ __launch_bounds__(256) void k_backward_rows_b16(const uint16_t* in, i
   __shared__ __attribute__((aligned(16))) uint16_t tile[64 * 72];
   const int nrows = valid_rows(n_scored, chunk_start, chunk_rows);
   const int nzero = (nrows + 127) / 128 * 128 < chunk_rows ? (nrows + 127) / 128 * 128 : chunk_rows;
+  if ((int)blockIdx.y >= row_tiles + 127) {
+    // (behind those: the valid stash rows are read, kFetched vectors of a row per thread, for the memory-side cache)
+    const int each = gridDim.x * 256 * kFetched, parts = (Vp / 8 + each - 1) / each, b = blockIdx.y - row_tiles - 127, i = b / parts;
+    if (i >= nrows) return;
+    const int v0 = b % parts * each + blockIdx.x * 256 + threadIdx.x;
+    u32x4 x[kFetched];
+#pragma unroll
+    for (int k = 0; k < kFetched; ++k) {
+      const int v = v0 + k * (int)gridDim.x * 256;
+      x[k] = *reinterpret_cast<const u32x4*>(E + (int64_t)i * lde + (v < Vp / 8 ? v : 0) * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < kFetched; ++k) asm volatile("" :: "v"(x[k]));
+    return;
+  }
   if ((int)blockIdx.y >= row_tiles) {
     const int i = nrows + blockIdx.y - row_tiles;
     if (i >= nzero) return;
@@ -1018,9 +1035,9 @@ void launch_convert_f32(float* ZP, int64_t ldz, const float* lse_c,
 
 void launch_backward_rows_b16(const void* Hc, int64_t ldh, const float* scale, void* Ht, int64_t ldht,
                               const int64_t* n_scored, int64_t chunk_start, int chunk_rows, int dp, void* E, int64_t lde,
-                              int Vp, bool in_blocks, hipStream_t stream) {
-  const int row_tiles = chunk_rows / 64;
-  hipLaunchKernelGGL(k_backward_rows_b16, dim3(dp / 64, (unsigned)(row_tiles + 127)), dim3(256), 0, stream,
+                              int Vp, bool in_blocks, bool fetch, hipStream_t stream) {
+  const int row_tiles = chunk_rows / 64, each = dp / 64 * 256 * kFetched, fetches = fetch ? chunk_rows * ((Vp / 8 + each - 1) / each) : 0;
+  hipLaunchKernelGGL(k_backward_rows_b16, dim3(dp / 64, (unsigned)(row_tiles + 127 + fetches)), dim3(256), 0, stream,
                      static_cast<const uint16_t*>(Hc), ldh, scale, static_cast<uint16_t*>(Ht), ldht, n_scored,
                      chunk_start, chunk_rows, row_tiles, static_cast<uint16_t*>(E), lde, Vp, in_blocks);
 }

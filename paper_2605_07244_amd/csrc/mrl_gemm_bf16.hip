@@ -1449,6 +1449,29 @@ constexpr int D_LOADS = 6;                                          // direct lo
 // tiles leave little to gain, 327 rows 483 and 484, 1000 rows 825 and 846 a call.
 constexpr int kFewDwRows = 1024;
 
+// 16 rows of a bf16 dW from row v0 on, 64 columns from n0 on, of accumulators that hold row frow, columns 16 j + 4 fq + e per lane: 16 bytes per lane; of a pair of
+// them, lanes frow < 8 and frow >= 8 exchange one, and a store covers 8 rows x 128 bytes.
+__device__ __forceinline__ void put_16_rows(const Params& p, const f32x4* acc, int v0, int n0) {
+  const int lane = threadIdx.x & 63, frow = lane & 15, fq = lane >> 4;
+  const u32x4_any a = eight_bf16(acc[0], acc[1]), b = eight_bf16(acc[2], acc[3]);
+  const int n = n0 + (2 * (frow >> 3) + (fq & 1)) * 16 + 8 * (fq >> 1);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    u32x4_any x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = half == 0 ? (uint32_t)__builtin_amdgcn_update_dpp((int)a[e], (int)b[e], 0x128, 0xf, 0xc, false)
+                       : (uint32_t)__builtin_amdgcn_update_dpp((int)b[e], (int)a[e], 0x128, 0xf, 0x3, false);
+    const int v = v0 + (frow & 7) + 8 * half;
+    uint16_t* const at = reinterpret_cast<uint16_t*>(p.dW) + (int64_t)v * p.d + n;
+    if (v < p.V && n < p.d) {
+      // (as the compiler has it, the two stores become one, and no streaming one)
+      if (p.streaming) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" :: "v"(at), "v"(x) : "memory");
+      else *reinterpret_cast<u32x4_any*>(at) = x;
+    }
+  }
+}
+
 template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_bf16(Params p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1535,27 +1558,10 @@ template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_b
   // columns, the second rows 8 - 15.
   const int v0 = m0 + wm * 64 + (frow & 7), nb = n0 + wn * 128 + 16 * (frow >> 3) + 4 * fq;
   if (BF16_OUT) {
-    // 16 bytes per lane; of a pair of them, lanes frow < 8 and frow >= 8 exchange one, and a store covers 8 rows x 128 bytes
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u32x4_any a = eight_bf16(acc[i][4 * q], acc[i][4 * q + 1]), b = eight_bf16(acc[i][4 * q + 2], acc[i][4 * q + 3]);
-        const int n = n0 + wn * 128 + (4 * q + 2 * (frow >> 3) + (fq & 1)) * 16 + 8 * (fq >> 1);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          u32x4_any x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[e] = half == 0 ? (uint32_t)__builtin_amdgcn_update_dpp((int)a[e], (int)b[e], 0x128, 0xf, 0xc, false)
-                             : (uint32_t)__builtin_amdgcn_update_dpp((int)b[e], (int)a[e], 0x128, 0xf, 0x3, false);
-          const int v = v0 + i * 16 + 8 * half;
-          uint16_t* const at = reinterpret_cast<uint16_t*>(p.dW) + (int64_t)v * p.d + n;
-          if (v < p.V && n < p.d) {
-            if (p.streaming) __builtin_nontemporal_store(x, reinterpret_cast<u32x4_any*>(at)); else *reinterpret_cast<u32x4_any*>(at) = x;
-          }
-        }
-      }
+      for (int q = 0; q < 2; ++q) put_16_rows(p, acc[i] + 4 * q, m0 + wm * 64 + i * 16, n0 + wn * 128 + q * 64);
     return;
   }
 #pragma unroll
@@ -1588,6 +1594,117 @@ template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_b
         if (p.streaming) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" :: "v"(at[j]), "v"(x[j]) : "memory");
         else *reinterpret_cast<f32x4_any*>(at[j]) = x[j];
       }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// A bf16 dW of at most 256 rows: a workgroup of eight waves keeps its 256 columns of the scaled hidden rows in registers, 64 columns a wave and all rows of them, and
+// goes through a range of the vocabulary, 64 stash columns at a time, four to twelve such stages in LDS (what 160 KB hold of them).  Bound by its stores: they go out
+// while the next stages' products run, so that a launch takes little more than the stores alone (probe, V = 151936: d = 1536 95 us, d = 4096 220).  Launch, us, here and
+// before (the larger tiles, a product and its stores after one another): d = 1536, 30 rows 99 and 194, 200 rows 107 to 140 with the clock that is left under load (without its stores
+// 97), before 208; d = 4096, 256 rows 285 to 360 and 525; V = 50257, d = 712, 200 rows 26 and 41.
+// Reads from memory wait behind the stores: with the stash read from there, forward's stores being long displaced by W, 200 rows took 182 us, however
+// many stages were on their way.  So launch_backward_rows_b16 reads the stash once (10 us of 78 MB), and this launch comes next, before dH reads W again.
+// ---------------------------------------------------------------------------------------------
+constexpr int GM = 64, GN = 256, G_ROWS = 256, G_LDS = 160 * 1024, G_STORES = 4 /*of a wave and stage*/, G_THREADS = 512;
+
+// Stash rows in LDS, 128 bytes each: row k's slot of 32 bytes s is at s ^ gswz(k), so that the transposing reads of rows 0 - 3 and 8 - 11 fall on all banks.
+__device__ inline int gswz(int k) { return (k >> 1 & 1) | (k >> 3 & 1) << 1; }
+
+// NK: 32-row steps of the products.
+template <int NK> __device__ __forceinline__ void dw_resident_range(const Params& p, unsigned char* smem, int n0, int first, int last) {
+  constexpr int NL = (NK + 1) / 2, kStage = NL * 64 * GM * 2, kFit = G_LDS / kStage, G_STAGES = kFit < 12 ? kFit : 12;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int frow = lane & 15, fq = lane >> 4, wm = wave >> 2, nw = n0 + (wave & 3) * 64;
+  // direct loads of 1 KB: 8 stash rows x 128 bytes
+  const uint16_t* src[NL];
+  uint32_t dst[NL];
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int blk = wave * NL + i, k = blk * 8 + (lane >> 3);
+    src[i] = p.A + (int64_t)k * p.lda + (((lane & 7) ^ (gswz(k) << 1)) << 3);
+    dst[i] = __builtin_amdgcn_readfirstlane(lds_base + blk * 1024);
+  }
+  auto load = [&](int t, int slot) {
+    t = t < last ? t : last - 1;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      uint64_t addr;
+      asm volatile("s_mov_b32 m0, %3\n\tv_lshl_add_u64 %0, %1, 0, %2\n\tglobal_load_lds_dwordx4 %0, off"
+                   : "=&v"(addr) : "v"(src[i]), "s"((int64_t)t * (GM * 2)), "s"(dst[i] + slot * kStage) : "memory");
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < G_STAGES - 1; ++s) load(first + s, s);
+  bf16x8 fb[NK][4];
+#pragma unroll
+  for (int k = 0; k < NK; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int n = nw + j * 16 + frow;
+      fb[k][j] = *reinterpret_cast<const bf16x8*>(p.B + ((int64_t)k * p.ldb + (n < p.N ? n : p.N - 1)) * kRowBlock + 8 * fq);
+    }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  const int kr = 8 * fq + (frow >> 2);
+  const uint32_t a_base = kr * (GM * 2) + ((frow & 3) << 3);
+  const bool live = nw < p.d;                          // the wave has columns to store
+  int slot = 0, load_slot = G_STAGES - 1;
+  for (int t = first; t < last; ++t) {
+    // This stage has landed when what was issued behind its loads is all that is outstanding: the next two stages' loads, and the last three
+    // stages' stores (every one of which is issued: only a range's last stage has rows behind V).
+    if (live && t - first >= G_STAGES - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((G_STAGES - 2) * NL + (G_STAGES - 1) * G_STORES));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm((G_STAGES - 2) * NL));
+    __syncthreads();
+    load(t + G_STAGES - 1, load_slot);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f32x4 acc[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        typedef short v4i16 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) v4i16* lds_v4i16;
+        unsigned char* const q = smem + slot * kStage + k * (32 * GM * 2) + a_base + (((wm * 2 + i) ^ gswz(kr)) << 5);
+        const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16)q);
+        const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16)(q + 4 * (GM * 2)));
+        const bf16x8 fa = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[k][j], fa, acc[j], 0, 0, 0);
+      }
+      if (live) put_16_rows(p, acc, t * GM + wm * 32 + i * 16, nw);
+    }
+    slot = (slot + 1) % G_STAGES;
+    load_slot = (load_slot + 1) % G_STAGES;
+  }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));            // no direct load may outlive the wave
+}
+
+__global__ __launch_bounds__(G_THREADS) void dw_resident_bf16(Params p) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  int64_t nv64 = *p.n_scored - p.chunk_start;
+  const int nvalid = nv64 < 0 ? 0 : (nv64 > p.chunk_rows ? p.chunk_rows : (int)nv64);
+  // groups of workgroups, one for each 256 columns, side by side on an XCD: they go through the same part of the stash
+  const int across = (p.d + GN - 1) / GN, groups = kRound / across, rank = blockIdx.x % NXCD * kXcdCus + blockIdx.x / NXCD, group = rank / across;
+  if (group >= groups) return;
+  const int n0 = rank % across * GN, T = (p.V + GM - 1) / GM;
+  const int first = (int)((int64_t)T * group / groups), last = (int)((int64_t)T * (group + 1) / groups);
+  if (first >= last) return;
+  switch ((nvalid + 31) / 32) {
+    case 0: {
+      const int v_last = last * GM < p.V ? last * GM : p.V;
+      if (threadIdx.x < NTHREADS) zero_rows(p.dW + ((int64_t)first * GM * p.d + n0) / 2, p.d / 2, v_last - first * GM, (p.d - n0 < GN ? p.d - n0 : GN) / 2);
+      return;
+    }
+    case 1: return dw_resident_range<1>(p, smem, n0, first, last);
+    case 2: return dw_resident_range<2>(p, smem, n0, first, last);
+    case 3: return dw_resident_range<3>(p, smem, n0, first, last);
+    case 4: return dw_resident_range<4>(p, smem, n0, first, last);
+    case 5: return dw_resident_range<5>(p, smem, n0, first, last);
+    case 6: return dw_resident_range<6>(p, smem, n0, first, last);
+    case 7: return dw_resident_range<7>(p, smem, n0, first, last);
+    default: return dw_resident_range<8>(p, smem, n0, first, last);
   }
 }
 
@@ -1972,12 +2089,14 @@ int gemm_tail_items(size_t head_bytes) {
 }
 // (as many of 256 x 256: what a workspace had before the tiles grew; their last round is then cut into fewer slices)
 size_t gemm_tail_bytes_least(size_t head_bytes) { return (size_t)gemm_tail_items(head_bytes) * RES * RES * sizeof(float); }
-// A bf16 dW has half the stores to hide, and with enough tiles the larger ones' smaller traffic counts for more at any number of rows.  dW's share of a call, us, this launch
-// and the large tile: V = 151936, d = 4096, 200 rows 618 and 514, 1000 rows 1304 and 1070; d = 1536 260 and 256, 539 and 470; V = 100000, d = 1536 (2346 tiles of
-// 256) 300 rows 193 and 183, 1000 rows 355 and 324; V = 32000, d = 4096 (2000) 156 and 161, 282 and 273; V = 50257, d = 2048 (1576) 400 rows 159 and 185, 700 rows 190 and 212.
+// Passes of up to 256 rows with a bf16 dW keep their hidden rows in registers (as many columns as workgroups are there for them).  Of the longer ones, those with many
+// tiles take the large ones: a bf16 dW has half the stores to hide, and the larger tiles' smaller traffic counts for more.  dW's share of a call, us, the launch for
+// few rows and the large tile: V = 151936, d = 1536 (3564 tiles of 256) 300 rows 305 and 300, 600 rows 371 and 358, 1000 rows 520 and 470; V = 128256, d = 3584 (7014) 457 and 462, 640 and 600,
+// 930 and 830; V = 32000, d = 4096 (2000) 145 and 161, 183 and 194, 270 and 281; V = 50257, d = 2048 (1576) 114 and 140, 163 and 201, 226 and 262.
 constexpr int kFewDw16Tiles = 8 * kRound;
-bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16) {
-  return rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles);
+bool dw_resident(int chunk_rows, int d, bool dw_bf16) { return dw_bf16 && chunk_rows <= G_ROWS && d <= 64 * GN; }
+bool dw_rows_in_blocks(int rows, int chunk_rows, int V, int d, bool dw_bf16) {
+  return dw_resident(chunk_rows, d, dw_bf16) || (rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles));
 }
 
 void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldht,
@@ -1994,7 +2113,12 @@ void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldh
   if (in_blocks) {
     p.N = (int)ldht;                                  // (rows of a block: d rounded up to 128)
     p.streaming = d % (dw_bf16 ? 64 : 32) == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
-    static LdsLimit lds_limit[2];
+    static LdsLimit lds_limit[3];
+    if (dw_resident(chunk_rows, d, dw_bf16 != 0)) {
+      lds_limit[2].ensure(reinterpret_cast<const void*>(&dw_resident_bf16), G_LDS);
+      hipLaunchKernelGGL(dw_resident_bf16, dim3(kRound), dim3(G_THREADS), G_LDS, stream, p);
+      return;
+    }
     const auto kernel = dw_bf16 ? &dw_few_bf16<true> : &dw_few_bf16<false>;
     lds_limit[dw_bf16].ensure(reinterpret_cast<const void*>(kernel), D_LDS);
     const int64_t tiles = (int64_t)((V + DM - 1) / DM) * ((d + DN - 1) / DN);
@@ -2058,7 +2182,7 @@ extern "C" int mrl_diag_gemm_cut(int32_t launch, int32_t rows, int32_t expected,
     out9[4] = all % kRound; out9[5] = split; out9[6] = blocks;
   };
   if (launch == MRL_PROF_GEMM_DW) {
-    if (dw_rows_in_blocks(expected, V, d, false)) return MRL_OK;
+    if (dw_rows_in_blocks(expected, chunk_rows, V, d, false)) return MRL_OK;
     const DwPlan plan = plan_dw(chunk_rows, expected, V, d, items);
     const int panels = dw_panels(rows, chunk_rows);
     if (plan.wide) put(tiles(V, RING), 0, 0, plan.tiles, plan.rest > 0 ? dw_split(plan.rest, panels, items) : 1, plan.blocks);

@@ -92,7 +92,8 @@ void launch_gemm_dh_bf16(const void* E, int64_t lde, const void* W, int64_t ldw,
 size_t gemm_tail_tile_bytes();
 int gemm_tail_items(size_t head_bytes);               // of a workspace, for a head of so many bytes
 size_t gemm_tail_bytes_least(size_t head_bytes);      // ... in one that has no room for them all
-bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16);
+bool dw_resident(int chunk_rows, int d, bool dw_bf16);
+bool dw_rows_in_blocks(int rows, int chunk_rows, int V, int d, bool dw_bf16);
 void launch_gemm_dw_bf16(const void* P, int64_t ldp, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                          int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
@@ -220,10 +221,11 @@ void launch_convert_f32(float* ZP, int64_t ldz, const float* lse_c,
 // bf16 path, operands of the dW launch (Hc as the row preparation wrote it): Ht[c][r] = scale[r] * Hc[r][c] (c < dp, a multiple of 64) for the
 // pass's valid rows, zeros up to their multiple of 128; the stash rows in between are cleared (the
 // dW contraction runs over pairs of 64-row panels; the forward kernel writes valid rows only).
-// in_blocks: Ht[r / 32][c][r % 32] instead.
+// in_blocks: Ht[r / 32][c][r % 32] instead.  fetch (at most 256 rows): the valid stash rows are read as well, which leaves them in the memory-side cache for a launch
+// that comes next and would wait for them behind its own stores.
 void launch_backward_rows_b16(const void* Hc, int64_t ldh, const float* scale, void* Ht, int64_t ldht,
                               const int64_t* n_scored, int64_t chunk_start, int chunk_rows, int dp, void* E, int64_t lde,
-                              int Vp, bool in_blocks, hipStream_t stream);
+                              int Vp, bool in_blocks, bool fetch, hipStream_t stream);
 
 // Group-relative advantages (Sec. 3) with pooled / own statistics and SGT gate flags.
 void launch_group_advantages(const float* rewards, const int32_t* group_id, const uint8_t* in_stats,

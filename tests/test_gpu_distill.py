@@ -205,6 +205,30 @@ def test_bf16_gradient_of_a_large_head_and_few_rows(mrl, N, d, V):
     assert torch.all((a["dW"] - b["dW"].float()).abs() <= 2.0 ** -8 * a["dW"].abs() + 2 * N * U * mag)
 
 
+@pytest.mark.parametrize("N,scored,d,V", [
+    (1, 1, 8, 1), (32, 32, 264, 63), (33, 33, 712, 64), (70, 64, 1536, 1000), (100, 100, 256, 20011), (130, 128, 136, 70001), (140, 129, 1032, 4097),
+    (192, 161, 4096, 3001), (200, 200, 1536, 9999), (225, 225, 2056, 5003), (256, 256, 3080, 12345), (256, 0, 520, 777), (200, 0, 2048, 30000),
+    (256, 250, 16384, 500), (256, 250, 16392, 300), (20, 20, 64, 151936)])
+def test_bf16_gradient_of_up_to_256_rows(mrl, N, scored, d, V):
+    """Hidden rows in registers: every number of steps, one stage and many of them, ranges of the vocabulary that end beside it, widths beside the waves'."""
+    h, w = rand((N, d), BF16, N), rand((V, d), BF16, N + 1, 2.0 / d ** 0.5)
+    g = torch.Generator("cuda").manual_seed(N)
+    ids = torch.randint(0, V, (N, 7), device="cuda", generator=g, dtype=torch.int32)
+    logp = -3 * torch.rand(N, 7, device="cuda", generator=g)
+    mask = (torch.randperm(N, device="cuda", generator=g) < scored).to(torch.uint8)
+    out = []
+    for dw in (mrl.F32, mrl.BF16, mrl.BF16):
+        cfg = mrl.DistillConfig(dw_dtype=dw)
+        ws = torch.full((mrl.distill_loss_workspace(N, d, V, 7, mrl.BF16, cfg),), 255, dtype=torch.uint8, device="cuda")
+        dW = torch.full((V + 2, d), float("nan"), device="cuda", dtype=F32 if dw == mrl.F32 else BF16)
+        r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, cfg, token_mask=mask, out_dW=dW[1:V + 1], want_dH=len(out) < 2, workspace=ws)
+        assert torch.all(torch.isnan(dW[0].float())) and torch.all(torch.isnan(dW[V + 1].float()))
+        out.append(r)
+    a, b, c = out
+    assert torch.equal(a["dW"].bfloat16(), b["dW"]) and torch.equal(b["dW"], c["dW"]) and torch.equal(a["dH"], b["dH"]) and torch.equal(a["kl"], c["kl"])
+    assert scored > 0 or torch.all(b["dW"] == 0)
+
+
 def test_bf16_gradient_at_any_address(mrl):
     N, d, V = 1500, 136, 900
     h, w, ids, logp = _case(N, d, V, 7, BF16, 3)
