@@ -92,7 +92,7 @@ def _check_back(mrl, dy, ids, V, scale=1.0, mask=None, out=F32, base=None):
     return got
 
 
-@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 33, 64, 65, 1000, 4095, 4096, 4097, 8193, 20000])
+@pytest.mark.parametrize("N", [1, 2, 7, 8, 9, 15, 16, 17, 33, 64, 65, 1000, 4095, 4096, 4097, 8193, 20000])
 @pytest.mark.parametrize("V", [1, 3, 511, 512, 5000])
 def test_gradient_sizes(mrl, N, V):
     _check_back(mrl, rand((N, 72), F32, N + V), _ids(N, V, N * V, -1, V + 1), V, 1.7)
