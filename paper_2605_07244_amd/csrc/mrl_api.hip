@@ -651,7 +651,7 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     // (rows of the pass at most, as far as the caller says)
     const int64_t hinted = cfg->scored_rows_hint > 0 ? cfg->scored_rows_hint - c0 : L.chunk_rows;
     const int expected = (int)(hinted < L.chunk_rows ? hinted : L.chunk_rows);
-    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected, L.chunk_rows, V, d, false);
+    const bool dw_blocks = bf16 && dw_rows_in_blocks(expected, V, d, false);
     if (bf16 && out_dW) {
       // the stash already holds the backward operand; the dW launch needs the pass's gathered rows, each
       // times its row scale, transposed, and zeros behind the last valid row
@@ -685,7 +685,7 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
     if (out_dW) {
       Scope sc(MRL_PROF_GEMM_DW, s);
       launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0,
-                          L.chunk_rows, V, d, out_dW, 0, overwrite, at<float>(ws, L.tail), L.tail_items, expected, dw_blocks, s);
+                          L.chunk_rows, V, d, out_dW, 0, overwrite, at<float>(ws, L.tail), L.tail_items, expected, dw_blocks, false, s);
     }
   }
   if (!finalized) {
@@ -784,11 +784,11 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
       if (dW) { Scope sc(MRL_PROF_GEMM_DW, s); launch_gemm_f32(p.w, s); }
       continue;
     }
-    const bool dw16 = dw_bf16 && !sum_apart, dw_blocks = dw_rows_in_blocks(rows, L.chunk_rows, V, d, dw16), resident = dw_resident(L.chunk_rows, d, dw16);
+    const bool dw16 = dw_bf16 && !sum_apart, resident = dw_can_be_resident(L.chunk_rows, d, overwrite), dw_blocks = resident || dw_rows_in_blocks(rows, V, d, dw16);
     auto head_gradient = [&] {
       Scope sc(MRL_PROF_GEMM_DW, s);
       launch_gemm_dw_bf16(at<void>(ws, L.Z), L.ldz, at<void>(ws, L.Ht), dw_blocks ? L.dp : L.ldr, n_scored, c0, L.chunk_rows, V, d, dW, dw16, overwrite,
-                          at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, s);
+                          at<float>(ws, L.tail), L.tail_items, rows, dw_blocks, resident, s);
     };
     if (dW) {
       Scope sc(MRL_PROF_CONVERT, s);

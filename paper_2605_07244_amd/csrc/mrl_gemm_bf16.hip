@@ -1598,22 +1598,52 @@ template <bool BF16_OUT> __global__ __launch_bounds__(NTHREADS, 2) void dw_few_b
 }
 
 // ---------------------------------------------------------------------------------------------
-// A bf16 dW of at most 256 rows: a workgroup of eight waves keeps its 256 columns of the scaled hidden rows in registers, 64 columns a wave and all rows of them, and
-// goes through a range of the vocabulary, 64 stash columns at a time, four to twelve such stages in LDS (what 160 KB hold of them).  Bound by its stores: they go out
-// while the next stages' products run, so that a launch takes little more than the stores alone (probe, V = 151936: d = 1536 95 us, d = 4096 220).  Launch, us, here and
-// before (the larger tiles, a product and its stores after one another): d = 1536, 30 rows 99 and 194, 200 rows 107 to 140 with the clock that is left under load (without its stores
-// 97), before 208; d = 4096, 256 rows 285 to 360 and 525; V = 50257, d = 712, 200 rows 26 and 41.
-// Reads from memory wait behind the stores: with the stash read from there, forward's stores being long displaced by W, 200 rows took 182 us, however
+// dW of a pass of at most 256 rows, overwritten: a workgroup of eight waves keeps its 256 columns of the scaled hidden rows in registers, 64 columns a wave and all rows of
+// them, and goes through a range of the vocabulary, 64 stash columns at a time, five to twelve such stages in LDS (what 160 KB hold of them).  Bound by its stores: they go
+// out while the next stages' products run, so that a launch takes little more than the stores alone (probe, bf16, V = 151936: d = 1536 95 us, d = 4096 220).  Launch with a bf16
+// dW, us, here and on the larger tiles, a product and its stores after one another: d = 1536, 30 rows 99 and 194, 200 rows 107 to 140 with the clock that is left under load (without
+// its stores 97) and 208; d = 4096, 256 rows 285 to 360 and 525; V = 50257, d = 712, 200 rows 26 and 41.  dW's share of a call with a float dW, here and in dw_few_bf16: V = 151936, d = 1536, 200
+// rows 215 and 319, d = 4096 460 and 743; V = 50257, d = 2048 80 and 134; one row 211 and 222, 427 and 460, 91 and 88, and V = 128256, d = 3584 385 and 350.
+// Reads from memory wait behind the stores: with the stash read from there, forward's stores being long displaced by W, 200 rows took 182 us (bf16), however
 // many stages were on their way.  So launch_backward_rows_b16 reads the stash once (10 us of 78 MB), and this launch comes next, before dH reads W again.
 // ---------------------------------------------------------------------------------------------
-constexpr int GM = 64, GN = 256, G_ROWS = 256, G_LDS = 160 * 1024, G_STORES = 4 /*of a wave and stage*/, G_THREADS = 512;
+constexpr int GM = 64, GN = 256, G_ROWS = 256, G_LDS = 160 * 1024, G_THREADS = 512;
 
 // Stash rows in LDS, 128 bytes each: row k's slot of 32 bytes s is at s ^ gswz(k), so that the transposing reads of rows 0 - 3 and 8 - 11 fall on all banks.
 __device__ inline int gswz(int k) { return (k >> 1 & 1) | (k >> 3 & 1) << 1; }
 
+// As put_16_rows, floats: a store covers 8 rows x 128 bytes, half the columns of a pair of blocks.
+__device__ __forceinline__ void put_16_float_rows(const Params& p, const f32x4* acc, int v0, int n0) {
+  const int lane = threadIdx.x & 63, frow = lane & 15, fq = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const f32x4 a = acc[j & ~1], b = acc[j | 1];
+    f32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int ia = __float_as_int(a[e]), ib = __float_as_int(b[e]);
+      x[e] = __int_as_float((j & 1) == 0 ? __builtin_amdgcn_update_dpp(ia, ib, 0x128, 0xf, 0xc, false)
+                                         : __builtin_amdgcn_update_dpp(ib, ia, 0x128, 0xf, 0x3, false));
+    }
+    const int v = v0 + (frow & 7) + 8 * (j & 1), n = n0 + 16 * (frow >> 3) + 4 * fq + 16 * (j & ~1);
+    float* const at = p.dW + (int64_t)v * p.d + n;
+    if (v < p.V && n < p.d) {
+      if (p.streaming) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" :: "v"(at), "v"(x) : "memory");
+      else *reinterpret_cast<f32x4_any*>(at) = x;
+    }
+  }
+}
+
+// Stages: what fits, and no more than the counter of outstanding accesses can tell apart.
+constexpr int g_stages(int loads, int stores) {
+  int n = 2;
+  while (n < 12 && (n + 1) * loads * 64 * GM * 2 <= G_LDS && (n - 1) * loads + n * stores <= 63) ++n;
+  return n;
+}
+
 // NK: 32-row steps of the products.
-template <int NK> __device__ __forceinline__ void dw_resident_range(const Params& p, unsigned char* smem, int n0, int first, int last) {
-  constexpr int NL = (NK + 1) / 2, kStage = NL * 64 * GM * 2, kFit = G_LDS / kStage, G_STAGES = kFit < 12 ? kFit : 12;
+template <bool BF16_OUT, int NK> __device__ __forceinline__ void dw_resident_range(const Params& p, unsigned char* smem, int n0, int first, int last) {
+  constexpr int NL = (NK + 1) / 2, kStage = NL * 64 * GM * 2, G_STORES = BF16_OUT ? 4 : 8 /*of a wave and stage*/, G_STAGES = g_stages(NL, G_STORES);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int frow = lane & 15, fq = lane >> 4, wm = wave >> 2, nw = n0 + (wave & 3) * 64;
   // direct loads of 1 KB: 8 stash rows x 128 bytes
@@ -1673,7 +1703,8 @@ template <int NK> __device__ __forceinline__ void dw_resident_range(const Params
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[k][j], fa, acc[j], 0, 0, 0);
       }
-      if (live) put_16_rows(p, acc, t * GM + wm * 32 + i * 16, nw);
+      if (!live) continue;
+      if (BF16_OUT) put_16_rows(p, acc, t * GM + wm * 32 + i * 16, nw); else put_16_float_rows(p, acc, t * GM + wm * 32 + i * 16, nw);
     }
     slot = (slot + 1) % G_STAGES;
     load_slot = (load_slot + 1) % G_STAGES;
@@ -1681,7 +1712,7 @@ template <int NK> __device__ __forceinline__ void dw_resident_range(const Params
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));            // no direct load may outlive the wave
 }
 
-__global__ __launch_bounds__(G_THREADS) void dw_resident_bf16(Params p) {
+template <bool BF16_OUT> __global__ __launch_bounds__(G_THREADS) void dw_resident(Params p) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   int64_t nv64 = *p.n_scored - p.chunk_start;
   const int nvalid = nv64 < 0 ? 0 : (nv64 > p.chunk_rows ? p.chunk_rows : (int)nv64);
@@ -1694,17 +1725,18 @@ __global__ __launch_bounds__(G_THREADS) void dw_resident_bf16(Params p) {
   switch ((nvalid + 31) / 32) {
     case 0: {
       const int v_last = last * GM < p.V ? last * GM : p.V;
-      if (threadIdx.x < NTHREADS) zero_rows(p.dW + ((int64_t)first * GM * p.d + n0) / 2, p.d / 2, v_last - first * GM, (p.d - n0 < GN ? p.d - n0 : GN) / 2);
+      constexpr int per = BF16_OUT ? 2 : 1;
+      if (threadIdx.x < NTHREADS) zero_rows(p.dW + ((int64_t)first * GM * p.d + n0) / per, p.d / per, v_last - first * GM, (p.d - n0 < GN ? p.d - n0 : GN) / per);
       return;
     }
-    case 1: return dw_resident_range<1>(p, smem, n0, first, last);
-    case 2: return dw_resident_range<2>(p, smem, n0, first, last);
-    case 3: return dw_resident_range<3>(p, smem, n0, first, last);
-    case 4: return dw_resident_range<4>(p, smem, n0, first, last);
-    case 5: return dw_resident_range<5>(p, smem, n0, first, last);
-    case 6: return dw_resident_range<6>(p, smem, n0, first, last);
-    case 7: return dw_resident_range<7>(p, smem, n0, first, last);
-    default: return dw_resident_range<8>(p, smem, n0, first, last);
+    case 1: return dw_resident_range<BF16_OUT, 1>(p, smem, n0, first, last);
+    case 2: return dw_resident_range<BF16_OUT, 2>(p, smem, n0, first, last);
+    case 3: return dw_resident_range<BF16_OUT, 3>(p, smem, n0, first, last);
+    case 4: return dw_resident_range<BF16_OUT, 4>(p, smem, n0, first, last);
+    case 5: return dw_resident_range<BF16_OUT, 5>(p, smem, n0, first, last);
+    case 6: return dw_resident_range<BF16_OUT, 6>(p, smem, n0, first, last);
+    case 7: return dw_resident_range<BF16_OUT, 7>(p, smem, n0, first, last);
+    default: return dw_resident_range<BF16_OUT, 8>(p, smem, n0, first, last);
   }
 }
 
@@ -2089,20 +2121,20 @@ int gemm_tail_items(size_t head_bytes) {
 }
 // (as many of 256 x 256: what a workspace had before the tiles grew; their last round is then cut into fewer slices)
 size_t gemm_tail_bytes_least(size_t head_bytes) { return (size_t)gemm_tail_items(head_bytes) * RES * RES * sizeof(float); }
-// Passes of up to 256 rows with a bf16 dW keep their hidden rows in registers (as many columns as workgroups are there for them).  Of the longer ones, those with many
-// tiles take the large ones: a bf16 dW has half the stores to hide, and the larger tiles' smaller traffic counts for more.  dW's share of a call, us, the launch for
+// Of passes with a bf16 dW those with many tiles take the large ones: it has half the stores to hide, and the larger tiles' smaller traffic counts for more.  dW's share of a call, us, the launch for
 // few rows and the large tile: V = 151936, d = 1536 (3564 tiles of 256) 300 rows 305 and 300, 600 rows 371 and 358, 1000 rows 520 and 470; V = 128256, d = 3584 (7014) 457 and 462, 640 and 600,
 // 930 and 830; V = 32000, d = 4096 (2000) 145 and 161, 183 and 194, 270 and 281; V = 50257, d = 2048 (1576) 114 and 140, 163 and 201, 226 and 262.
 constexpr int kFewDw16Tiles = 8 * kRound;
-bool dw_resident(int chunk_rows, int d, bool dw_bf16) { return dw_bf16 && chunk_rows <= G_ROWS && d <= 64 * GN; }
-bool dw_rows_in_blocks(int rows, int chunk_rows, int V, int d, bool dw_bf16) {
-  return dw_resident(chunk_rows, d, dw_bf16) || (rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles));
+// (columns: four workgroups to each part of the vocabulary at least)
+bool dw_can_be_resident(int chunk_rows, int d, int overwrite) { return overwrite && chunk_rows <= G_ROWS && d <= 64 * GN; }
+bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16) {
+  return rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles);
 }
 
 void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                          int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
-                         hipStream_t stream) {
+                         bool resident, hipStream_t stream) {
   Params p = {};
   p.A = static_cast<const uint16_t*>(E); p.lda = lde;
   p.B = static_cast<const uint16_t*>(Ht); p.ldb = ldht; p.N = d;
@@ -2113,12 +2145,14 @@ void launch_gemm_dw_bf16(const void* E, int64_t lde, const void* Ht, int64_t ldh
   if (in_blocks) {
     p.N = (int)ldht;                                  // (rows of a block: d rounded up to 128)
     p.streaming = d % (dw_bf16 ? 64 : 32) == 0 && (reinterpret_cast<uintptr_t>(dW) & 127) == 0;
-    static LdsLimit lds_limit[3];
-    if (dw_resident(chunk_rows, d, dw_bf16 != 0)) {
-      lds_limit[2].ensure(reinterpret_cast<const void*>(&dw_resident_bf16), G_LDS);
-      hipLaunchKernelGGL(dw_resident_bf16, dim3(kRound), dim3(G_THREADS), G_LDS, stream, p);
+    if (resident) {
+      static LdsLimit lds_limit[2];
+      const auto kernel = dw_bf16 ? &dw_resident<true> : &dw_resident<false>;
+      lds_limit[dw_bf16].ensure(reinterpret_cast<const void*>(kernel), G_LDS);
+      hipLaunchKernelGGL(kernel, dim3(kRound), dim3(G_THREADS), G_LDS, stream, p);
       return;
     }
+    static LdsLimit lds_limit[2];
     const auto kernel = dw_bf16 ? &dw_few_bf16<true> : &dw_few_bf16<false>;
     lds_limit[dw_bf16].ensure(reinterpret_cast<const void*>(kernel), D_LDS);
     const int64_t tiles = (int64_t)((V + DM - 1) / DM) * ((d + DN - 1) / DN);
@@ -2182,7 +2216,7 @@ extern "C" int mrl_diag_gemm_cut(int32_t launch, int32_t rows, int32_t expected,
     out9[4] = all % kRound; out9[5] = split; out9[6] = blocks;
   };
   if (launch == MRL_PROF_GEMM_DW) {
-    if (dw_rows_in_blocks(expected, chunk_rows, V, d, false)) return MRL_OK;
+    if (dw_rows_in_blocks(expected, V, d, false)) return MRL_OK;
     const DwPlan plan = plan_dw(chunk_rows, expected, V, d, items);
     const int panels = dw_panels(rows, chunk_rows);
     if (plan.wide) put(tiles(V, RING), 0, 0, plan.tiles, plan.rest > 0 ? dw_split(plan.rest, panels, items) : 1, plan.blocks);

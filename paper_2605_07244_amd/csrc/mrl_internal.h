@@ -89,15 +89,16 @@ void launch_gemm_dh_bf16(const void* E, int64_t lde, const void* W, int64_t ldw,
 // tiles; rows: the scored rows expected (which tiles the launch takes; right for any number).
 // in_blocks: the launch for few rows, with Ht in blocks of kRowBlock token rows, [chunk_rows / 32][ldht][32], ldht = d
 // rounded up to 128; dw_rows_in_blocks says where it is the faster one (rows: the scored rows expected; right for any number).
+// resident (in_blocks too, where dw_can_be_resident): the launch for at most 256 rows; wants the stash in the memory-side cache.
 size_t gemm_tail_tile_bytes();
 int gemm_tail_items(size_t head_bytes);               // of a workspace, for a head of so many bytes
 size_t gemm_tail_bytes_least(size_t head_bytes);      // ... in one that has no room for them all
-bool dw_resident(int chunk_rows, int d, bool dw_bf16);
-bool dw_rows_in_blocks(int rows, int chunk_rows, int V, int d, bool dw_bf16);
+bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16);
 void launch_gemm_dw_bf16(const void* P, int64_t ldp, const void* Ht, int64_t ldht,
                          const int64_t* n_scored, int64_t chunk_start, int chunk_rows,
                          int V, int d, void* dW, int dw_bf16, int overwrite, float* tail_part, int tail_items, int rows, bool in_blocks,
-                         hipStream_t stream);
+                         bool resident, hipStream_t stream);
+bool dw_can_be_resident(int chunk_rows, int d, int overwrite);
 
 // Scored rows of the pass of chunk_rows rows from chunk_start on.
 __device__ inline int valid_rows(const int64_t* n_scored, int64_t chunk_start, int chunk_rows) {

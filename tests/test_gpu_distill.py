@@ -209,7 +209,7 @@ def test_bf16_gradient_of_a_large_head_and_few_rows(mrl, N, d, V):
     (1, 1, 8, 1), (32, 32, 264, 63), (33, 33, 712, 64), (70, 64, 1536, 1000), (100, 100, 256, 20011), (130, 128, 136, 70001), (140, 129, 1032, 4097),
     (192, 161, 4096, 3001), (200, 200, 1536, 9999), (225, 225, 2056, 5003), (256, 256, 3080, 12345), (256, 0, 520, 777), (200, 0, 2048, 30000),
     (256, 250, 16384, 500), (256, 250, 16392, 300), (20, 20, 64, 151936)])
-def test_bf16_gradient_of_up_to_256_rows(mrl, N, scored, d, V):
+def test_gradient_of_the_head_of_up_to_256_rows(mrl, N, scored, d, V):
     """Hidden rows in registers: every number of steps, one stage and many of them, ranges of the vocabulary that end beside it, widths beside the waves'."""
     h, w = rand((N, d), BF16, N), rand((V, d), BF16, N + 1, 2.0 / d ** 0.5)
     g = torch.Generator("cuda").manual_seed(N)
@@ -227,6 +227,9 @@ def test_bf16_gradient_of_up_to_256_rows(mrl, N, scored, d, V):
     a, b, c = out
     assert torch.equal(a["dW"].bfloat16(), b["dW"]) and torch.equal(b["dW"], c["dW"]) and torch.equal(a["dH"], b["dH"]) and torch.equal(a["kl"], c["kl"])
     assert scored > 0 or torch.all(b["dW"] == 0)
+    # the launch that adds into a float dW, of nothing: the same products in the same order
+    r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(accumulate_dw=1), token_mask=mask, out_dW=torch.zeros(V, d, device="cuda"), want_dH=False)
+    assert torch.equal(r["dW"], a["dW"])
 
 
 def test_bf16_gradient_at_any_address(mrl):
