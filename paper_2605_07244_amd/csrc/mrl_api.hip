@@ -696,6 +696,9 @@ int mrl_grpo_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const int32
 }
 
 // --------------------------------------------------------------------------- (10)
+// A stash that the memory-side cache of 256 MB has room for is read into it before the launch that waits for it (dW's share of a call, us, with that and without: V = 450000, d = 1024,
+// 256 rows (230 MB) 320 and 357, 128 rows 215 and 303; V = 600000, 256 rows (307 MB) 470 and 465; V = 1000000, d = 512, 128 rows (256 MB) 389 and 327).
+constexpr int64_t kCachedStash = (int64_t)240 << 20;
 static int check_distill(int64_t N, int32_t d, int32_t V, int32_t k, int32_t dtype, const mrl_distill_config* c) {
   const int rc = check_common(N, d, V, dtype);
   if (rc != MRL_OK) return rc;
@@ -793,7 +796,7 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
     if (dW) {
       Scope sc(MRL_PROF_CONVERT, s);
       launch_backward_rows_b16(at<void>(ws, L.Hc), L.ldh, a.row_scale + c0, at<void>(ws, L.Ht), L.ldr, n_scored, c0, L.chunk_rows, L.dp,
-                               at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, resident, s);
+                               at<void>(ws, L.Z), L.ldz, (int)L.Vp, dw_blocks, resident && rows * L.Vp * 2 <= kCachedStash, s);
     }
     if (dW && resident) head_gradient();                  // (before the head's rows push the stash out of the memory-side cache)
     if (out_dH) {

@@ -881,6 +881,10 @@ __global__ __launch_bounds__(256) void k_convert_f32(float* ZP, int64_t ldz, con
 // multiple of 64, 16-byte aligned rows on both sides.  The blocks behind the tiles clear the stash
 // rows between the valid count and that multiple (the contraction must not meet stale bits there).
 constexpr int kFetched = 4;
+__host__ __device__ inline int fetch_parts(int Vp, int each) {         // blocks of a row (128 at most: 256 rows of them and the others are a grid's height)
+  const int n = (Vp / 8 + each - 1) / each;
+  return n < 128 ? n : 128;
+}
 __global__ __launch_bounds__(256) void k_backward_rows_b16(const uint16_t* in, int64_t ld_in, const float* scale,
                                                            uint16_t* out, int64_t ld_out, const int64_t* n_scored,
                                                            int64_t chunk_start, int chunk_rows, int row_tiles,
@@ -889,18 +893,19 @@ __global__ __launch_bounds__(256) void k_backward_rows_b16(const uint16_t* in, i
   const int nrows = valid_rows(n_scored, chunk_start, chunk_rows);
   const int nzero = (nrows + 127) / 128 * 128 < chunk_rows ? (nrows + 127) / 128 * 128 : chunk_rows;
   if ((int)blockIdx.y >= row_tiles + 127) {
-    // (behind those: the valid stash rows are read, kFetched vectors of a row per thread, for the memory-side cache)
-    const int each = gridDim.x * 256 * kFetched, parts = (Vp / 8 + each - 1) / each, b = blockIdx.y - row_tiles - 127, i = b / parts;
+    // (behind those: the valid stash rows are read, kFetched vectors of a row per thread at a time, for the memory-side cache)
+    const int each = gridDim.x * 256 * kFetched, parts = fetch_parts(Vp, each), b = blockIdx.y - row_tiles - 127, i = b / parts;
     if (i >= nrows) return;
-    const int v0 = b % parts * each + blockIdx.x * 256 + threadIdx.x;
-    u32x4 x[kFetched];
+    for (int v0 = b % parts * each + blockIdx.x * 256 + threadIdx.x; v0 < Vp / 8; v0 += parts * each) {
+      u32x4 x[kFetched];
 #pragma unroll
-    for (int k = 0; k < kFetched; ++k) {
-      const int v = v0 + k * (int)gridDim.x * 256;
-      x[k] = *reinterpret_cast<const u32x4*>(E + (int64_t)i * lde + (v < Vp / 8 ? v : 0) * 8);
+      for (int k = 0; k < kFetched; ++k) {
+        const int v = v0 + k * (int)gridDim.x * 256;
+        x[k] = *reinterpret_cast<const u32x4*>(E + (int64_t)i * lde + (v < Vp / 8 ? v : v0) * 8);
+      }
+#pragma unroll
+      for (int k = 0; k < kFetched; ++k) asm volatile("" :: "v"(x[k]));
     }
-#pragma unroll
-    for (int k = 0; k < kFetched; ++k) asm volatile("" :: "v"(x[k]));
     return;
   }
   if ((int)blockIdx.y >= row_tiles) {
@@ -1036,7 +1041,7 @@ void launch_convert_f32(float* ZP, int64_t ldz, const float* lse_c,
 void launch_backward_rows_b16(const void* Hc, int64_t ldh, const float* scale, void* Ht, int64_t ldht,
                               const int64_t* n_scored, int64_t chunk_start, int chunk_rows, int dp, void* E, int64_t lde,
                               int Vp, bool in_blocks, bool fetch, hipStream_t stream) {
-  const int row_tiles = chunk_rows / 64, each = dp / 64 * 256 * kFetched, fetches = fetch ? chunk_rows * ((Vp / 8 + each - 1) / each) : 0;
+  const int row_tiles = chunk_rows / 64, each = dp / 64 * 256 * kFetched, fetches = fetch ? chunk_rows * fetch_parts(Vp, each) : 0;
   hipLaunchKernelGGL(k_backward_rows_b16, dim3(dp / 64, (unsigned)(row_tiles + 127 + fetches)), dim3(256), 0, stream,
                      static_cast<const uint16_t*>(Hc), ldh, scale, static_cast<uint16_t*>(Ht), ldht, n_scored,
                      chunk_start, chunk_rows, row_tiles, static_cast<uint16_t*>(E), lde, Vp, in_blocks);
