@@ -33,19 +33,21 @@ template <int kEach> struct Alternatives {
   float t[kEach];
   double q[kEach], log_q[kEach], m;
   bool any;                                            // the slot counts
+  int too_large;                                       // ids that name no token though they are not negative
   __device__ void load(const DistillArgs& a, int64_t slot) {
     const int lane = threadIdx.x & 63;
     const int32_t* ids = a.ids + slot * a.k;
     const float* logp = a.logp + slot * a.k;
+    too_large = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int j = 64 * i + lane;
-      id[i] = -1;
-      t[i] = -INFINITY;
-      if (j < a.k) {
-        const int v = ids[j];
-        if (v >= 0 && v < a.V) { id[i] = v; t[i] = logp[j]; }
-      }
+      const bool in = j < a.k;
+      const int v = ids[in ? j : 0];
+      const float p = logp[in ? j : 0];                // (both under way at once)
+      id[i] = in && v >= 0 && v < a.V ? v : -1;
+      t[i] = id[i] >= 0 ? p : -INFINITY;
+      too_large += __popcll(__ballot(in && v >= a.V));
     }
   }
   // (best: the largest t; with nothing above -infinity and no NaN, nothing counts)
@@ -97,12 +99,6 @@ template <int kEach> struct Alternatives {
 
 __device__ inline float weight_of(const DistillArgs& a, int64_t slot) {
   return a.weight != nullptr ? a.weight[slot] : (float)(1.0 / (double)*a.n_scored);
-}
-// Ids that name no token though they are not negative.
-__device__ inline double too_large(const DistillArgs& a, int64_t slot) {
-  int n = 0;
-  for (int j = threadIdx.x & 63; j < a.k; j += 64) n += a.ids[slot * a.k + j] >= a.V;
-  return wave_sum((double)n);
 }
 
 // A wave per slot: the id of its best alternative, or -1.
@@ -180,7 +176,7 @@ __global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
 }
 
 // Behind the forward launch: a workgroup adds the partial sums of 16 rows, then a wave takes each.  (Blocks of 64 rows, four to a wave, left most of the chip idle:
-// V = 151936, 200 rows, k = 32 50 us, now 14; 8192 rows, k = 64 77, now 34, 39 MB of partial sums and the alternatives' logits.)
+// V = 151936, 200 rows, k = 32 50 us, now 14; 8192 rows, k = 64 77, now 33, 39 MB of partial sums and the alternatives' logits.)
 constexpr int kRows = 16, kRowThreads = 64 * kRows, kLanes = kRowThreads / (kRows / 4);
 template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_rows(DistillArgs a) {
   __shared__ float sh[kLanes * (kRows + 1)];
@@ -189,6 +185,17 @@ template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_ro
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double q[kDistillSums] = {};
   if (r0 < nvalid) {
+    // what the wave's row needs is under way before the partial sums are
+    const int64_t r = r0 + wave, ci = a.chunk_start + (r < nvalid ? r : nvalid - 1), slot = a.row_index[ci];
+    const float zt = a.zt[ci], w = weight_of(a, slot);
+    Alternatives<kEach> alt;
+    alt.load(a, slot);
+    float z[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int j = 64 * e + lane;
+      z[e] = a.zk[(ci - a.chunk_start) * a.k + (j < a.k ? j : 0)];
+    }
     // a thread adds every kLanes-th partial of four rows; the rows behind the valid ones hold whatever the buffer held
     const int quad = threadIdx.x & 3, part = threadIdx.x >> 2;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -200,34 +207,27 @@ template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_ro
     float* const cell = sh + part * (kRows + 1) + quad * 4;
     cell[0] = s.x; cell[1] = s.y; cell[2] = s.z; cell[3] = s.w;
     __syncthreads();
-    const int64_t r = r0 + wave;
     if (r < nvalid) {
       float S = 0.f;
 #pragma unroll
       for (int i = 0; i < kLanes / 64; ++i) S += sh[(64 * i + lane) * (kRows + 1) + wave];
       S = lanes_sum<64>(S);
-      const int64_t ci = a.chunk_start + r, slot = a.row_index[ci];
-      const float c2 = fmaf(a.zt[ci], a.scale2, kStashMargin2), w = weight_of(a, slot);
-      Alternatives<kEach> alt;
-      alt.load(a, slot);
+      const float c2 = fmaf(zt, a.scale2, kStashMargin2);
       alt.weigh(a, alt.best_t());
       const double log2_sum = (double)c2 + log2((double)S);        // of exponentials in the log2 domain, with the very c2 that the launch took
       double kl = 0.0;
-      float z[kEach];
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        const int j = 64 * e + lane;
-        z[e] = j < a.k ? a.zk[r * a.k + j] : 0.f;
         if (alt.q[e] != 0.0) kl += alt.q[e] * (alt.log_q[e] - ((double)z[e] * (double)a.scale2 - log2_sum) * LN2);
       }
       kl = wave_sum(kl);
       // the alternative that the student thinks most of is beyond the operands' range: not in the loss, as an empty row
       // (NaN is not: the launches' clamps go past it, so it enters the gradients with the row's scale)
       const bool number = fabs(kl) < (double)INFINITY;
-      const bool saturated = number && ((double)a.zt[ci] * (double)a.scale2 - log2_sum) * LN2 < (double)kSaturatedLogp;
+      const bool saturated = number && ((double)zt * (double)a.scale2 - log2_sum) * LN2 < (double)kSaturatedLogp;
       if (lane == 0) a.out_kl[slot] = (float)kl;
       if (saturated) q[1] += 1.0; else q[0] += (double)w * kl;
-      q[2] += too_large(a, slot);
+      q[2] += alt.too_large;
       if (a.row_scale != nullptr && lane == 0) a.row_scale[ci] = saturated ? 0.f : !number ? __builtin_nanf("") : (float)((double)w * (double)a.temperature * alt.m / (double)S);
       if (a.row_scale != nullptr && !saturated) {
         float total[kEach];
@@ -298,7 +298,7 @@ template <int kEach, int kHeld> __global__ __launch_bounds__(256) void k_distill
     kl = wave_sum(kl);
     if (lane == 0) a.out_kl[slot] = (float)kl;
     q[0] = (double)w * kl;
-    q[2] = too_large(a, slot);
+    q[2] = alt.too_large;
     if (a.write_dz) {
       const float g = (float)((double)w * (double)a.temperature), scale = (float)((double)w * (double)a.temperature * alt.m / (double)S);
       float total[kEach];
