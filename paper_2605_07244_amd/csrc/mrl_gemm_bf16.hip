@@ -1679,12 +1679,16 @@ template <bool BF16_OUT, int NK> __device__ __forceinline__ void dw_resident_ran
   const int kr = 8 * fq + (frow >> 2);
   const uint32_t a_base = kr * (GM * 2) + ((frow & 3) << 3);
   const bool live = nw < p.d;                          // the wave has columns to store
+  // ... and in every store (of floats, half of them are of its second 32 columns)
+  const bool all_stores = live && (BF16_OUT || p.d - nw > 32);
+  constexpr int kLoadsBehind = (G_STAGES - 2) * NL;
   int slot = 0, load_slot = G_STAGES - 1;
   for (int t = first; t < last; ++t) {
-    // This stage has landed when what was issued behind its loads is all that is outstanding: the next two stages' loads, and the last three
-    // stages' stores (every one of which is issued: only a range's last stage has rows behind V).
-    if (live && t - first >= G_STAGES - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((G_STAGES - 2) * NL + (G_STAGES - 1) * G_STORES));
-    else __builtin_amdgcn_s_waitcnt(waitcnt_vm((G_STAGES - 2) * NL));
+    // This stage has landed when what was issued behind its loads is all that is outstanding: the loads of the next stages but one, and the stores of all of them.
+    // None of these may be counted that a wave without a lane for it skips; all rows are there but in a range's last stage, behind which nothing is waited for.
+    if (t - first < G_STAGES - 1 || !live) __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoadsBehind));
+    else if (all_stores) __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoadsBehind + (G_STAGES - 1) * G_STORES));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(kLoadsBehind + (G_STAGES - 1) * G_STORES / 2));
     __syncthreads();
     load(t + G_STAGES - 1, load_slot);
 #pragma unroll

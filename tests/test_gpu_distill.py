@@ -209,6 +209,7 @@ def test_bf16_gradient_of_a_large_head_and_few_rows(mrl, N, d, V):
     (1, 1, 8, 1), (32, 32, 264, 63), (33, 33, 712, 64), (70, 64, 1536, 1000), (100, 100, 256, 20011), (130, 128, 136, 70001), (140, 129, 1032, 4097),
     (192, 161, 4096, 3001), (200, 200, 1536, 9999), (225, 225, 2056, 5003), (256, 256, 3080, 12345), (256, 0, 520, 777), (200, 0, 2048, 30000),
     (256, 250, 16384, 500), (256, 250, 16392, 300), (20, 20, 64, 151936),
+    (60, 50, 72, 400003), (256, 240, 328, 151936), (30, 30, 712, 60000),   # widths whose last wave has half its columns, and skips half the stores of floats
     (200, 190, 8, 3000001)])                            # (blocks that read the stash take several pieces of a row)
 def test_gradient_of_the_head_of_up_to_256_rows(mrl, N, scored, d, V):
     """Hidden rows in registers: every number of steps, one stage and many of them, ranges of the vocabulary that end beside it, widths beside the waves'."""
