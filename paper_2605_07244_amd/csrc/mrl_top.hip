@@ -391,7 +391,8 @@ template <bool kBf16, int T> __global__ __launch_bounds__(T, kWavesAtOnce) void 
     return;
   }
   if (threadIdx.x == 0) a.parts[item] = p;
-  for (int i = threadIdx.x; i < a.k; i += T) a.keys[item * a.k + i] = sh.best[i];
+  // (a last slice may be shorter than the list: zeros, which stand for none, where it has no logits)
+  for (int i = threadIdx.x; i < a.k; i += T) a.keys[item * a.k + i] = i < k ? sh.best[i] : 0;
 }
 
 template <bool kBf16> __global__ __launch_bounds__(kMostThreads) void k_top_join(TopArgs a) {

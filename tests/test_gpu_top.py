@@ -187,6 +187,17 @@ def test_long_rows(mrl, N, V, k, dtype):
         assert abs(float(r["entropy"][n]) - H) <= (2 + H) * A + U * 200 ** 2 / 4
 
 
+@pytest.mark.parametrize("N,V,k", [(1, 65537, 8), (31, 65537, 20), (1, 151553, 13), (1, 63489, 2), (1, 151557, 13)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_last_slice_shorter_than_the_list(mrl, N, V, k, dtype):
+    """Rows in slices of which the last has one logit, or five: what calls with larger logits left in the chip's memory is none of theirs."""
+    mrl.top_logprobs(rand((2048, 70001), dtype, 1, 3.0) + 5000.0, 256)      # (a workgroup a row: their lists)
+    z = rand((N, V), dtype, N + V + k, 3.0)
+    _check(mrl, z, k, T=0.7)
+    z[:, V - 1] = 50.0                                  # and the last logit counts
+    _check(mrl, z, k)
+
+
 @pytest.mark.parametrize("N", [3, 1100])
 def test_one_thread_holds_the_largest(mrl, N):
     """All alternatives among the logits that one thread of the workgroup looks at; and more equal logits than the list holds."""
