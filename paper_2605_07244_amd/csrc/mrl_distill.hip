@@ -111,10 +111,10 @@ template <int kEach> __global__ __launch_bounds__(256) void k_distill_targets(Di
     alt.load(a, n);
     const float best = alt.best_t();
     alt.weigh(a, best);
-    // the lowest lane that has it (of NaN alone: any alternative)
+    // the lowest lane that has it (of NaN alone, where the largest is NaN if every lane holds one and else -infinity: any alternative)
 #pragma unroll
     for (int i = kEach - 1; i >= 0; --i) {
-      const unsigned long long has = __ballot(alt.id[i] >= 0 && (alt.t[i] == best || best == -INFINITY));
+      const unsigned long long has = __ballot(alt.id[i] >= 0 && (alt.t[i] == best || !(best > -INFINITY)));
       if (has != 0) target = __builtin_amdgcn_readlane(alt.id[i], __builtin_ctzll(has));
     }
     if (!alt.any) target = -1;

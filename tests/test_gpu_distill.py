@@ -312,6 +312,22 @@ def test_nan_stays_in_its_row_of_dH(mrl, dtype):
     assert torch.isnan(r["dW"]).any() and np.isnan(mrl.read_distill_stats(r["stats"])["loss_total"])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("k", [1, 63, 64, 128, 256])
+@pytest.mark.parametrize("renormalize", [0, 1])
+def test_log_probs_that_are_all_nan_count(mrl, dtype, k, renormalize):
+    """Every lane of the wave that looks at them holds NaN, at 64 alternatives and multiples; a NaN is no empty row."""
+    N, d, V = 12, 64, 300
+    h, w, ids, logp = _case(N, d, V, k, dtype, 8)
+    ids.clamp_(min=0)
+    logp[5] = float("nan")
+    r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(renormalize=renormalize, dh_dtype=mrl.F32))
+    st = mrl.read_distill_stats(r["stats"])
+    bad = torch.arange(N, device="cuda") == 5
+    assert torch.equal(torch.isnan(r["kl"]), bad) and torch.equal(torch.isnan(r["dH"]).any(1), bad)
+    assert torch.isnan(r["dW"]).any() and np.isnan(st["loss_total"]) and st["n_scored_rows"] == N and st["n_empty_rows"] == 0
+
+
 def test_saturated_rows_are_counted_and_left_out(mrl):
     N, d, V = 20, 64, 200
     h = torch.zeros(N, d, device="cuda", dtype=BF16)
