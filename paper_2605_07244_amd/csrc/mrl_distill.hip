@@ -62,7 +62,16 @@ template <int kEach> struct Alternatives {
     }
     m = wave_sum(sum);
     any = m != m || m >= kLeastMass;
-    if (!a.renormalize) return;
+    if (!a.renormalize) {
+      // an infinite mass is no distribution's: NaN, as the quotients of infinities below
+      const double nan = __builtin_nan("");
+      if (m == (double)INFINITY) {
+        m = nan;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) q[i] = id[i] >= 0 ? nan : 0.0;
+      }
+      return;
+    }
     const double log_m = log(m), inv = 1.0 / m;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) { q[i] *= inv; log_q[i] -= log_m; }

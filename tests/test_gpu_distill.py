@@ -328,6 +328,19 @@ def test_log_probs_that_are_all_nan_count(mrl, dtype, k, renormalize):
     assert torch.isnan(r["dW"]).any() and np.isnan(st["loss_total"]) and st["n_scored_rows"] == N and st["n_empty_rows"] == 0
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("renormalize", [0, 1])
+def test_infinite_log_probs_are_nan(mrl, dtype, renormalize):
+    N, d, V, k = 12, 64, 300, 6
+    h, w, ids, logp = _case(N, d, V, k, dtype, 8)
+    logp[5, 0] = float("inf")
+    ids[6], logp[6] = 7, float("inf")
+    r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(renormalize=renormalize, dh_dtype=mrl.F32))
+    bad = (torch.arange(N, device="cuda") - 5).div(2, rounding_mode="floor") == 0
+    assert torch.equal(torch.isnan(r["kl"]), bad) and torch.equal(torch.isnan(r["dH"]).any(1), bad) and torch.all(torch.isfinite(r["kl"][~bad]))
+    assert torch.isnan(r["dW"]).any() and np.isnan(mrl.read_distill_stats(r["stats"])["loss_total"])
+
+
 def test_saturated_rows_are_counted_and_left_out(mrl):
     N, d, V = 20, 64, 200
     h = torch.zeros(N, d, device="cuda", dtype=BF16)
