@@ -2,10 +2,10 @@
 // q_j = exp t_j (renormalised: over their sum), m = sum q_j, p = softmax(z / T):
 //   kl = sum_j q_j (log q_j - log p[v_j])          L = T^2 sum_n w_n kl_n          dz = w T (m p - q)
 // With the forward launch's stash e = 2^(z log2(e) / T - c) and its sum S, p = e / S and
-//   dz = (w T m / S) (e - (S / m) q):  the stored row, changed at k places, times a scalar per row.
+//   dz = (w T m / S) (e - S (q / m)):  the stored row, changed at k places, times a scalar per row.
 // The offset c comes from the largest of the row's k logits, which are products of the row with k rows of the head, taken
 // before the forward launch in fp32: the divergence needs them to more bits than the stash has.  The weights and divergences of a row are taken in
-// 64 bits: a few dozen operations beside 6 d V.  What is rounded to 16 bits, and how far that takes the gradients: e (or e - (S / m) q) in the stash and the row of
+// 64 bits: a few dozen operations beside 6 d V.  What is rounded to 16 bits, and how far that takes the gradients: e (or e - S (q / m)) in the stash and the row of
 // hidden states times its scale, half a step of 2^-9 each on average a third of it; dH 1.7e-3 of its norm and dW 2.4e-3, with the rounding of a bf16 output 2.4e-3 and 2.9e-3.
 #include "mrl_internal.h"
 #include "mrl_vec.h"
@@ -14,7 +14,8 @@ namespace mrl {
 namespace {
 
 constexpr double LN2 = 0.6931471805599453;
-constexpr double kLeastMass = 1e-30;                   // of a row that counts: S / m stays a number
+constexpr double kLeastMass = 1e-30;                   // of a row that counts: w T m stays a normal float for weights down to 1e-8
+constexpr double kLeastScale = 0x1p-100;               // of a row: its products with ordinary hidden states stay normal floats and bf16
 
 __device__ inline double wave_sum(double x) {
 #pragma unroll
@@ -83,22 +84,22 @@ template <int kEach> struct Alternatives {
     for (int i = 1; i < kEach; ++i) b = fmaxf(b, t[i]);
     return wave_max(b);
   }
-  // Per alternative the probability of its id, however often that is listed, and whether this is the id's first place.
-  __device__ void by_id(int k, float (&total)[kEach], bool (&first)[kEach]) const {
+  // Per alternative its id's share of the mass, however often that is listed, and whether this is the id's first place.
+  __device__ void by_id(int k, float (&share)[kEach], bool (&first)[kEach]) const {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) { total[i] = 0.f; first[i] = id[i] >= 0; }
+    for (int i = 0; i < kEach; ++i) { share[i] = 0.f; first[i] = id[i] >= 0; }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int n = k - 64 * e < 64 ? k - 64 * e : 64;
-      const float mine = (float)q[e];
+      const float mine = (float)(q[e] / m);
       for (int l = 0; l < n; ++l) {
         const int other = __builtin_amdgcn_readlane(id[e], l);
         const float p = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), l));
 #pragma unroll
         for (int i = 0; i < kEach; ++i)
           if (id[i] == other && 64 * i < k) {
-            total[i] += p;
+            share[i] += p;
             if (64 * e + l < 64 * i + lane) first[i] = false;
           }
       }
@@ -237,17 +238,33 @@ template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_ro
       if (lane == 0) a.out_kl[slot] = (float)kl;
       if (saturated) q[1] += 1.0; else q[0] += (double)w * kl;
       q[2] += alt.too_large;
-      if (a.row_scale != nullptr && lane == 0) a.row_scale[ci] = saturated ? 0.f : !number ? __builtin_nanf("") : (float)((double)w * (double)a.temperature * alt.m / (double)S);
+      if (a.row_scale != nullptr && saturated && lane == 0) a.row_scale[ci] = 0.f;
       if (a.row_scale != nullptr && !saturated) {
-        float total[kEach];
-        bool first[kEach];
-        alt.by_id(a.k, total, first);
-        const float per = (float)((double)S / alt.m);
         uint16_t* const row = a.estash + r * a.lde;
+        // The row's scale.  Of a small mass beside a large sum (S is 2^-60 over the probability of the student's likeliest alternative, 2^80 at most) it is less than floats
+        // hold, though the gradient is not: the stored row is brought to a sum from 1 to 2 then, by a power of two.  (Alternatives that both hold for impossible: rare.)
+        float down = 1.f;
+        double scale = (double)w * (double)a.temperature * alt.m / (double)S;
+        if (__builtin_expect(fabs(scale) < kLeastScale && scale != 0.0 && S > 1.f, 0)) {
+          down = ldexpf(1.f, -ilogbf(S));
+          scale /= (double)down;
+#pragma unroll 1
+          for (int v = lane * 8; v < a.V; v += 512) {  // (rows are padded to whole vectors)
+            u32x4 x = *reinterpret_cast<const u32x4*>(row + v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = pack_bf16(bf16_low(x[i]) * down, bf16_high(x[i]) * down);
+            *reinterpret_cast<u32x4*>(row + v) = x;
+          }
+          __threadfence_block();                       // (the places below are other lanes' here)
+        }
+        if (lane == 0) a.row_scale[ci] = number ? (float)scale : __builtin_nanf("");
+        float share[kEach];
+        bool first[kEach];
+        alt.by_id(a.k, share, first);
 #pragma unroll
         for (int e = 0; e < kEach; ++e)
           if (first[e]) {
-            const float x = __builtin_amdgcn_exp2f(fminf(fmaf(z[e], a.scale2, -c2), kStashClamp2)) - per * total[e];
+            const float x = down * __builtin_amdgcn_exp2f(fminf(fmaf(z[e], a.scale2, -c2), kStashClamp2)) - down * S * share[e];
             row[alt.id[e]] = (uint16_t)pack_bf16(x, 0.f);
           }
       }
@@ -309,15 +326,16 @@ template <int kEach, int kHeld> __global__ __launch_bounds__(256) void k_distill
     q[0] = (double)w * kl;
     q[2] = alt.too_large;
     if (a.write_dz) {
-      const float g = (float)((double)w * (double)a.temperature), scale = (float)((double)w * (double)a.temperature * alt.m / (double)S);
-      float total[kEach];
+      const double g = (double)w * (double)a.temperature * alt.m;
+      const float scale = (float)(g / (double)S);
+      float share[kEach];
       bool first[kEach];
-      alt.by_id(a.k, total, first);
+      alt.by_id(a.k, share, first);
       each([&](float& x, int v) { row[v] = scale * (kHeld > 0 ? x : expf((x - mx) * inv_T)); });
       __threadfence_block();                           // (the places below are other lanes' above)
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
-        if (first[e]) row[alt.id[e]] = scale * expf((z[e] - mx) * inv_T) - g * total[e];
+        if (first[e]) row[alt.id[e]] = scale * expf((z[e] - mx) * inv_T) - (float)g * share[e];
     }
   }
   if (lane == 0) {

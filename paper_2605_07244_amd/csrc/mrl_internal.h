@@ -266,7 +266,7 @@ constexpr int kDistillSums = 3;                      // weighted loss, saturated
 void launch_distill_targets(const DistillArgs& a, hipStream_t stream);
 // bf16 path, before a pass's forward launch: the alternatives' logits zk, and zt.
 void launch_distill_logits(const DistillArgs& a, hipStream_t stream);
-// bf16 path, behind it: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S q / m.
+// bf16 path, behind it: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S (q / m).
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream);
 int distill_row_blocks(int chunk_rows);
 // fp32 path: divergence, and dz in the place of the pass's logits.

@@ -341,6 +341,48 @@ def test_infinite_log_probs_are_nan(mrl, dtype, renormalize):
     assert torch.isnan(r["dW"]).any() and np.isnan(mrl.read_distill_stats(r["stats"])["loss_total"])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("given", [-20.0, -45.0, -65.0])
+@pytest.mark.parametrize("seen", [60.0, 75.0, 95.0])
+def test_small_masses_of_ids_that_the_student_rules_out(mrl, dtype, given, seen):
+    """Masses down to e^-65 beside sums of exponentials e^seen times the id's own: their quotient and the row's scale are beyond fp32, the gradient is not."""
+    N, d, V = 20, 64, 300
+    h, w = rand((N, d), dtype, 1, 0.3), rand((V, d), dtype, 2, 0.1)
+    h[:, 0], w[:, 0] = seen, 0.0
+    w[5, 0] = 1.0                                       # the student's token, with a logit of `seen` more than the others
+    ids = torch.full((N, 1), 9, device="cuda", dtype=torch.int32)
+    logp = torch.full((N, 1), given, device="cuda")
+    for dh in (mrl.F32, mrl.BF16) if dtype == BF16 else (mrl.F32,):
+        r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(renormalize=0, dh_dtype=dh))
+        kl, loss, dH, dW = to.distill(f64(h), f64(w), ids.cpu().numpy(), f64(logp), renormalize=False)
+        # a log-prob is off by twice what a logit is, d roundings at the sum of its products' magnitudes, and by the exponents' and sums' roundings
+        A = (np.abs(f64(h)) @ np.abs(f64(w)).T).max()
+        off = 2 * d * U * A + (4 * A + 120 + V / 128 + 150) * U
+        assert np.all(np.abs(f64(r["kl"]) - kl) <= np.exp(given) * off + 2 * U * np.abs(kl))
+        st = mrl.read_distill_stats(r["stats"])
+        assert st["n_saturated_rows"] == 0 and st["n_scored_rows"] == N and abs(st["loss_total"] - loss) <= np.exp(given) * off + 2 * U * abs(loss)
+        tol = util.F32_REL_TOL if dtype == F32 else util.REL_TOL
+        for name, got, want in (("dH", r["dH"], dH), ("dW", r["dW"], dW)):
+            util.check_gradient(name, f64(got), want, tol)
+
+
+@pytest.mark.parametrize("N", [40, 300])
+def test_a_row_of_small_mass_among_others(mrl, N):
+    d, V, k = 64, 300, 7
+    h, w, ids, logp = _case(N, d, V, k, BF16, 4, scale=1.0)
+    h[7] = (70.0 * w[5].float() / w[5].float().square().sum()).bfloat16()      # the student's token is 5, by 70 more than what it sees none of
+    z = (h[7].float() @ w.float().t()).cpu()
+    ids[7] = -1
+    ids[7, 0] = int(z.abs().argmin())
+    logp[7, 0] = -65.0
+    r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, mrl.DistillConfig(renormalize=0, dh_dtype=mrl.F32))
+    _, _, dH, dW = to.distill(f64(h), f64(w), ids.cpu().numpy(), f64(logp), renormalize=False)
+    assert mrl.read_distill_stats(r["stats"])["n_saturated_rows"] == 0
+    util.check_gradient("dW", f64(r["dW"]), dW)
+    util.check_gradient("dH", f64(r["dH"]), dH)
+    util.check_gradient("dH of the row", f64(r["dH"])[7:8], dH[7:8])
+
+
 def test_saturated_rows_are_counted_and_left_out(mrl):
     N, d, V = 20, 64, 200
     h = torch.zeros(N, d, device="cuda", dtype=BF16)
