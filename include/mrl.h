@@ -490,6 +490,8 @@ int mrl_top_logprobs(const void* logits /*[N, row_stride] dev*/, int64_t row_str
  * has the sum of its probabilities, the divergence a term for each.  A log-prob of -infinity is a probability of 0.
  * A row counts where its mask is not 0 (token_mask NULL: every row) and its alternatives' mass is above 0 (renormalize = 0: at least 1e-30); the others have
  * out_kl and out_dH of zero and add nothing; those with mask 0 are not read.  NaN, or an infinite hidden state or log-prob, in a row that counts makes its outputs NaN, and out_dW.
+ * So does an entry of the head that is not finite, in every row where it makes a logit NaN or +infinite; a logit of -infinity is a probability of 0 (in a
+ * saturated row, see below, it may be NaN as well).
  * Numerical range (bf16 path): a row whose most likely alternative has a log-prob below about -97 with the student reports a divergence that may be too small, is left
  * out of the loss and the gradients and counted in n_saturated_rows.
  * dtype, d and V as in call (3).  dh_dtype, dw_dtype: types of the gradients; MRL_BF16 with bf16 inputs only, dw_dtype MRL_BF16 only

@@ -775,7 +775,7 @@ int mrl_distill_loss_fwd_bwd(const void* hidden, const void* lm_head_w, const in
     forward_chunk(hidden, lm_head_w, d, V, bf16, L, ws, c0, bwd, s, false, false, a.scale2);
     {
       Scope sc(MRL_PROF_ROW_EPI, s);
-      if (bf16) launch_distill_rows(a, s); else launch_distill_f32(a, rows, s);
+      if (bf16) { launch_distill_hidden_nan(a, s); launch_distill_rows(a, s); } else launch_distill_f32(a, rows, s);
       a.partial_block_offset += bf16 ? distill_row_blocks(L.chunk_rows) : distill_f32_blocks(rows);
     }
     if (!bwd) continue;

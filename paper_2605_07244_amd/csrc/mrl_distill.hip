@@ -185,7 +185,34 @@ __global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
   if (threadIdx.x == 0) a.zt[a.chunk_start + r] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
 }
 
-// Behind the forward launch: a workgroup adds the partial sums of 16 rows, then a wave takes each.  (Blocks of 64 rows, four to a wave, left most of the chip idle:
+// Behind the forward launch: what its clamp hides.  Exponentials are clamped at 2^kStashClamp2, and so are those of NaN and +infinity, which would pass for logits far
+// above the alternatives'.  A workgroup per partial sum, those of kPartialRows rows of the head: where a token's reaches the clamp and the rows hold anything that is not finite, that
+// token's sum is NaN.  The head is read at clamped sums only, once at most.  (Finite logits that reach the clamp beside such an entry: their row is saturated, and NaN with it.)
+// (A call of 200 rows, V = 151936, d = 1536 425 us without it and 429 with; of 900, V = 50257 325 and 330; of 8192, d = 4096 21150 and 21170.)
+constexpr int kPartialRows = 128;
+__global__ __launch_bounds__(256) void k_distill_hidden_nan(DistillArgs a) {
+  const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows);
+  const int64_t v0 = (int64_t)blockIdx.x * kPartialRows;
+  const int rows = a.V - v0 < kPartialRows ? (int)(a.V - v0) : kPartialRows;
+  float* const sums = a.part_sum + (int64_t)blockIdx.x * a.chunk_rows;
+  constexpr float clamped = 0x1p99f;                   // (half of it, however it is rounded)
+  static_assert(kStashClamp2 == 100.f, "the clamp");
+  bool any = false;
+  for (int n = threadIdx.x; n < nvalid; n += 256) any |= sums[n] >= clamped;
+  if (!__syncthreads_or(any)) return;
+  const uint16_t* const w = static_cast<const uint16_t*>(a.W) + v0 * a.d;
+  bool bad = false;
+  for (int64_t i = threadIdx.x * 8; i < (int64_t)rows * a.d; i += 256 * 8) {
+    const u32x4 x = load_any<2, u32x4>(w + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bad |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+  }
+  if (!__syncthreads_or(bad)) return;
+  for (int n = threadIdx.x; n < nvalid; n += 256)
+    if (sums[n] >= clamped) sums[n] = __builtin_nanf("");
+}
+
+// Behind that: a workgroup adds the partial sums of 16 rows, then a wave takes each.  (Blocks of 64 rows, four to a wave, left most of the chip idle:
 // V = 151936, 200 rows, k = 32 50 us, now 14; 8192 rows, k = 64 77, now 33, 39 MB of partial sums and the alternatives' logits.)
 constexpr int kRows = 16, kRowThreads = 64 * kRows, kLanes = kRowThreads / (kRows / 4);
 template <int kEach> __global__ __launch_bounds__(kRowThreads) void k_distill_rows(DistillArgs a) {
@@ -398,6 +425,9 @@ void launch_distill_targets(const DistillArgs& a, hipStream_t stream) {
 }
 void launch_distill_logits(const DistillArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(k_distill_logits, dim3(a.chunk_rows), dim3(256), 0, stream, a);
+}
+void launch_distill_hidden_nan(const DistillArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(k_distill_hidden_nan, dim3((a.V + kPartialRows - 1) / kPartialRows), dim3(256), 0, stream, a);
 }
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
   hipLaunchKernelGGL(by_count(a.k, k_distill_rows<1>, k_distill_rows<2>, k_distill_rows<4>), dim3(a.chunk_rows / kRows), dim3(kRowThreads), 0, stream, a);

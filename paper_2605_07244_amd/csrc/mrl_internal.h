@@ -255,7 +255,7 @@ struct DistillArgs {
   int32_t* targets;                                  // [N]: the best alternative's id, or -1 for a slot that does not count
   const int32_t* row_index; const int64_t* n_scored; int64_t chunk_start; int chunk_rows;
   float* zt; float* zk;                              // [N] compacted: the largest of the row's logits zk [chunk_rows, k]
-  const float* part_sum; int n_partials;             // bf16 path
+  float* part_sum; int n_partials;                   // bf16 path
   uint16_t* estash; int64_t lde; float* row_scale;   // (nullptr: no backward pass)
   float* Z; int64_t ldz; int write_dz;               // fp32 path
   float* out_kl;                                     // [N] per slot
@@ -266,7 +266,9 @@ constexpr int kDistillSums = 3;                      // weighted loss, saturated
 void launch_distill_targets(const DistillArgs& a, hipStream_t stream);
 // bf16 path, before a pass's forward launch: the alternatives' logits zk, and zt.
 void launch_distill_logits(const DistillArgs& a, hipStream_t stream);
-// bf16 path, behind it: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S (q / m).
+// bf16 path, behind it: partial sums are NaN where a logit is NaN or +infinite, which the launch's clamp hides.
+void launch_distill_hidden_nan(const DistillArgs& a, hipStream_t stream);
+// ... then: divergence, row scale m w T / S, and the stash's columns of alternatives: e - S (q / m).
 void launch_distill_rows(const DistillArgs& a, hipStream_t stream);
 int distill_row_blocks(int chunk_rows);
 // fp32 path: divergence, and dz in the place of the pass's logits.

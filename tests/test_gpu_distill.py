@@ -383,6 +383,35 @@ def test_a_row_of_small_mass_among_others(mrl, N):
     util.check_gradient("dH of the row", f64(r["dH"])[7:8], dH[7:8])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V", [(40, 300), (300, 700), (600, 5003)])
+@pytest.mark.parametrize("grads", [True, False])
+def test_nan_and_infinities_in_the_head(mrl, dtype, N, V, grads):
+    """... in a row that no alternative names: the softmax of every row that it makes NaN or +infinite is NaN, and of no other."""
+    d, k, v = 64, 6, V - 7
+    h, w, ids, logp = _case(N, d, V, k, dtype, 8)
+    ids[ids == v] = -1
+    ids[:, 0] = torch.where(ids[:, 0] < 0, 3, ids[:, 0])
+    h[:, 3] = torch.where(torch.arange(N, device="cuda") % 3 == 0, 1.0, -0.5)
+    cfg = mrl.DistillConfig(dh_dtype=mrl.F32)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        w[v, 3] = value
+        r = mrl.distill_loss_fwd_bwd(h, w, ids, logp, cfg, want_dH=grads, want_dW=grads)
+        st = mrl.read_distill_stats(r["stats"])
+        bad = torch.isnan(h[:, 3] * value) | (h[:, 3] * value > 0)
+        assert torch.equal(torch.isnan(r["kl"]), bad), value
+        assert np.isnan(st["loss_total"]) and st["n_scored_rows"] == N and st["n_saturated_rows"] == 0
+        # the others: the token's probability is 0
+        rest = torch.cat([w[:v], w[v + 1:]])
+        i = torch.where(ids > v, ids - 1, ids)
+        want, _, _, _ = to.distill(f64(h), f64(rest), i.cpu().numpy(), f64(logp))
+        ok = (~bad).cpu().numpy()
+        bound = _kl_bound(h, rest, 1.0, V, np.ones(N))
+        assert np.all(np.abs(f64(r["kl"]) - want)[ok] <= bound[ok])
+        if grads:
+            assert torch.isnan(r["dW"]).any() and torch.all(torch.isnan(r["dH"][bad]).any(1))
+
+
 def test_saturated_rows_are_counted_and_left_out(mrl):
     N, d, V = 20, 64, 200
     h = torch.zeros(N, d, device="cuda", dtype=BF16)
