@@ -1,6 +1,6 @@
 // Top alternatives of given logits, with the log-probs of given tokens and the entropy.  Row n of [N, V], s2 = log2(e) / T:
 //   u_v = z_v s2 - m s2,  S = sum 2^u,  E = sum 2^u u     (m: the largest logit met; all in the log2 domain)
-//   lse = (m s2 + log2 S) ln 2,  entropy = (log2 S - E / S) ln 2,  log-prob = z / T - lse
+//   lse = (m s2 + log2 S) ln 2,  entropy = (log2 S - E / S) ln 2,  log-prob = (z s2 - m s2 - log2 S) ln 2
 //   alternatives: the k largest by (logit, then the lower id first), exactly those
 // One pass reads the logits once.  A thread notes the largest of every few tiles it has seen.  The k-th largest of the threads' maxima is a lower bound of the
 // k-th largest logit (each maximum is another element); behind the pass, the notes that reach it say where the logits that do can be, and those places, k and a
@@ -32,13 +32,14 @@ constexpr int kIdBits = 24;                            // V <= 2^24
 constexpr uint64_t kIdMask = ((uint64_t)1 << kIdBits) - 1;
 constexpr float kNone = -1e30f;                        // the running maximum of no logits: finite, and so is its product with s2
 constexpr float kLeastU = -200.f;                      // 2^u is 0 there; u itself must not be infinite in the product 2^u u
+constexpr float kLeastSum = 0x1p-100f;                 // of a row: its largest logit is 2^u with u the rounding of m s2, less than -100 only beyond 1e9
 constexpr double LN2 = 0.6931471805599453;
 
 struct Part { float m2, S, E; };
 struct TopArgs {
   const void* z; int64_t ld; const int32_t* targets; const uint8_t* mask;
   int64_t N; int V, k, split, slice;
-  float s2; double inv_T;
+  float s2;
   int32_t* ids; float* top; float* logp; float* lse; float* entropy;
   Part* parts; uint64_t* keys;                         // [N][split], [N][split][k]
 };
@@ -248,7 +249,7 @@ template <int T> __device__ inline Part join_all(Shared<T>& sh, Part p) {
   return join_lanes<8>(w < T / 64 ? Part{sh.wave[w][0], sh.wave[w][1], sh.wave[w][2]} : Part{p.m2, 0.f, 0.f});
 }
 
-// Sums of a row that the pass has none for: its largest logit is NaN, infinite, below kNone, or so large that m s2, or its distance from kNone s2, is not finite
+// Sums of a row that the pass has none for: its largest logit is NaN, infinite, below kNone, or so large that m s2, its distance from kNone s2, or 2 to the power of its rounding is not finite
 // (there E alone may be NaN).  Two passes, the differences to the largest logit first.  S is NaN where there is no distribution.
 template <bool kBf16, int T> __device__ inline void careful_sums(Shared<T>& sh, const TopArgs& a, const void* row, double& offset, float& S, float& E) {
   uint32_t most = 0;
@@ -279,20 +280,23 @@ template <bool kBf16, int T> __device__ inline void put_row(Shared<T>& sh, const
   const void* row = static_cast<const char*>(a.z) + n * a.ld * (kBf16 ? 2 : 4);
   double offset = p.m2;
   float S = p.S, E = p.E;
-  if (!(S > 0.f && S < INFINITY) || E != E) careful_sums<kBf16>(sh, a, row, offset, S, E);
+  if (!(S > kLeastSum && S < INFINITY) || E != E) careful_sums<kBf16>(sh, a, row, offset, S, E);
   if ((int)(threadIdx.x & ~63u) >= (a.k > 1 ? a.k : 1)) return;      // (waves without outputs; no barrier from here on)
-  const double log2_S = log2((double)S), lse = (offset + log2_S) * LN2;
+  const double log2_S = log2((double)S);
+  // As the sums took it: the difference to the offset is exact, so that far from zero (rows masked throughout with the type's lowest value) the log-probs are those of the
+  // logits' differences.  z / T - lse was off by what the scale's rounding makes of z itself.
+  const auto log_prob = [&](float z) { return (float)(((double)z * (double)a.s2 - offset - log2_S) * LN2); };
   for (int i = threadIdx.x; i < a.k; i += T) {
     const uint64_t key = sh.best[i];
     if (a.ids != nullptr) a.ids[n * a.k + i] = id_of(key);
-    if (a.top != nullptr) a.top[n * a.k + i] = (float)((double)logit_of(key) * a.inv_T - lse);
+    if (a.top != nullptr) a.top[n * a.k + i] = log_prob(logit_of(key));
   }
   if (threadIdx.x == 0) {
-    if (a.lse != nullptr) a.lse[n] = (float)lse;
+    if (a.lse != nullptr) a.lse[n] = (float)((offset + log2_S) * LN2);
     if (a.entropy != nullptr) a.entropy[n] = (float)((log2_S - (double)E / (double)S) * LN2);
     if (a.logp != nullptr) {
       const int y = a.targets[n];
-      a.logp[n] = y >= 0 && y < a.V ? (float)((double)logit_at<kBf16>(row, y) * a.inv_T - lse) : 0.f;
+      a.logp[n] = y >= 0 && y < a.V ? log_prob(logit_at<kBf16>(row, y)) : 0.f;
     }
   }
 }
@@ -468,7 +472,7 @@ extern "C" int mrl_top_logprobs(const void* logits, int64_t row_stride, const in
     return MRL_ERR_WORKSPACE;
   const int rc = require_gfx950();
   if (rc != MRL_OK) return rc;
-  TopArgs a = {logits, row_stride, target_ids, token_mask, N, V, k, s.split, s.slice, (float)(1.4426950408889634 / (double)temperature), 1.0 / (double)temperature,
+  TopArgs a = {logits, row_stride, target_ids, token_mask, N, V, k, s.split, s.slice, (float)(1.4426950408889634 / (double)temperature),
                out_ids, out_top_logp, out_logp, out_lse, out_entropy, nullptr, nullptr};
   if (s.split > 1) {
     a.parts = static_cast<Part*>(workspace);

@@ -130,6 +130,42 @@ def test_infinities_nan_and_lowest_values(mrl, V, dtype):
         assert torch.allclose(a["lse"].view(80, 14), b["lse"].expand(80, 14), rtol=1e-6, atol=1e-5, equal_nan=True)
 
 
+@pytest.mark.parametrize("N", [2, 1100])
+@pytest.mark.parametrize("V", [9, 700, 30011])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_log_probs_of_logits_far_from_zero(mrl, N, V, dtype, T):
+    """Rows masked throughout with the type's lowest value, and others whose logits have much in common: log-probs are those of the differences."""
+    low = torch.finfo(dtype).min
+    far = [low, low / 2, -1e30, -1e20, -1e9, 1e5, 1e9, 3e9, 1e15, 1e30, 1e36]
+    z = torch.tensor(far, device="cuda").to(dtype)[:, None].repeat(1, V)
+    z[5:8, 1::3] -= z[5:8, 1::3].abs() * 2.0 ** -7      # (3e9 too: by 2e7)
+    z[0, 4], z[4, 4] = low / 2, 0.0                 # one that is not masked
+    target = torch.tensor([0, 4] * 6, device="cuda", dtype=torch.int32)[:len(far)]
+    x = z.double().cpu().numpy()
+    s = (x - x.max(1, keepdims=True)) / T
+    want = s - np.log(np.exp(s).sum(1, keepdims=True))
+    k = min(V, 7)
+    ids = to.top(x, k)[0]
+    p = np.exp(want)
+    entropy = -(p * np.where(p > 0, want, 0.0)).sum(1)
+    many = z.repeat(-(-N // len(far)), 1)
+    r = mrl.top_logprobs(many, k, target_ids=target.repeat(len(many) // len(far)), temperature=T)
+    # The exponents' residue where the largest logit is taken to is 128 at most (beyond that the row is summed anew), rounded to U of itself; the scale is rounded by U, which
+    # moves differences; sums as above; then the results' rounding.
+    A = (V / 512 + 16 + 40) * U + 4 * U * 128
+    for n in range(0, len(many), len(far)):
+        rows = slice(n, n + len(far))
+        assert np.array_equal(r["ids"][rows].cpu().numpy(), ids)
+        for name, got, exact in (("top", r["top_logp"], np.take_along_axis(want, ids, 1)), ("logp", r["logp"], want[np.arange(len(far)), target.cpu().numpy()])):
+            with np.errstate(over="ignore"):
+                exact = exact.astype(np.float32).astype(np.float64)      # (the lowest value over 0.7 is no float)
+            _near(name, got[rows], exact, A + 4 * U * np.abs(np.where(np.isfinite(exact), exact, 0.0)))
+        _near("entropy", r["entropy"][rows], entropy, (2 + entropy) * A + 4 * U * 200)
+        if n == 0 and V == 9:
+            assert abs(float(r["top_logp"][2, 0]) + np.log(9.0)) <= A + U * 3
+
+
 @pytest.mark.parametrize("V", [9, 700, 30011])
 @pytest.mark.parametrize("N", [2, 1100])
 def test_logits_that_fill_the_range(mrl, N, V):
