@@ -117,6 +117,14 @@ def test_options(mrl, T, renormalize, dh, dw):
     _check(mrl, h, w, ids, logp, mrl.DistillConfig(temperature=T, renormalize=renormalize, dh_dtype=dh, dw_dtype=dw), grads=False)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,scale", [(0.01, 0.02), (0.1, 0.2), (100.0, 100.0), (100.0, 2.0)])
+@pytest.mark.parametrize("renormalize", [0, 1])
+def test_temperatures_at_the_ends_of_the_range(mrl, dtype, T, scale, renormalize):
+    h, w, ids, logp = _case(300, 136, 900, 12, dtype, 5, T, scale)
+    _check(mrl, h, w, ids, logp, mrl.DistillConfig(temperature=T, renormalize=renormalize, dh_dtype=mrl.F32))
+
+
 @pytest.mark.parametrize("N,d,V,k", [(1, 1, 1, 1), (5, 3, 7, 3), (64, 64, 512, 16), (300, 50, 2100, 100), (4100, 8, 33, 5), (9, 100, 5000, 256)])
 @pytest.mark.parametrize("T,renormalize", [(1.0, 1), (3.0, 0)])
 def test_fp32(mrl, N, d, V, k, T, renormalize):
