@@ -464,6 +464,7 @@ int mrl_adamw_check(const mrl_param_tensor* tensors /*host*/, int32_t count, int
  *   outside [0, V).  token_mask [N] or NULL: rows with mask 0 are not read; their ids are -1, the other outputs 0.
  *   -infinity is a logit like others (probability 0).  A row that holds NaN or +infinity, or nothing above -infinity, has no
  *   distribution: its lse, log-probs and entropy are NaN; its ids are in order all the same, NaN before everything, zeros of either sign alike.
+ *   A row that a mask left at the type's lowest value throughout is a uniform one (log-probs are taken from differences, not from lse).
  *   The sums have a fixed order: bit-reproducible.  temperature from 1e-4 to 1e4.  N = 0 is a no-op.
  *   The workspace is needed where few rows are split over several workgroups each; a query of 256 means that none is.
  * ---------------------------------------------------------------------- */
@@ -491,9 +492,9 @@ int mrl_top_logprobs(const void* logits /*[N, row_stride] dev*/, int64_t row_str
  * A row counts where its mask is not 0 (token_mask NULL: every row) and its alternatives' mass is above 0 (renormalize = 0: at least 1e-30); the others have
  * out_kl and out_dH of zero and add nothing; those with mask 0 are not read.  NaN, or an infinite hidden state or log-prob, in a row that counts makes its outputs NaN, and out_dW.
  * So does an entry of the head that is not finite, in every row where it makes a logit NaN or +infinite; a logit of -infinity is a probability of 0 (in a
- * saturated row, see below, it may be NaN as well).
+ * saturated row, see below, it may be NaN as well, and out_dH = dz W is NaN beside an infinite entry all the same).
  * Numerical range (bf16 path): a row whose most likely alternative has a log-prob below about -97 with the student reports a divergence that may be too small, is left
- * out of the loss and the gradients and counted in n_saturated_rows.
+ * out of the loss and the gradients and counted in n_saturated_rows.  Row weights up to 1e18.
  * dtype, d and V as in call (3).  dh_dtype, dw_dtype: types of the gradients; MRL_BF16 with bf16 inputs only, dw_dtype MRL_BF16 only
  * without accumulate_dw (passes are added in fp32 and rounded once).  Either gradient may be NULL; without both the call scores only.
  * k from 1 to 256; N from 1.  Bit-reproducible from run to run; no host synchronisation.
@@ -534,7 +535,8 @@ int mrl_distill_loss_fwd_bwd(const void* hidden /*[N,d] dev*/, const void* lm_he
  *   table, y, dy, dtable: MRL_F32 or MRL_BF16 each; products and sums are in fp32 and rounded once.  accumulate = 1 needs a float
  *   out_dtable.  A token with an id outside [0, V) (-1 for none, say) or with mask 0 is none: its row of y is zero, its row of dy is not
  *   read and adds nothing.  Any d from 1 to 2^20, any alignment that the types have; V to 2^24.  N = 0: (11) is a no-op, (12) clears the table or
- *   leaves it.  N to 2^30 in (11), to 2^24 in (12) (more tokens: several calls, all but the first with accumulate).
+ *   leaves it.  N to 2^30 in (11), to 2^24 in (12) (more tokens: several calls, all but the first with accumulate;
+ *   of narrow rows and more than 2^22 tokens several calls take less, since the sort's time grows faster than N).
  *   (12) adds the rows of a token in the order of n, in a fixed grouping: bit-reproducible.  out_dtable must not overlap dy.
  * ---------------------------------------------------------------------- */
 int mrl_embedding(const void* table /*[V,d] dev*/, const int32_t* ids /*[N] dev*/, const uint8_t* token_mask /*[N] dev | NULL*/, int64_t N,

@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void k_distill_logits(DistillArgs a) {
 // Behind the forward launch: what its clamp hides.  Exponentials are clamped at 2^kStashClamp2, and so are those of NaN and +infinity, which would pass for logits far
 // above the alternatives'.  A workgroup per partial sum, those of kPartialRows rows of the head: where a token's reaches the clamp and the rows hold anything that is not finite, that
 // token's sum is NaN.  The head is read at clamped sums only, once at most.  (Finite logits that reach the clamp beside such an entry: their row is saturated, and NaN with it.)
-// (A call of 200 rows, V = 151936, d = 1536 425 us without it and 429 with; of 900, V = 50257 325 and 330; of 8192, d = 4096 21150 and 21170.)
+// (It takes 5 us of 200 rows and of 900, 19 of 8192, V = 151936: 39 MB.  A call of 200 rows, d = 1536 425 us without it and 429 with; of 900, V = 50257, d = 712 325 and 330.)
 constexpr int kPartialRows = 128;
 __global__ __launch_bounds__(256) void k_distill_hidden_nan(DistillArgs a) {
   const int nvalid = valid_rows(a.n_scored, a.chunk_start, a.chunk_rows);
@@ -434,6 +434,8 @@ void launch_distill_rows(const DistillArgs& a, hipStream_t stream) {
 }
 int distill_row_blocks(int chunk_rows) { return chunk_rows / kRows; }
 int distill_f32_blocks(int64_t rows) { return (int)((rows + 3) / 4); }
+// Rows of up to 512 logits stay in registers, eight to a lane (call, d = 64, k = 16, us, so and with every look from memory: 256 rows, V = 64 28.3 and 28.2, 300 30.2 and 30.9,
+// 512 32.4 and 33.7; 2048 rows of 512 69.0 and 69.7).  Sixteen to a lane would do the same for longer ones (256 rows, V = 1000 40.0 for 43.1) and cost a little here (64 rows, V = 512 30.8 and 31.3).
 void launch_distill_f32(const DistillArgs& a, int rows, hipStream_t stream) {
   const auto kernel = a.V <= 8 * 64 ? by_count(a.k, k_distill_f32<1, 8>, k_distill_f32<2, 8>, k_distill_f32<4, 8>)
                                     : by_count(a.k, k_distill_f32<1, 0>, k_distill_f32<2, 0>, k_distill_f32<4, 0>);

@@ -149,7 +149,8 @@ __global__ __launch_bounds__(kSortThreads) void k_sort_count(SortArgs a, int pas
   if (pass == 0 && a.used != nullptr) clear_marks(a, (int64_t)blockIdx.x * kSortThreads + threadIdx.x, (int64_t)gridDim.x * kSortThreads);
 }
 
-// A pass: every item to its place by the pass's digit, equal ones in their order.  The first reads the tokens and marks them.
+// A pass: every item to its place by the pass's digit, equal ones in their order.  The first reads the tokens and marks them.  Every workgroup adds up the counts of all, which saves a
+// launch and grows with the square of N (V = 151936, d = 8 in bf16, us: 2^18 tokens 82, 2^20 172, 2^22 696, 2^24 4830).
 __global__ __launch_bounds__(kSortThreads) void k_sort_pass(SortArgs a, int pass) {
   __shared__ SortShared sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, shift = pass * kDigitBits;

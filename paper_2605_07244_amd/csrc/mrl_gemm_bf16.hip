@@ -2129,7 +2129,8 @@ size_t gemm_tail_bytes_least(size_t head_bytes) { return (size_t)gemm_tail_items
 // few rows and the large tile: V = 151936, d = 1536 (3564 tiles of 256) 300 rows 305 and 300, 600 rows 371 and 358, 1000 rows 520 and 470; V = 128256, d = 3584 (7014) 457 and 462, 640 and 600,
 // 930 and 830; V = 32000, d = 4096 (2000) 145 and 161, 183 and 194, 270 and 281; V = 50257, d = 2048 (1576) 114 and 140, 163 and 201, 226 and 262.
 constexpr int kFewDw16Tiles = 8 * kRound;
-// (256 workgroups over 64 tiles of columns at most: 65 of them would leave a quarter without work)
+// (256 workgroups over 64 tiles of columns at most: 65 of them would leave a quarter without work.  Of one or some dozen rows dw_few_bf16 may be faster, a float dW of one row by 3 % with
+// V = 50257, d = 2048 and by 9 with V = 128256, d = 3584, and slower by 5 and 7 with V = 151936, d = 1536 and 4096; from 200 rows on it is slower by 30 % and more.  One rule for all of them.)
 bool dw_can_be_resident(int chunk_rows, int d, int overwrite) { return overwrite && chunk_rows <= G_ROWS && d <= 64 * GN; }
 bool dw_rows_in_blocks(int rows, int V, int d, bool dw_bf16) {
   return rows <= kFewDwRows && !(dw_bf16 && (int64_t)tiles(V, RES) * tiles(d, RES) >= kFewDw16Tiles);
